@@ -67,9 +67,12 @@ enum {
   TV_STATUS_TIMEOUT = 32u,     /* a bounded device wait gave up (not expected; the tree's
                                   outputs are -1) */
   TV_STATUS_BAD_ROW = 64u,     /* a target row the traversal needed has no finite logit */
-  TV_STATUS_DRAFT_EXHAUSTED = 128u  /* tv_draft_children: a node had more children than
+  TV_STATUS_DRAFT_EXHAUSTED = 128u, /* tv_draft_children: a node had more children than
                                        tokens of positive draft probability left (or a
                                        row without positive finite mass) */
+  TV_STATUS_BAD_SLOT = 256u,   /* a context slot outside [0, slots): the row is processed
+                                  without a context, the update is dropped */
+  TV_STATUS_BAD_MASK = 512u    /* a mask index outside [-1, n_masks): the row is not masked */
 };
 
 /* Flags for tv_create.  At most one path flag may be given; with none the
@@ -309,6 +312,147 @@ int tv_verify_batch_stats(tv_handle* h, int B, int N, const int32_t* parents,
                           const float* row_stats, int32_t* out_accepted_path,
                           int32_t* out_accept_len, int32_t* out_bonus_token, float* out_node_p,
                           int32_t* out_stats, void* cuda_stream);
+
+/*
+ * Serving steps between the target model's last layer and verification, for 8-bit
+ * checkpoints and requests with penalties, biases or grammars (no counterpart in the
+ * paper, whose method takes the target's logits as given).  "e4m3" is the 8-bit
+ * floating-point format with 4 exponent and 3 mantissa bits and no infinities (largest
+ * value 448); a group is 128 consecutive columns, the last one of a row may be shorter.
+ *
+ * tv_rms_norm -- the final root-mean-square norm of M rows with the residual's addition:
+ *     h = x + residual;  y = h * weight / sqrt(mean(h^2) + eps)
+ * in fp32, each output rounded once.
+ *   K              columns; K % 8 == 0, 8 <= K <= 65536.
+ *   dtype          element type of x, residual and out_residual.
+ *   x, residual    [M][K], 16-byte aligned; residual may be NULL (h = x).
+ *   weight         [K] of type weight_dtype, 16-byte aligned.
+ *   eps            finite and > 0.
+ *   out_residual   [M][K] h; may be x or residual (in place), or NULL.
+ *   out            [M][K], 16-byte aligned: bf16 where out_scales is NULL, else e4m3
+ *                  (y / scale to the nearest, ties to even).
+ *   out_scales     [M][ceil(K / 128)] fp32: max(max |y| of the group, 2^-100) / 448; NULL
+ *                  for bf16 output.  A group with an infinity or NaN has such a scale.
+ * The handle gives the device only (its sizes do not bound M).  M = 0 is a no-op.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CUDA.
+ */
+int tv_rms_norm(tv_handle* h, int M, int K, tv_dtype dtype, const void* x, const void* residual,
+                tv_dtype weight_dtype, const void* weight, float eps, void* out_residual,
+                void* out, float* out_scales, void* cuda_stream);
+
+/*
+ * tv_quantize_weight -- an output embedding in e4m3 with one scale for each block of 128
+ * rows and 128 columns (the last ones may be smaller), the weight of tv_lm_head_scaled.
+ *   rows, K     K % 16 == 0, K >= 16.
+ *   weight      [rows][K] of type dtype, 16-byte aligned.
+ *   out         [rows][K] e4m3, 16-byte aligned.
+ *   out_scales  [ceil(rows / 128)][ceil(K / 128)] fp32, as tv_rms_norm's.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CUDA.
+ */
+int tv_quantize_weight(tv_handle* h, int rows, int K, tv_dtype dtype, const void* weight,
+                       void* out, float* out_scales, void* cuda_stream);
+
+/*
+ * tv_lm_head_scaled -- tv_lm_head on e4m3 operands with block scales:
+ *     l[i][v] = sum over groups g of hidden_scales[i][g] weight_scales[v / 128][g]
+ *               * (sum over k in g of hidden[i][k] weight[v][k])
+ * in fp32, rounded once to bf16.
+ *   M, K            as tv_lm_head, K % 16 == 0, K >= 16.
+ *   hidden          [M][K] e4m3, 16-byte aligned; hidden_scales [M][ceil(K / 128)] fp32
+ *                   (tv_rms_norm writes both).
+ *   weight          [V][K] e4m3, 16-byte aligned; weight_scales
+ *                   [ceil(V / 128)][ceil(K / 128)] fp32 (tv_quantize_weight).
+ *   out_logits      [M][V] bf16, 16-byte aligned.
+ *   out_row_stats   [M][2] fp32 (max, sum), 8-byte aligned, of the stored logits at
+ *                   `temperature`; NULL for the logits alone (temperature is then unused).
+ * The handle must have been created for bf16 logits; any V.  The first call with row
+ * statistics allocates the handle's scratch for max_batch * (max_nodes + 1) rows.
+ * Errors: as tv_lm_head.
+ */
+int tv_lm_head_scaled(tv_handle* h, int M, int K, const void* hidden,
+                      const float* hidden_scales, const void* weight,
+                      const float* weight_scales, float temperature, void* out_logits,
+                      float* out_row_stats, void* cuda_stream);
+
+/*
+ * A token context: what the texts of up to `slots` requests add up to, in device arrays
+ * that the caller owns (the struct itself is read on the host during a call).
+ *   counts  [slots][V]: times token x was generated << 1 | 1 if x is in the prompt.
+ *   bias    [slots][V] fp32, added to the logit.
+ *   marks   [slots][ceil(V / 32)]: bit x % 32 of word x / 32 is set for every token with
+ *           a count, a prompt bit or a bias (it may be set for others); a token
+ *           without its bit is taken to have none.
+ * All zeros is an empty context.
+ */
+typedef struct {
+  int32_t slots;
+  uint32_t* counts;
+  float* bias;
+  uint32_t* marks;
+} tv_context;
+
+/* What tv_context_add adds. */
+enum { TV_CONTEXT_PROMPT = 0, TV_CONTEXT_GENERATED = 1, TV_CONTEXT_BIAS = 2 };
+
+/*
+ * tv_context_clear -- empties n slots (slots [n] int32, device).
+ * tv_context_add -- adds tokens [B][n] int32 to B requests (negative entries are
+ *   skipped): as prompt tokens, as generated ones, or with values [B][n] fp32 as their
+ *   biases (a token given twice in one call keeps either value; values is NULL for the
+ *   other kinds).
+ * tv_context_accept -- adds what a verification accepted: out_accepted_path [B][N] and
+ *   out_bonus_token [B] of tv_verify_batch with its draft_tokens [B][N+1]; a tree marked
+ *   invalid adds nothing.
+ * slots [B] int32 (device) gives each request's slot; NULL means request b uses slot b.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CUDA.  Bad slots and tokens are reported in the
+ * status word and skipped.
+ */
+int tv_context_clear(tv_handle* h, const tv_context* context, int n, const int32_t* slots,
+                     void* cuda_stream);
+int tv_context_add(tv_handle* h, const tv_context* context, int kind, int B, int n,
+                   const int32_t* slots, const int32_t* tokens, const float* values,
+                   void* cuda_stream);
+int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
+                      const int32_t* slots, const int32_t* draft_tokens, const int32_t* path,
+                      const int32_t* bonus, void* cuda_stream);
+
+/*
+ * tv_process_logits -- penalties for repeated tokens, biases and grammar masks on the
+ * logits of every tree row, and the rows' normalisers after them.  Row i has seen the
+ * request's context and the drafted tokens of the nodes on the path from the root to i
+ * (node i's own among them, the root's not: it belongs to the context).  With n = times
+ * generated + times on the path:
+ *     l = l > 0 ? l / repetition : l * repetition     where prompt bit or n > 0
+ *     l = l - frequency * n - presence                where n > 0
+ *     l = l + bias
+ *     l = -inf                                        where the row's mask bit is 0
+ * in fp32, rounded once to the handle's logit type.  N = 0 is the form for single tokens.
+ *   context        or NULL: only the path's tokens are penalised, no biases.
+ *   slots          as above (checked against B when NULL).
+ *   parents, draft_tokens  [B][N+1] as tv_verify_batch (a row whose path leaves the tree,
+ *                  or a token outside the vocabulary, is reported in the status word and
+ *                  the path taken without it); siblings may share a token here.
+ *   penalties      [B][3] fp32 (repetition > 0, frequency, presence); NULL means 1, 0, 0.
+ *   masks          [n_masks][ceil(V / 32)] words, bit x % 32 of word x / 32 set where token
+ *                  x is allowed; mask_index [B][N+1] int32 gives a row's mask, -1 for
+ *                  none.  Both NULL (n_masks = 0): no masks.
+ *   temperature    > 0, the temperature the normalisers are for.
+ *   logits         [B][N+1][V] of the handle's type, 16-byte aligned.
+ *   out_logits     same shape, 16-byte aligned; may be logits (in place), and must not
+ *                  overlap it in any other way.
+ *   out_row_stats  [B][N+1][2] fp32 (max, sum of 2^((l - max) log2(e) / T)), 8-byte
+ *                  aligned, of what is stored; a row whose mask leaves nothing gets
+ *                  (-inf, 0), which verification reports as TV_STATUS_BAD_ROW if it
+ *                  needs the row.
+ * The first call allocates the handle's scratch.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CAPACITY, TV_ERR_TEMPERATURE, TV_ERR_CUDA.
+ */
+int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
+                      const int32_t* slots, const int32_t* parents,
+                      const int32_t* draft_tokens, const float* penalties,
+                      const uint32_t* masks, const int32_t* mask_index, int n_masks,
+                      float temperature, const void* logits, void* out_logits,
+                      float* out_row_stats, void* cuda_stream);
 
 /*
  * tv_debug_withhold_job -- test hook for the failure path; no counterpart in

@@ -21,7 +21,11 @@ TV_STATUS = {
     "TIMEOUT": 32,
     "BAD_ROW": 64,
     "DRAFT_EXHAUSTED": 128,
+    "BAD_SLOT": 256,
+    "BAD_MASK": 512,
 }
+# columns (of a weight: and rows) of an 8-bit operand that share a scale
+GROUP = 128
 
 
 class LibraryError(RuntimeError):
@@ -43,6 +47,12 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
 
+
+class _Context(ctypes.Structure):
+    """tv_context of include/tv.h."""
+    _fields_ = [("slots", ctypes.c_int32), ("counts", _P), ("bias", _P), ("marks", _P)]
+
+
 _SIGS = {
     "tv_create": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, ctypes.c_uint]),
     "tv_verify_batch": (_I, [_P, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P]),
@@ -53,6 +63,13 @@ _SIGS = {
                                    _P]),
     "tv_lm_head": (_I, [_P, _I, _I, _P, _P, _F, _P, _P, _P]),
     "tv_draft_children": (_I, [_P, _I, _I, _P, _P, _P, _P, _P]),
+    "tv_rms_norm": (_I, [_P, _I, _I, _I, _P, _P, _I, _P, _F, _P, _P, _P, _P]),
+    "tv_quantize_weight": (_I, [_P, _I, _I, _I, _P, _P, _P, _P]),
+    "tv_lm_head_scaled": (_I, [_P, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P]),
+    "tv_context_clear": (_I, [_P, _P, _I, _P, _P]),
+    "tv_context_add": (_I, [_P, _P, _I, _I, _I, _P, _P, _P, _P]),
+    "tv_context_accept": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P]),
+    "tv_process_logits": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _I, _F, _P, _P, _P, _P]),
     "tv_last_host_copy_bytes": (_I, [_P, _P, _P]),
     "tv_get_status": (_I, [_P, ctypes.POINTER(ctypes.c_uint32)]),
     "tv_debug_withhold_job": (_I, [_P, _I]),
@@ -108,6 +125,13 @@ def _check_out(t, dtype, shape, device):
             or t.device != device:
         raise ValueError(f"output: expected a contiguous {dtype} {tuple(shape)} tensor on "
                          f"{device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _check_in(t, dtype, shape, device, name):
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() \
+            or t.device != device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} {shape} tensor on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class Verifier:
@@ -254,6 +278,150 @@ class Verifier:
             raise LibraryError("tv_draft_children", rc, self.lib)
         return tokens
 
+    def _float_code(self, t, name):
+        import torch
+        if t.dtype == torch.bfloat16:
+            return TV_BF16
+        if t.dtype == torch.float32:
+            return TV_FP32
+        raise ValueError(f"{name}: expected a bf16 or float32 tensor, got {t.dtype}")
+
+    def rms_norm(self, x, weight, residual=None, eps=1e-5, quantize=True, out=None, stream=None):
+        """Root-mean-square norm of the rows of x + residual (tv_rms_norm).
+        x, residual [M, K] bf16 or fp32 of one type, weight [K] bf16 or fp32.
+        Returns (values e4m3 [M, K], scales fp32 [M, ceil(K / 128)], residual) with
+        ``quantize``, else (values bf16 [M, K], residual); the last is x + residual in
+        x's type, None without a residual.  ``out`` gives the same tuple to write into
+        (its residual may be x or residual itself)."""
+        import torch
+        M, K = x.shape
+        code, wcode = self._float_code(x, "x"), self._float_code(weight, "weight")
+        _check_in(x, x.dtype, (M, K), self.device, "x")
+        _check_in(weight, weight.dtype, (K,), self.device, "weight")
+        if residual is not None:
+            _check_in(residual, x.dtype, (M, K), self.device, "residual")
+        kind = torch.float8_e4m3fn if quantize else torch.bfloat16
+        groups = (K + GROUP - 1) // GROUP
+        if out is None:
+            y = torch.empty(M, K, dtype=kind, device=self.device)
+            scales = torch.empty(M, groups, dtype=torch.float32, device=self.device) \
+                if quantize else None
+            total = torch.empty_like(x) if residual is not None else None
+        else:
+            y, scales, total = out if quantize else (out[0], None, out[1])
+            _check_out(y, kind, (M, K), self.device)
+            if quantize:
+                _check_out(scales, torch.float32, (M, groups), self.device)
+            if (total is None) != (residual is None):
+                raise ValueError("output: a residual is written where one is given")
+            if total is not None:
+                _check_out(total, x.dtype, (M, K), self.device)
+        rc = self.lib.tv_rms_norm(self.handle, M, K, code, _ptr(x), _ptr(residual), wcode,
+                                  _ptr(weight), float(eps), _ptr(total), _ptr(y), _ptr(scales),
+                                  _stream_ptr(stream))
+        if rc != 0:
+            raise LibraryError("tv_rms_norm", rc, self.lib)
+        return (y, scales, total) if quantize else (y, total)
+
+    def quantize_weight(self, weight, out=None, stream=None):
+        """(values e4m3 [rows, K], scales fp32 [ceil(rows / 128), ceil(K / 128)]) of a bf16
+        or fp32 weight [rows, K], one scale per 128 x 128 block (tv_quantize_weight)."""
+        import torch
+        rows, K = weight.shape
+        code = self._float_code(weight, "weight")
+        _check_in(weight, weight.dtype, (rows, K), self.device, "weight")
+        blocks = ((rows + GROUP - 1) // GROUP, (K + GROUP - 1) // GROUP)
+        if out is None:
+            q = torch.empty(rows, K, dtype=torch.float8_e4m3fn, device=self.device)
+            scales = torch.empty(blocks, dtype=torch.float32, device=self.device)
+        else:
+            q, scales = out
+            _check_out(q, torch.float8_e4m3fn, (rows, K), self.device)
+            _check_out(scales, torch.float32, blocks, self.device)
+        rc = self.lib.tv_quantize_weight(self.handle, rows, K, code, _ptr(weight), _ptr(q),
+                                         _ptr(scales), _stream_ptr(stream))
+        if rc != 0:
+            raise LibraryError("tv_quantize_weight", rc, self.lib)
+        return q, scales
+
+    def lm_head_fp8(self, hidden, hidden_scales, weight, weight_scales, temperature=None,
+                    out=None, stream=None):
+        """lm_head() on e4m3 operands with block scales (tv_lm_head_scaled): hidden [M, K] with
+        scales [M, ceil(K / 128)] (rms_norm), weight [V, K] with scales
+        [ceil(V / 128), ceil(K / 128)] (quantize_weight).  Returns (logits [M, V] bf16,
+        row_stats [M, 2] fp32); without a temperature the latter is None and not
+        computed.  ``out`` = (logits, row_stats)."""
+        import torch
+        M, K = hidden.shape
+        V, groups = self.vocab, (K + GROUP - 1) // GROUP
+        _check_in(hidden, torch.float8_e4m3fn, (M, K), self.device, "hidden")
+        _check_in(hidden_scales, torch.float32, (M, groups), self.device, "hidden_scales")
+        _check_in(weight, torch.float8_e4m3fn, (V, K), self.device, "weight")
+        _check_in(weight_scales, torch.float32, ((V + GROUP - 1) // GROUP, groups), self.device,
+                  "weight_scales")
+        if out is None:
+            logits = torch.empty(M, V, dtype=torch.bfloat16, device=self.device)
+            row_stats = torch.empty(M, 2, dtype=torch.float32, device=self.device) \
+                if temperature is not None else None
+        else:
+            logits, row_stats = out
+            _check_out(logits, torch.bfloat16, (M, V), self.device)
+            if (row_stats is None) != (temperature is None):
+                raise ValueError("output: row_stats are written where a temperature is given")
+            if row_stats is not None:
+                _check_out(row_stats, torch.float32, (M, 2), self.device)
+        rc = self.lib.tv_lm_head_scaled(
+            self.handle, M, K, _ptr(hidden), _ptr(hidden_scales), _ptr(weight),
+            _ptr(weight_scales), float(temperature) if temperature is not None else 0.0,
+            _ptr(logits), _ptr(row_stats), _stream_ptr(stream))
+        if rc != 0:
+            raise LibraryError("tv_lm_head_scaled", rc, self.lib)
+        return logits, row_stats
+
+    def process_logits(self, context, parents, tokens, logits, temperature, slots=None,
+                       penalties=None, masks=None, mask_index=None, out=None, stream=None):
+        """Penalties, biases and grammar masks on the logits of every tree row, and the
+        rows' normalisers after them (tv_process_logits).  context: a TokenContext or
+        None; parents, tokens [B, N+1] int32; logits [B, N+1, V]; slots [B] int32 (None:
+        request b is slot b); penalties [B, 3] fp32 (repetition, frequency, presence);
+        masks [n, ceil(V / 32)] int32 (a set bit allows the token) with mask_index
+        [B, N+1] int32 (-1: none).  Returns (logits [B, N+1, V], row_stats [B, N+1, 2]
+        fp32), which verify_stats() takes; ``out`` the same to write into (its logits may
+        be ``logits``)."""
+        import torch
+        B, R = parents.shape
+        V = self.vocab
+        _check_in(parents, torch.int32, (B, R), self.device, "parents")
+        _check_in(tokens, torch.int32, (B, R), self.device, "tokens")
+        _check_in(logits, self.logit_dtype, (B, R, V), self.device, "logits")
+        if slots is not None:
+            _check_in(slots, torch.int32, (B,), self.device, "slots")
+        if penalties is not None:
+            _check_in(penalties, torch.float32, (B, 3), self.device, "penalties")
+        n_masks = 0
+        if (masks is None) != (mask_index is None):
+            raise ValueError("masks and mask_index go together")
+        if masks is not None:
+            n_masks = masks.shape[0]
+            _check_in(masks, torch.int32, (n_masks, (V + 31) // 32), self.device, "masks")
+            _check_in(mask_index, torch.int32, (B, R), self.device, "mask_index")
+        if context is not None and (context.vocab != V or context.device != self.device):
+            raise ValueError("the context is for another vocabulary or device")
+        if out is None:
+            res = torch.empty_like(logits)
+            row_stats = torch.empty(B, R, 2, dtype=torch.float32, device=self.device)
+        else:
+            res, row_stats = out
+            _check_out(res, self.logit_dtype, (B, R, V), self.device)
+            _check_out(row_stats, torch.float32, (B, R, 2), self.device)
+        rc = self.lib.tv_process_logits(
+            self.handle, context.ref if context is not None else None, B, R - 1, _ptr(slots),
+            _ptr(parents), _ptr(tokens), _ptr(penalties), _ptr(masks), _ptr(mask_index), n_masks,
+            float(temperature), _ptr(logits), _ptr(res), _ptr(row_stats), _stream_ptr(stream))
+        if rc != 0:
+            raise LibraryError("tv_process_logits", rc, self.lib)
+        return res, row_stats
+
     def verify_stats(self, parents, tokens, logits, drafts, temperature, uniforms, row_stats,
                      out=None, stream=None, debug=False):
         """verify() with the rows' normalisers given ([B, N+1, 2] or [B*(N+1), 2]
@@ -344,3 +512,78 @@ class Verifier:
         if rc != 0:
             raise LibraryError("tv_get_status", rc, self.lib)
         return v.value
+
+
+class TokenContext:
+    """What the texts of up to ``slots`` requests add up to (tv_context): per slot and
+    token the count of generated occurrences and a prompt bit (``counts`` [slots, V]
+    int32: count << 1 | prompt), a bias (``bias`` [slots, V] fp32) and a bit in ``marks``
+    [slots, ceil(V / 32)] int32 for every token that has any.  Empty when created
+    without arrays.  Its updates run on the given (default: current) stream."""
+
+    def __init__(self, verifier, slots, counts=None, bias=None, marks=None):
+        import torch
+        self.verifier, self.slots = verifier, slots
+        self.vocab, self.device = verifier.vocab, verifier.device
+        V, dev = self.vocab, self.device
+        words = (V + 31) // 32
+        self.counts = torch.zeros(slots, V, dtype=torch.int32, device=dev) \
+            if counts is None else counts
+        self.bias = torch.zeros(slots, V, dtype=torch.float32, device=dev) if bias is None \
+            else bias
+        self.marks = torch.zeros(slots, words, dtype=torch.int32, device=dev) if marks is None \
+            else marks
+        _check_in(self.counts, torch.int32, (slots, V), dev, "counts")
+        _check_in(self.bias, torch.float32, (slots, V), dev, "bias")
+        _check_in(self.marks, torch.int32, (slots, words), dev, "marks")
+        self.struct = _Context(slots, self.counts.data_ptr(), self.bias.data_ptr(),
+                               self.marks.data_ptr())
+        self.ref = ctypes.cast(ctypes.pointer(self.struct), _P)
+
+    def _slots(self, slots, B):
+        import torch
+        if slots is not None:
+            _check_in(slots, torch.int32, (B,), self.device, "slots")
+        return _ptr(slots)
+
+    def _call(self, name, *args):
+        rc = getattr(self.verifier.lib, name)(self.verifier.handle, self.ref, *args)
+        if rc != 0:
+            raise LibraryError(name, rc, self.verifier.lib)
+
+    def clear(self, slots, stream=None):
+        """Empties the given slots ([n] int32, distinct)."""
+        self._call("tv_context_clear", slots.numel(), self._slots(slots, slots.numel()),
+                   _stream_ptr(stream))
+
+    def _add(self, kind, tokens, values, slots, stream):
+        import torch
+        B, n = tokens.shape
+        _check_in(tokens, torch.int32, (B, n), self.device, "tokens")
+        if values is not None:
+            _check_in(values, torch.float32, (B, n), self.device, "values")
+        self._call("tv_context_add", kind, B, n, self._slots(slots, B), _ptr(tokens),
+                   _ptr(values), _stream_ptr(stream))
+
+    def add_prompt(self, tokens, slots=None, stream=None):
+        """Prompt tokens [B, n] int32 of B requests; negative entries are skipped."""
+        self._add(0, tokens, None, slots, stream)
+
+    def add_generated(self, tokens, slots=None, stream=None):
+        """Generated tokens [B, n] int32; negative entries are skipped."""
+        self._add(1, tokens, None, slots, stream)
+
+    def set_bias(self, tokens, values, slots=None, stream=None):
+        """Biases values [B, n] fp32 of tokens [B, n] int32 (each token once)."""
+        self._add(2, tokens, values, slots, stream)
+
+    def accept(self, tokens, path, bonus, slots=None, stream=None):
+        """Adds what a verification accepted: draft tokens [B, N+1], and its path [B, N]
+        and bonus [B]."""
+        import torch
+        B, R = tokens.shape
+        _check_in(tokens, torch.int32, (B, R), self.device, "tokens")
+        _check_in(path, torch.int32, (B, R - 1), self.device, "path")
+        _check_in(bonus, torch.int32, (B,), self.device, "bonus")
+        self._call("tv_context_accept", B, R - 1, self._slots(slots, B), _ptr(tokens),
+                   _ptr(path), _ptr(bonus), _stream_ptr(stream))

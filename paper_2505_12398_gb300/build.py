@@ -22,8 +22,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtv.so")
 SOURCES = ["tv_api.cu", "tv_kernels.cu", "tv_tree.cu", "tv_flow.cu", "tv_noalloc.cu", "tv_gemm.cu",
            "tv_bonus.cu",
-           "tv_draft.cu"]
-HEADERS = ["tv_device.cuh", "tv_launch.h", "tv_ptx.cuh", "tv_control.cuh"]
+           "tv_draft.cu", "tv_gemm8.cu", "tv_norm.cu", "tv_logits.cu"]
+HEADERS = ["tv_device.cuh", "tv_launch.h", "tv_ptx.cuh", "tv_control.cuh", "tv_umma.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 

@@ -37,6 +37,9 @@ struct tv_handle {
   int withhold_tree = -1;        // test hook for the next persistent call (-1: none)
   // per-(row, tile) scratch of tv_lm_head (allocated on first use)
   float2* lmh_part = nullptr;
+  // the same of tv_lm_head_scaled, and per-(row, chunk) scratch of tv_process_logits
+  float2* lmh8_part = nullptr;
+  float2* proc_part = nullptr;
   // staging for tv_verify_batch_host (allocated on first use), and the bytes
   // its last call copied each way
   char* stage = nullptr;
@@ -213,6 +216,40 @@ bool capturing(cudaStream_t st) {
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+bool temperature_ok(float t) { return std::isfinite(t) && t > 0.f; }
+
+// log2(e) / T as c_hi + c_lo.
+void split_scale(float temperature, float* c_hi, float* c_lo) {
+  const double c = 1.4426950408889634 / static_cast<double>(temperature);
+  *c_hi = static_cast<float>(c);
+  *c_lo = static_cast<float>(c - static_cast<double>(*c_hi));
+}
+
+// Per-row scratch of `entries` partial normalisers, allocated on first use.
+bool scratch(float2** p, size_t entries) {
+  if (*p) return true;
+  if (entries == 0 || cudaMalloc(p, entries * sizeof(float2)) != cudaSuccess) {
+    cudaGetLastError();
+    *p = nullptr;
+    return false;
+  }
+  return true;
+}
+
+// A context's arrays; false where the struct cannot be one.
+bool context_args(const tv_context* c, ContextArgs* out) {
+  if (!c || c->slots < 1 || !c->counts || !c->bias || !c->marks || !aligned4(c->counts) ||
+      !aligned4(c->bias) || !aligned4(c->marks))
+    return false;
+  out->n_slots = c->slots;
+  out->counts = c->counts;
+  out->bias = c->bias;
+  out->marks = c->marks;
+  return true;
+}
 
 int check_call(const tv_handle* h, int B, int N, const void* parents, const void* tokens,
                const void* logits, const void* drafts, float temperature,
@@ -639,6 +676,178 @@ int tv_draft_children(tv_handle* h, int B, int N, const int32_t* parents,
   return rc == 0 ? TV_OK : TV_ERR_CUDA;
 }
 
+int tv_rms_norm(tv_handle* h, int M, int K, tv_dtype dtype, const void* x, const void* residual,
+                tv_dtype weight_dtype, const void* weight, float eps, void* out_residual,
+                void* out, float* out_scales, void* cuda_stream) {
+  NvtxRange range("tv_rms_norm");
+  if (!h || M < 0 || K < 8 || (K % 8) != 0 || K > tv_norm_max_columns())
+    return TV_ERR_INVALID_ARG;
+  if ((dtype != TV_BF16 && dtype != TV_FP32) ||
+      (weight_dtype != TV_BF16 && weight_dtype != TV_FP32))
+    return TV_ERR_INVALID_ARG;
+  if (!(std::isfinite(eps) && eps > 0.f)) return TV_ERR_INVALID_ARG;
+  if (M == 0) return TV_OK;
+  if (!x || !weight || !out || !aligned16(x) || !aligned16(residual) || !aligned16(weight) ||
+      !aligned16(out_residual) || !aligned16(out) || !aligned4(out_scales))
+    return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_rms_norm(M, K, dtype == TV_BF16, x, residual, weight_dtype == TV_BF16,
+                                    weight, eps, out_residual, out, out_scales,
+                                    static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_quantize_weight(tv_handle* h, int rows, int K, tv_dtype dtype, const void* weight,
+                       void* out, float* out_scales, void* cuda_stream) {
+  NvtxRange range("tv_quantize_weight");
+  if (!h || rows < 0 || K < 16 || (K % 16) != 0) return TV_ERR_INVALID_ARG;
+  if (dtype != TV_BF16 && dtype != TV_FP32) return TV_ERR_INVALID_ARG;
+  // (one block of the grid for each 128 x 128 block)
+  if (((long long)rows + 127) / 128 * (((long long)K + 127) / 128) > 0x7fffffffll)
+    return TV_ERR_INVALID_ARG;
+  if (rows == 0) return TV_OK;
+  if (!weight || !out || !out_scales || !aligned16(weight) || !aligned16(out) ||
+      !aligned4(out_scales))
+    return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_quantize_weight(rows, K, dtype == TV_BF16, weight, out, out_scales,
+                                           static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_lm_head_scaled(tv_handle* h, int M, int K, const void* hidden,
+                      const float* hidden_scales, const void* weight,
+                      const float* weight_scales, float temperature, void* out_logits,
+                      float* out_row_stats, void* cuda_stream) {
+  NvtxRange range("tv_lm_head_scaled");
+  if (!h || M < 0 || K < 16 || (K % 16) != 0) return TV_ERR_INVALID_ARG;
+  if (h->dtype != TV_BF16) return TV_ERR_INVALID_ARG;
+  if ((size_t)M > (size_t)h->max_batch * (h->max_nodes + 1)) return TV_ERR_CAPACITY;
+  if (out_row_stats && !temperature_ok(temperature)) return TV_ERR_TEMPERATURE;
+  if (M == 0) return TV_OK;
+  if (!hidden || !hidden_scales || !weight || !weight_scales || !out_logits ||
+      !aligned16(hidden) || !aligned4(hidden_scales) || !aligned16(weight) ||
+      !aligned4(weight_scales) || !aligned16(out_logits) || !aligned8(out_row_stats))
+    return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  float c_hi = 0.f, c_lo = 0.f;
+  if (out_row_stats) {
+    if (!h->lmh8_part &&
+        !scratch(&h->lmh8_part, tv_lm_head_scaled_scratch(
+                                    (size_t)h->max_batch * (h->max_nodes + 1), h->vocab)))
+      return TV_ERR_CUDA;
+    split_scale(temperature, &c_hi, &c_lo);
+  }
+  const int rc = tv_launch_lm_head_scaled(
+      hidden, hidden_scales, weight, weight_scales, M, K, h->vocab, c_hi, c_lo, out_logits,
+      h->lmh8_part, reinterpret_cast<float2*>(out_row_stats), h->status,
+      static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_context_clear(tv_handle* h, const tv_context* context, int n, const int32_t* slots,
+                     void* cuda_stream) {
+  NvtxRange range("tv_context_clear");
+  ContextArgs c;
+  if (!h || !context_args(context, &c) || n < 0 || (n > 0 && !slots)) return TV_ERR_INVALID_ARG;
+  if (n == 0) return TV_OK;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_context_clear(c, n, slots, h->vocab, h->status,
+                                         static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_context_add(tv_handle* h, const tv_context* context, int kind, int B, int n,
+                   const int32_t* slots, const int32_t* tokens, const float* values,
+                   void* cuda_stream) {
+  NvtxRange range("tv_context_add");
+  ContextArgs c;
+  if (!h || !context_args(context, &c) || B < 0 || n < 0) return TV_ERR_INVALID_ARG;
+  if (kind < TV_CONTEXT_PROMPT || kind > TV_CONTEXT_BIAS ||
+      (kind == TV_CONTEXT_BIAS) != (values != nullptr) || (!slots && B > c.n_slots))
+    return TV_ERR_INVALID_ARG;
+  if (B == 0 || n == 0) return TV_OK;
+  if (!tokens || (long long)B * n > 0x7fffffffll) return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_context_add(c, kind, B, n, slots, tokens, values, h->vocab, h->status,
+                                       static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
+                      const int32_t* slots, const int32_t* draft_tokens, const int32_t* path,
+                      const int32_t* bonus, void* cuda_stream) {
+  NvtxRange range("tv_context_accept");
+  ContextArgs c;
+  if (!h || !context_args(context, &c) || B < 0 || N < 0) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch || N > h->max_nodes) return TV_ERR_CAPACITY;
+  if (!slots && B > c.n_slots) return TV_ERR_INVALID_ARG;
+  if (B == 0) return TV_OK;
+  if (!bonus || (N > 0 && (!draft_tokens || !path))) return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_context_accept(c, B, N, slots, draft_tokens, path, bonus, h->vocab,
+                                          h->status, static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
+                      const int32_t* slots, const int32_t* parents,
+                      const int32_t* draft_tokens, const float* penalties,
+                      const uint32_t* masks, const int32_t* mask_index, int n_masks,
+                      float temperature, const void* logits, void* out_logits,
+                      float* out_row_stats, void* cuda_stream) {
+  NvtxRange range("tv_process_logits");
+  if (!h || B < 0 || N < 0 || n_masks < 0) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch || N > h->max_nodes) return TV_ERR_CAPACITY;
+  if (!temperature_ok(temperature)) return TV_ERR_TEMPERATURE;
+  if (B == 0) return TV_OK;
+  ProcessArgs a = {};
+  if (context) {
+    ContextArgs c;
+    if (!context_args(context, &c) || (!slots && B > c.n_slots)) return TV_ERR_INVALID_ARG;
+    a.n_slots = c.n_slots;
+    a.counts = c.counts;
+    a.bias = c.bias;
+    a.marks = c.marks;
+  }
+  if (!parents || !draft_tokens || !logits || !out_logits || !out_row_stats ||
+      !aligned16(logits) || !aligned16(out_logits) || !aligned8(out_row_stats) ||
+      !aligned4(penalties) || !aligned4(masks))
+    return TV_ERR_INVALID_ARG;
+  if ((mask_index != nullptr) != (masks != nullptr) || (masks != nullptr) != (n_masks > 0))
+    return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  if (!h->proc_part &&
+      !scratch(&h->proc_part,
+               tv_process_scratch((size_t)h->max_batch * (h->max_nodes + 1), h->vocab)))
+    return TV_ERR_CUDA;
+  a.B = B;
+  a.N = N;
+  a.V = h->vocab;
+  a.slots = slots;
+  a.parents = parents;
+  a.tokens = draft_tokens;
+  a.penalties = penalties;
+  a.masks = masks;
+  a.mask_index = mask_index;
+  a.n_masks = n_masks;
+  a.logits = logits;
+  a.out = out_logits;
+  a.part = h->proc_part;
+  a.row_stats = reinterpret_cast<float2*>(out_row_stats);
+  split_scale(temperature, &a.c_hi, &a.c_lo);
+  a.status = h->status;
+  const int rc = tv_launch_process(a, h->dtype == TV_BF16, static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
 int tv_debug_withhold_job(tv_handle* h, int tree) {
   if (!h || tree < 0 || tree >= h->max_batch) return TV_ERR_INVALID_ARG;
   h->withhold_tree = tree;
@@ -722,6 +931,8 @@ int tv_destroy(tv_handle* h) {
     if (h->flow_ws) cudaFree(h->flow_ws);
     if (h->stage) cudaFree(h->stage);
     if (h->lmh_part) cudaFree(h->lmh_part);
+    if (h->lmh8_part) cudaFree(h->lmh8_part);
+    if (h->proc_part) cudaFree(h->proc_part);
     cudaGetLastError();
   }
   delete h;

@@ -72,12 +72,11 @@
 #include "tv_device.cuh"
 #include "tv_launch.h"
 #include "tv_ptx.cuh"
+#include "tv_umma.cuh"
 
 namespace tvk {
 namespace gemm {
 
-constexpr int kBM = 128;          // rows of a tile per CTA (TMEM lanes)
-constexpr int kBN = 256;          // columns of a tile at most (TMEM columns)
 constexpr int kBK = 64;           // K per stage: 128 bytes of bf16, one swizzle row
 constexpr int kUmmaK = 16;        // K per tcgen05.mma of kind::f16
 constexpr int kMaxStages = 8;
@@ -89,8 +88,6 @@ constexpr size_t kGroupBytes = 32u << 20;
 constexpr int kEpiWarps = 8;      // two per TMEM lane quarter
 constexpr int kThreads = 64 + 32 * kEpiWarps;   // TMA warp, MMA warp, epilogue warps
 constexpr uint32_t kRowBytes = kBK * 2;         // one row of a stage's operand tile
-constexpr int kAccBufs = 2;                     // accumulators in tensor memory
-constexpr uint32_t kTmemCols = kAccBufs * kBN;  // fp32: one column per output column
 constexpr size_t kSmemBytes = kRingBytes + 1024;   // + alignment slack
 
 // Instruction descriptor of tcgen05.mma kind::f16: fp32 accumulator (bits
@@ -99,68 +96,6 @@ constexpr size_t kSmemBytes = kRingBytes + 1024;   // + alignment slack
 __device__ __forceinline__ uint32_t instr_desc(int m, int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(m >> 4) << 24);
-}
-
-// Shared-memory matrix descriptor of a K-major operand tile written by TMA
-// with the 128-byte swizzle: start address >> 4 (bits 0-13), leading byte
-// offset (unused with this swizzle, set to 1; bits 16-29), stride byte offset
-// 1024 B >> 4 between groups of 8 rows (bits 32-45), descriptor version 1
-// (bit 46), swizzle mode 2 = 128 B (bits 61-63).  Tiles are 1024-byte aligned
-// (base offset 0).  Stepping K by 16 bf16 inside the swizzled 128-byte row
-// advances the start address by 32 bytes.
-__device__ __forceinline__ uint64_t smem_desc(const void* p) {
-  const uint64_t addr = smem_u32(p);
-  return ((addr >> 4) & 0x3FFFull) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         (1ull << 46) | (2ull << 61);
-}
-
-// 2-D tiled TMA load of box {x .. x+box0, y .. y+box1} (x in elements, a
-// multiple of 64 here, so 16-byte aligned) into this CTA's shared memory,
-// counted on the barrier at cluster address `bar` (kPair: the pair leader's).
-template <bool kPair>
-__device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y,
-                                            uint32_t bar) {
-  if constexpr (kPair)
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::"
-        "bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-  else
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-}
-
-// Row and column tile of the t-th tile in the kernel's order.
-__device__ __forceinline__ void tile_coords(int t, int m_tiles, int n_tiles, int group,
-                                            int& mt, int& nt) {
-  const int g = group > 0 && group < m_tiles ? group : m_tiles;
-  const int full = (m_tiles / g) * g * n_tiles;       // tiles in whole groups
-  if (t < full) {
-    const int grp = t / (g * n_tiles), r = t - grp * g * n_tiles;
-    mt = grp * g + r % g;
-    nt = r / g;
-  } else {
-    const int gt = m_tiles - (m_tiles / g) * g, r = t - full;
-    mt = (m_tiles / g) * g + r % gt;
-    nt = r / gt;
-  }
-}
-
-// True in one lane of a converged warp.  The loops around the tensor-core and TMA
-// instructions run in the whole warp with those instructions alone in the chosen
-// lane: their operands (descriptors, addresses, coordinates) then stay in the
-// warp's uniform registers, which the instructions read, instead of being moved
-// there one by one from a divergent lane's.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t p;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(p));
-  return p != 0;
 }
 
 template <bool kPair>
@@ -180,97 +115,6 @@ __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint64_t a, uint64_t 
         : "memory");
 }
 
-// Arrives on `bar` (kPair: on the barrier at that offset in both CTAs) once
-// every tcgen05.mma issued so far by this thread is done.
-template <bool kPair>
-__device__ __forceinline__ void umma_commit(uint64_t* bar) {
-  if constexpr (kPair)
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
-        " [%0], %1;" ::"r"(smem_u32(bar)),
-        "h"((uint16_t)3)
-        : "memory");
-  else
-    asm volatile(
-        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-            smem_u32(bar))
-        : "memory");
-}
-
-template <bool kPair>
-__device__ __forceinline__ void tmem_alloc(uint32_t* slot) {   // a whole warp (of each CTA)
-  if constexpr (kPair) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                     smem_u32(slot)),
-                 "r"(kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  } else {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
-                     smem_u32(slot)),
-                 "r"(kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-}
-
-template <bool kPair>
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr) {   // the allocating warp(s)
-  if constexpr (kPair)
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr),
-                 "r"(kTmemCols)
-                 : "memory");
-  else
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr),
-                 "r"(kTmemCols)
-                 : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() {
-  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-}
-__device__ __forceinline__ void tc_fence_after() {
-  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-}
-
-// 32 consecutive fp32 accumulator columns of this warp's 32 TMEM lanes (lane
-// i of the warp reads TMEM lane base + i): one row per thread.  The registers
-// hold the columns after tmem_wait only, which takes them through an asm
-// statement of its own so that no use of them precedes it.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
-        "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]),
-        "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
-        "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]),
-        "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]),
-        "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]),
-        "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-      :
-      : "memory");
-}
-
-__device__ __forceinline__ void st_global_32b(void* p, const uint32_t* w) {   // 32-byte aligned
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]),
-               "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity) ? 1 : 0) != 0;
-}
-
 // Launch shape: tile width, H rows a TMA box takes per CTA, ring stages.
 struct Shape {
   int bn, a_box, stages;
@@ -279,61 +123,6 @@ struct Shape {
     return (uint32_t)(pair ? bn / 2 : bn) * kRowBytes;
   }
 };
-
-// Rounds 32 accumulator columns of a row to bf16, stores the first n (a
-// multiple of 8) at dst (32-byte stores where `wide`: a 16-byte store writes
-// half a sector) and adds the stored values to the row's running (max, sum).
-__device__ __forceinline__ void store_and_sum(const uint32_t (&r)[32], __nv_bfloat16* dst, int n,
-                                              bool wide, float2 ch, float2 cl, float& m_run,
-                                              float& s_run) {
-  uint32_t packed[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const __nv_bfloat162 h =
-        __floats2bfloat162_rn(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1]));
-    packed[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-  if (wide && n >= 32) {
-    st_global_32b(dst, packed);
-    st_global_32b(dst + 16, packed + 8);
-  } else {
-    uint4* d4 = reinterpret_cast<uint4*>(dst);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (8 * i < n)
-        d4[i] = make_uint4(packed[4 * i], packed[4 * i + 1], packed[4 * i + 2],
-                           packed[4 * i + 3]);
-  }
-  // the maximum (exact on bf16 pairs) and the sum, two columns at a time;
-  // columns past the end count as -inf and weigh nothing
-  if (n < 32) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (2 * i >= n) packed[i] = 0xff80ff80u;   // two bf16 -inf
-  }
-  __nv_bfloat162 hm = *reinterpret_cast<const __nv_bfloat162*>(&packed[0]);
-#pragma unroll
-  for (int i = 1; i < 16; ++i)
-    hm = __hmax2(hm, *reinterpret_cast<const __nv_bfloat162*>(&packed[i]));
-  const float cm = fmaxf(__low2float(hm), __high2float(hm));
-  if (cm > m_run) {
-    if (m_run != TV_NEG_INF) s_run *= exp2_split(m_run - cm, 0.f, ch.x, cl.x);
-    m_run = cm;
-  }
-  const float2 mm = make_float2(-m_run, -m_run);
-  float2 acc[4];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    float2 d = __fadd2_rn(make_float2(bf16_lo(packed[i]), bf16_hi(packed[i])), mm);
-    d.x = fmaxf(d.x, -1.0e4f);      // -inf / NaN -> weight ~0
-    d.y = fmaxf(d.y, -1.0e4f);
-    float2 e = exp2_corrected_x2(d, ch, cl);
-    if (2 * i >= n) e = make_float2(0.f, 0.f);   // (n is even)
-    acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
-  }
-  const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
-  s_run += s2.x + s2.y;
-}
 
 // The tiles t = first, first + step, ... of l = H W^T (in the order of
 // tile_coords), stored as bf16, and each row's (max, sum of 2^((l - max) c))
@@ -621,33 +410,10 @@ __global__ void __launch_bounds__(kMergeThreads)
 
 namespace {
 
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                 const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, fetched once through the runtime (no link
-// dependency on the driver library).
-EncodeTiled encoder() {
-  static std::once_flag once;
-  static EncodeTiled fn = nullptr;
-  std::call_once(once, [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiled>(p);
-    else
-      cudaGetLastError();
-  });
-  return fn;
-}
-
 // Row-major bf16 [rows][K] as a 2-D tensor with 64 x box_rows boxes and the
 // 128-byte swizzle (rows past the end read as zeros).
 bool make_map(CUtensorMap* map, const void* base, int rows, int K, int box_rows) {
-  const EncodeTiled enc = encoder();
+  const tvk::gemm::EncodeTiled enc = tvk::gemm::encoder();
   if (!enc) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)K, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)K * 2};
@@ -764,6 +530,26 @@ int width_for(size_t M, int V, const GemmDevice& g) {
 
 }  // namespace
 
+int tv_launch_merge(const float2* part, int n_parts, int M, float c_hi, float c_lo, float2* out,
+                    cudaStream_t stream) {
+  using namespace tvk::gemm;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)M, 1, 1);
+  cfg.blockDim = dim3(kMergeThreads, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, lm_head_merge_kernel, part, n_parts, c_hi, c_lo, out) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return -5;
+  }
+  return 0;
+}
+
 size_t tv_lm_head_scratch(size_t rows, int V) {
   using namespace tvk::gemm;
   int device = 0;
@@ -821,19 +607,5 @@ int tv_launch_lm_head(const void* hidden, const void* weight, int M, int K, int 
     cudaGetLastError();
     return -5;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)M, 1, 1);
-  cfg.blockDim = dim3(kMergeThreads, 1, 1);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, lm_head_merge_kernel, (const float2*)part, n_tiles, c_hi,
-                         c_lo, row_stats) != cudaSuccess) {
-    cudaGetLastError();
-    return -5;
-  }
-  return 0;
+  return tv_launch_merge(part, n_tiles, M, c_hi, c_lo, row_stats, stream);
 }

@@ -164,3 +164,77 @@ int tv_launch_draft(const int32_t* parents, const float* drafts, const float* un
                     int32_t* tokens, int B, int N, int V, int sm_count, uint32_t* status,
                     cudaStream_t stream);
 
+
+// Partial normalisers part[M][n_parts] merged into out[M], queued behind the kernel
+// that writes them (tv_gemm.cu).  0 or -5 (launch failed).
+int tv_launch_merge(const float2* part, int n_parts, int M, float c_hi, float c_lo, float2* out,
+                    cudaStream_t stream);
+
+// ---- 8-bit LM head and its operands (tv_gemm8.cu, tv_norm.cu) ----
+
+// As tv_lm_head_scratch, for tv_launch_lm_head_scaled.
+size_t tv_lm_head_scaled_scratch(size_t rows, int V);
+// logits[M][V] (bf16) of e4m3 operands hidden[M][K] with a scale per 128 columns of a
+// row and weight[V][K] with a scale per 128 x 128 block; with row_stats, each row's
+// normaliser of what is stored (part then holds tv_lm_head_scaled_scratch(M, V)
+// entries).  Requires K % 16 == 0 and 16-byte aligned arrays.  0 or -5.
+int tv_launch_lm_head_scaled(const void* hidden, const float* hidden_scales, const void* weight,
+                             const float* weight_scales, int M, int K, int V, float c_hi,
+                             float c_lo, void* logits, float2* part, float2* row_stats,
+                             uint32_t* status, cudaStream_t stream);
+
+// Most columns of a row that the norm takes.
+int tv_norm_max_columns();
+// The norm of M rows of K columns (K % 8 == 0): out in e4m3 where out_scales is given,
+// else in bf16.  residual and out_residual may be null.  0 or -5.
+int tv_launch_rms_norm(int M, int K, int x_is_bf16, const void* x, const void* residual,
+                       int weight_is_bf16, const void* weight, float eps, void* out_residual,
+                       void* out, float* out_scales, cudaStream_t stream);
+// weight[V][K] (K % 16 == 0) in e4m3 with a scale per 128 x 128 block.  0 or -5.
+int tv_launch_quantize_weight(int V, int K, int is_bf16, const void* weight, void* out,
+                              float* out_scales, cudaStream_t stream);
+
+// ---- penalties, biases and masks on logits (tv_logits.cu) ----
+
+// What the requests' texts add up to, by slot.
+struct ContextArgs {
+  int n_slots;
+  uint32_t* counts;            // [n_slots][V] times generated << 1 | in the prompt
+  float* bias;                 // [n_slots][V]
+  uint32_t* marks;             // [n_slots][ceil(V / 32)] tokens with a count, bit or bias
+};
+
+struct ProcessArgs {
+  int B, N, V;
+  const int32_t* slots;        // [B] or nullptr: slot0 + b
+  int slot0;
+  int n_slots;
+  const uint32_t* counts;      // a context's arrays, or nullptr
+  const float* bias;
+  const uint32_t* marks;
+  const int32_t* parents;      // [B][N+1]
+  const int32_t* tokens;       // [B][N+1]
+  const float* penalties;      // [B][3] repetition, frequency, presence; or nullptr
+  const uint32_t* masks;       // [n_masks][ceil(V / 32)]
+  const int32_t* mask_index;   // [B][N+1] or nullptr
+  int n_masks;
+  const void* logits;          // [B][N+1][V]
+  void* out;
+  float2* part;                // tv_process_scratch(B (N+1), V) entries
+  float2* row_stats;           // [B][N+1]
+  float c_hi, c_lo;            // log2(e) / temperature
+  uint32_t* status;
+};
+
+// Partial normalisers (float2) that calls of up to `rows` rows need.
+size_t tv_process_scratch(size_t rows, int V);
+// 0 or -5 (launch failed), as for the three after it.
+int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, cudaStream_t stream);
+int tv_launch_context_clear(const ContextArgs& c, int n, const int32_t* slots, int V,
+                            uint32_t* status, cudaStream_t stream);
+int tv_launch_context_add(const ContextArgs& c, int kind, int B, int n, const int32_t* slots,
+                          const int32_t* tokens, const float* values, int V, uint32_t* status,
+                          cudaStream_t stream);
+int tv_launch_context_accept(const ContextArgs& c, int B, int N, const int32_t* slots,
+                             const int32_t* tokens, const int32_t* path, const int32_t* bonus,
+                             int V, uint32_t* status, cudaStream_t stream);
