@@ -33,11 +33,27 @@ constexpr int kUmmaK = 32;        // K per tcgen05.mma of kind::f8f6f4
 constexpr int kMaxStages = 8;
 constexpr size_t kRingBytes = 200u << 10;
 constexpr size_t kGroupBytes = 32u << 20;       // H bytes of a group of row tiles
-constexpr int kParts = 4;                       // epilogue warps per TMEM lane quarter
-constexpr int kEpiWarps = 4 * kParts;
-constexpr int kThreads = 64 + 32 * kEpiWarps;   // TMA warp, MMA warp, epilogue warps
-constexpr size_t kSmemBytes = kRingBytes + 1024;
-constexpr int kChunks = kBN / (32 * kParts);    // 32-column chunks of a thread at most
+constexpr int kParts = 2;                       // epilogue warps per TMEM lane quarter, one for
+constexpr int kEpiWarps = 4 * kParts;           // each half of the tile's columns
+constexpr int kThreads = 128 + 32 * kEpiWarps;  // TMA, scale and two MMA warps, epilogue
+constexpr int kScaleGroups = 8;                 // groups of K in a slot of scales
+constexpr int kScaleSlots = 4;
+constexpr int kRegsFew = 40, kRegsMany = 232;   // registers per thread after the split
+static_assert(128 * kRegsFew + 32 * kEpiWarps * kRegsMany <= kThreads * 168,
+              "the warpgroups' registers fit what the block was launched with");
+// The scales of one group: of a tile's rows, and of the weight block of each of its
+// 32-column chunks.
+struct Scales {
+  float row[kBM];
+  float chunk[kBN / 32];
+};
+constexpr size_t kSmemBytes =
+    kRingBytes + 1024 + (size_t)kScaleSlots * kScaleGroups * sizeof(Scales);
+constexpr int kHalf = 128;                      // columns of a product: a tile has one or two
+constexpr int kBufs = 4;                        // products in tensor memory
+constexpr int kHalves = kBN / kHalf;            // = 32-column chunks of a thread at most
+constexpr int kChunks = 4;                      // 32-column chunks of a thread
+static_assert(kHalf == 32 * kChunks * kParts / kHalves && kBufs * kHalf == (int)kTmemCols, "");
 
 // Instruction descriptor of tcgen05.mma kind::f8f6f4: fp32 accumulator (bits 4-5 =
 // 1), e4m3 A and B (bits 7-9, 10-12 = 0), both K-major, N >> 3 in bits 17-22, M >> 4
@@ -46,21 +62,130 @@ __device__ __forceinline__ uint32_t instr_desc(int m, int n) {
   return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
+// One group's product: four tcgen05.mma of 32 bytes of K each, the first from zero, on
+// descriptors (lo, hi) whose address field steps by 32 bytes.
 template <bool kPair>
-__device__ __forceinline__ void umma_e4m3(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc,
-                                          uint32_t accumulate) {
+__device__ __forceinline__ void issue(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                      uint32_t idesc) {
+#pragma unroll
+  for (int k = 0; k < kGroup / kUmmaK; ++k) {
+    const uint32_t off = (uint32_t)(k * kUmmaK) >> 4;
+    if constexpr (kPair)
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+          "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+          "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(tmem_d),
+          "r"(a_lo + off), "r"(b_lo + off), "r"(hi), "r"(idesc), "r"(k > 0 ? 1u : 0u)
+          : "memory");
+    else
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+          "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+          "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %4, p;\n\t}" ::"r"(tmem_d),
+          "r"(a_lo + off), "r"(b_lo + off), "r"(hi), "r"(idesc), "r"(k > 0 ? 1u : 0u)
+          : "memory");
+  }
+}
+
+// umma_commit on a barrier's shared-memory address.
+template <bool kPair>
+__device__ __forceinline__ void commit_to(uint32_t bar) {
   if constexpr (kPair)
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;" ::"r"(bar),
+        "h"((uint16_t)3)
         : "memory");
   else
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
         : "memory");
+}
+
+// Waits until the phase of the barrier at `bar` with this parity has completed, unless
+// an earlier wait gave up; whether none has.
+__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, bool ok) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  if (done) return ok;
+  for (uint32_t i = 0; ok && i < kSpinLimit; ++i) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "n"(kTrySuspendNs)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+
+// Arrives on the barrier at `bar` (kPair: an address in the leader) for a part of tensor
+// memory that tcgen05.wait::ld has read.  Nothing in memory is published with it, so the
+// arrive needs no release at cluster scope, whose fence took over 1500 clocks a group.
+template <bool kPair>
+__device__ __forceinline__ void arrive_read(uint32_t bar) {
+  if constexpr (kPair)
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+                 : "memory");
+  else
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// tmem_ld32 and tmem_wait of 16 columns.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+
+// sum[at .. at + 8) += s * (16 columns).
+__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], int at, const uint32_t (&r)[16],
+                                           float s) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    sum[at + i] =
+        __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])),
+                   make_float2(s, s), sum[at + i]);
+}
+
+// 4 bytes from global to shared memory, asynchronously.
+__device__ __forceinline__ void copy_async4(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src)
+               : "memory");
+}
+// Arrives on `bar` once this thread's copies so far have landed.
+__device__ __forceinline__ void copy_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar))
+               : "memory");
+}
+template <int kRegs>
+__device__ __forceinline__ void regs_fewer() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void regs_more() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
 // Launch shape: tile width, H rows a TMA box takes per CTA, ring stages.
@@ -75,14 +200,27 @@ struct Shape {
 // The widest stores that every row's 32-column chunks allow.
 enum { kStore2 = 0, kStore16 = 1, kStore32 = 2 };
 
-// Rounds 32 columns of a row to bf16 and stores the first n.
-__device__ __forceinline__ void store_row(const float2 (&a)[16], __nv_bfloat16* dst, int n,
-                                          int mode, uint32_t (&packed)[16]) {
+// 32 columns of a row, rounded to bf16.
+__device__ __forceinline__ void pack_row(const float2 (&a)[16], uint32_t (&packed)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a[i].x, a[i].y);
     packed[i] = *reinterpret_cast<const uint32_t*>(&h);
   }
+}
+
+// Keeps the compiler from working on these values before the running sums are there
+// (several chunks' exponentials at once take more registers than there are).
+__device__ __forceinline__ void in_order(uint32_t (&p)[16], float& m, float& s) {
+  asm volatile(""
+               : "+r"(p[0]), "+r"(p[1]), "+r"(p[2]), "+r"(p[3]), "+r"(p[4]), "+r"(p[5]),
+                 "+r"(p[6]), "+r"(p[7]), "+r"(p[8]), "+r"(p[9]), "+r"(p[10]), "+r"(p[11]),
+                 "+r"(p[12]), "+r"(p[13]), "+r"(p[14]), "+r"(p[15]), "+f"(m), "+f"(s));
+}
+
+// Stores the first n of 32 columns.
+__device__ __forceinline__ void store_row(const uint32_t (&packed)[16], __nv_bfloat16* dst, int n,
+                                          int mode) {
   if (mode == kStore32 && n >= 32) {
     st_global_32b(dst, packed);
     st_global_32b(dst + 16, packed + 8);
@@ -143,7 +281,8 @@ __device__ __forceinline__ void sum_row(uint32_t (&packed)[16], int n, float2 ch
 template <bool kPair, bool kStats>
 __global__ void __launch_bounds__(kThreads, 1)
     lm_head8_kernel(const __grid_constant__ CUtensorMap map_h,
-                    const __grid_constant__ CUtensorMap map_w, const float* __restrict__ h_scale,
+                    const __grid_constant__ CUtensorMap map_w,
+                    const __grid_constant__ CUtensorMap map_w1, const float* __restrict__ h_scale,
                     const float* __restrict__ w_scale, int M, int V, int K, Shape shape,
                     float c_hi, float c_lo, __nv_bfloat16* __restrict__ logits,
                     float2* __restrict__ part, int m_tiles, int n_tiles, int group, int store,
@@ -151,22 +290,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[kMaxStages];   // (kPair: the leader's are used)
   __shared__ __align__(8) uint64_t empty_bar[kMaxStages];
-  __shared__ __align__(8) uint64_t acc_full[kAccBufs];    // a group's product is ready
-  __shared__ __align__(8) uint64_t acc_empty[kAccBufs];   // it is read (kPair: the leader's)
+  __shared__ __align__(8) uint64_t acc_full[kBufs];       // a product is ready
+  __shared__ __align__(8) uint64_t acc_empty[kBufs];      // it is read (kPair: the leader's)
   __shared__ __align__(8) uint64_t drain_bar;
+  __shared__ __align__(8) uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots];
   __shared__ __align__(8) uint64_t ms_full[4], ms_empty[4];
   __shared__ float2 part_ms[kParts - 1][kBM];
   __shared__ uint32_t tmem_slot;
   __shared__ int failed;
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* smem = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  Scales* scales = reinterpret_cast<Scales*>(smem + kRingBytes);   // [slot][group]
 
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t rank = kPair ? cluster_rank() : 0u;
   const int first = kPair ? (int)blockIdx.x >> 1 : (int)blockIdx.x;
   const int step = kPair ? (int)gridDim.x >> 1 : (int)gridDim.x;
   const int tile_rows = kPair ? 2 * kBM : kBM;
-  const int bn = shape.bn, bn_own = kPair ? bn / 2 : bn;
+  const int bn = shape.bn;
+  // (kPair: each CTA holds half of the W rows of either product)
+  const int n_half[kHalves] = {min(bn, kHalf), max(bn - kHalf, 0)};
+  const int w_own = kPair ? n_half[0] / 2 : n_half[0];
   const uint32_t n_stages = (uint32_t)shape.stages;
   const uint32_t a_bytes = shape.a_bytes(), stage_bytes = a_bytes + shape.b_bytes(kPair);
   const int nkb = (K + kGroup - 1) / kGroup;
@@ -174,13 +318,17 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < n_stages; ++s) {
       mbar_init(&full_bar[s], 1);
-      mbar_init(&empty_bar[s], 1);
+      mbar_init(&empty_bar[s], bn > kHalf ? kHalves : 1);
     }
-    for (int k = 0; k < kAccBufs; ++k) {
+    for (int k = 0; k < kBufs; ++k) {
       mbar_init(&acc_full[k], 1);
-      mbar_init(&acc_empty[k], kPair ? 2 * kEpiWarps : kEpiWarps);
+      mbar_init(&acc_empty[k], (kPair ? 2 : 1) * kEpiWarps / kHalves);
     }
-    mbar_init(&drain_bar, 1);
+    mbar_init(&drain_bar, bn > kHalf ? kHalves : 1);
+    for (int k = 0; k < kScaleSlots; ++k) {
+      mbar_init(&scale_full[k], 32);
+      mbar_init(&scale_empty[k], bn > kHalf ? kEpiWarps : kEpiWarps / kHalves);
+    }
     for (int k = 0; k < 4; ++k) {
       mbar_init(&ms_full[k], kParts - 1);
       mbar_init(&ms_empty[k], 1);
@@ -196,182 +344,95 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = tmem_slot;
   asm volatile("griddepcontrol.launch_dependents;");
 
-  if (warp == 0) {
-    // ---- TMA producer: one ring across all of this CTA's tiles ----
-    uint32_t it = 0, s = 0, ph = 0;
-    bool ok = true;
-    for (int t = first; t < n_total && ok; t += step) {
-      int mt, nt;
-      tile_coords(t, m_tiles, n_tiles, group, mt, nt);
-      const int m0 = mt * tile_rows + (int)rank * kBM, n0 = nt * bn + (int)rank * bn_own;
-      for (int kb = 0; kb < nkb; ++kb, ++it) {
-        if (it >= n_stages && !wait_warp(&empty_bar[s], ph ^ 1u)) {
-          ok = false;
-          break;
-        }
-        uint8_t* a = smem + s * stage_bytes;
-        uint32_t bar = smem_u32(&full_bar[s]);
-        if constexpr (kPair) bar = map_shared(&full_bar[s], 0);
-        if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(&full_bar[s], kPair ? 2 * stage_bytes : stage_bytes);
-          tma_load_2d<kPair>(a, &map_h, kb * kGroup, m0, bar);
-          tma_load_2d<kPair>(a + a_bytes, &map_w, kb * kGroup, n0, bar);
-        }
-        __syncwarp();
-        if (++s == n_stages) { s = 0; ph ^= 1u; }
-      }
-    }
-    if (!ok) failed = 1;
-    if (rank == 0)      // the copies issued last have landed before the CTA may exit
-      for (uint32_t j = it > n_stages ? it - n_stages : 0u; j < it; ++j)
-        if (!wait_warp(&full_bar[j % n_stages], (j / n_stages) & 1)) failed = 1;
-  } else if (warp == 1) {
-    // ---- tensor-core issue: each group's product into the accumulators in turn ----
-    if (rank == 0) {
-      const uint32_t idesc = instr_desc(tile_rows, bn);
-      const uint64_t desc0 = smem_desc(smem);
-      uint32_t s = 0, ph = 0, g = 0;
-      bool ok = true;
-      for (int t = first; t < n_total && ok; t += step) {
-        for (int kb = 0; kb < nkb; ++kb, ++g) {
-          const uint32_t acc = g & 1u;
-          if (g >= kAccBufs) {
-            const uint32_t par = ((g >> 1) - 1) & 1;
-            const bool got = kPair ? mbar_wait_cluster(&acc_empty[acc], par)
-                                   : mbar_wait(&acc_empty[acc], par);
-            if (!__all_sync(0xffffffffu, got)) {
-              ok = false;
-              break;
-            }
-          }
-          if (!wait_warp(&full_bar[s], ph)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t d = tmem + acc * (uint32_t)kBN;
-          const uint64_t da = desc0 + (uint64_t)((s * stage_bytes) >> 4);
-          const uint64_t db = da + (uint64_t)(a_bytes >> 4);
-          if (elect_one()) {
-#pragma unroll
-            for (int k = 0; k < kGroup / kUmmaK; ++k) {
-              const uint64_t off = (uint64_t)((k * kUmmaK) >> 4);
-              umma_e4m3<kPair>(d, da + off, db + off, idesc, k > 0 ? 1u : 0u);
-            }
-            umma_commit<kPair>(&acc_full[acc]);
-            umma_commit<kPair>(&empty_bar[s]);
-          }
-          __syncwarp();
-          if (++s == n_stages) { s = 0; ph ^= 1u; }
-        }
-      }
-      if (!ok) failed = 1;
-      // every MMA issued has finished before tensor memory is freed
-      if (elect_one()) umma_commit<kPair>(&drain_bar);
-      __syncwarp();
-    }
-    // (kPair, the peer: the leader's last signal)
-    if (!wait_warp(&drain_bar, 0)) failed = 1;
-  } else {
-    // ---- scaled sums: one row per thread, every fourth 32-column chunk ----
+  if (warp >= 4) {
+    regs_more<kRegsMany>();
+    // ---- scaled sums: one row per thread, every other 32-column chunk ----
     const int q = warp & 3;                       // the TMEM lane quarter of this warp
-    const int mine = (warp - 2) >> 2;
+    const int mine = (warp - 4) >> 2;
     const float2 ch = make_float2(c_hi, c_hi), cl = make_float2(c_lo, c_lo);
-    const int w_blocks = (V + kGroup - 1) / kGroup;
-    uint32_t g = 0;
+    const int half = mine, col = kHalf * half;
+    const uint32_t full0 = smem_u32(&acc_full[half]);
+    uint32_t empty0 = smem_u32(&acc_empty[half]);
+    if constexpr (kPair) empty0 = map_shared(&acc_empty[half], 0);
+    uint32_t buf = 0, ph = 0, si = 0;             // the buffer of the next group, its phase
     int j = 0;
+    // A wait that gives up is reported and no longer waited for: the loops go on to
+    // their end (on whatever is there), so that no wait needs a way out of them.
     bool ok = true;
-    for (int t = first; t < n_total && ok; t += step, ++j) {
+    for (int t = first; t < n_total; t += step, ++j) {
       int mt, n_tile;
       tile_coords(t, m_tiles, n_tiles, group, mt, n_tile);
       const int n0 = n_tile * bn;
       const int row0 = mt * tile_rows + (int)rank * kBM + q * 32, row = row0 + lane;
       const bool live = row0 < M;                 // (the same in the whole warp)
-      const uint32_t tbase = tmem + ((uint32_t)(q * 32) << 16);
-      const float* sa = h_scale + (size_t)min(row, M - 1) * nkb;
-      const float* sw[kChunks];
+      const uint32_t tbase = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)col;
       float2 sum[kChunks][16];
-      float sa_next = __ldg(sa), sw_next[kChunks];
 #pragma unroll
-      for (int k = 0; k < kChunks; ++k) {
-        const int blk = min((n0 + 32 * (mine + kParts * k)) / kGroup, w_blocks - 1);
-        sw[k] = w_scale + (size_t)blk * nkb;
-        sw_next[k] = __ldg(sw[k]);
+      for (int k = 0; k < kChunks; ++k)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[k][i] = make_float2(0.f, 0.f);
-      }
-      for (int kb = 0; kb < nkb; ++kb, ++g) {
-        float s[kChunks];
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) s[k] = sa_next * sw_next[k];
-        if (kb + 1 < nkb) {                       // the next group's scales
-          sa_next = __ldg(sa + kb + 1);
-#pragma unroll
-          for (int k = 0; k < kChunks; ++k) sw_next[k] = __ldg(sw[k] + kb + 1);
-        }
-        const uint32_t acc = g & 1u;
-        if (!wait_warp(&acc_full[acc], (g >> 1) & 1)) {
-          if (lane == 0) failed = 1;
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-#pragma unroll
-        for (int k = 0; k < kChunks; ++k) {
-          const int c = 32 * (mine + kParts * k);
-          const bool last = k == kChunks - 1 || c + 32 * kParts >= bn;
-          if (c < bn) {                           // (the same in the whole warp)
-            uint32_t r[32];
+      if (n_half[half] > 0) {
+        for (int kb0 = 0; kb0 < nkb; kb0 += kScaleGroups, ++si) {
+          const uint32_t slot = si % kScaleSlots;
+          ok = wait_on(smem_u32(&scale_full[slot]), (si / kScaleSlots) & 1, ok);
+          const Scales* sc = scales + slot * kScaleGroups;
+          const Scales* end = sc + min(kScaleGroups, nkb - kb0);
+          for (; sc < end; ++sc) {
+            const float sa = sc->row[q * 32 + lane];
+            const float4 sw = *reinterpret_cast<const float4*>(&sc->chunk[kChunks * half]);
+            ok = wait_on(full0 + 16 * buf, ph, ok);
+            tc_fence_after();
             if (live) {
-              __syncwarp();
-              tmem_ld32(tbase + acc * (uint32_t)kBN + (uint32_t)c, r);
-              tmem_wait(r);
-            }
-            if (last) {       // all read: this accumulator may be overwritten
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) {
-                if constexpr (kPair) mbar_arrive_remote(map_shared(&acc_empty[acc], 0));
-                else mbar_arrive(&acc_empty[acc]);
+              // 16 columns are on their way from tensor memory while 16 are summed (all of
+              // a product's, whatever the tile's width: those past it are not stored)
+              uint32_t r[2][16];
+              const uint32_t at = tbase + 256 * buf;
+              const float scale[kChunks] = {sa * sw.x, sa * sw.y, sa * sw.z, sa * sw.w};
+              tmem_ld16(at, r[0]);
+#pragma unroll
+              for (int k = 0; k < 2 * kChunks; ++k) {
+                tmem_wait16(r[k & 1]);
+                if (k + 1 < 2 * kChunks) {
+                  tmem_ld16(at + 16 * (k + 1), r[(k + 1) & 1]);
+                } else {
+                  tc_fence_before();
+                  // (every lane's part is read: the load and its wait are the warp's)
+                  if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
+                }
+                scaled_sum(sum[k >> 1], 8 * (k & 1), r[k & 1], scale[k >> 1]);
               }
+            } else {
+              if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
             }
-            if (live) {
-              const float2 ss = make_float2(s[k], s[k]);
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                sum[k][i] = __ffma2_rn(
-                    make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), ss,
-                    sum[k][i]);
-            }
+            buf ^= 1u;
+            ph ^= buf ^ 1u;
           }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&scale_empty[slot]);
         }
       }
-      if (!ok) break;
       float m_run = TV_NEG_INF, s_run = 0.f;
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
-        const int c = 32 * (mine + kParts * k), col0 = n0 + c;
+        const int c = col + 32 * k, col0 = n0 + c;
         const int n = min(32, V - col0);          // columns of the chunk that exist
-        if (c < bn && row < M && n > 0) {
-          uint32_t packed[16];
-          store_row(sum[k], logits + (size_t)row * V + col0, n, store, packed);
-          if constexpr (kStats) sum_row(packed, n, ch, cl, m_run, s_run);
+        if (c >= bn || n <= 0) break;             // (the same in the whole warp)
+        uint32_t packed[16];
+        pack_row(sum[k], packed);
+        if (row < M) store_row(packed, logits + (size_t)row * V + col0, n, store);
+        if constexpr (kStats) {
+          in_order(packed, m_run, s_run);
+          sum_row(packed, n, ch, cl, m_run, s_run);
         }
       }
       if constexpr (kStats) {    // one partial per row and tile from the quarter's warps
         if (mine > 0) {
-          if (j > 0 && !wait_warp(&ms_empty[q], (j - 1) & 1)) {
-            if (lane == 0) failed = 1;
-            break;
-          }
+          if (j > 0) ok = wait_on(smem_u32(&ms_empty[q]), (j - 1) & 1, ok);
           part_ms[mine - 1][q * 32 + lane] = make_float2(m_run, s_run);
           __syncwarp();
           if (lane == 0) mbar_arrive(&ms_full[q]);
         } else {
-          if (!wait_warp(&ms_full[q], j & 1)) {
-            if (lane == 0) failed = 1;
-            break;
-          }
+          ok = wait_on(smem_u32(&ms_full[q]), j & 1, ok);
           float2 o[kParts - 1];
           float mx = m_run;
 #pragma unroll
@@ -390,6 +451,119 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
+    if (!ok) failed = 1;
+  } else {
+  regs_fewer<kRegsFew>();
+  if (warp == 0) {
+    // ---- TMA producer: one ring across all of this CTA's tiles ----
+    uint32_t it = 0, s = 0, ph = 0;
+    bool ok = true;
+    for (int t = first; t < n_total && ok; t += step) {
+      int mt, nt;
+      tile_coords(t, m_tiles, n_tiles, group, mt, nt);
+      const int m0 = mt * tile_rows + (int)rank * kBM, n0 = nt * bn + (int)rank * w_own;
+      const int n1 = nt * bn + kHalf + (int)rank * (n_half[1] / 2);
+      for (int kb = 0; kb < nkb; ++kb, ++it) {
+        if (it >= n_stages && !wait_warp(&empty_bar[s], ph ^ 1u)) {
+          ok = false;
+          break;
+        }
+        uint8_t* a = smem + s * stage_bytes;
+        uint32_t bar = smem_u32(&full_bar[s]);
+        if constexpr (kPair) bar = map_shared(&full_bar[s], 0);
+        if (elect_one()) {
+          if (rank == 0) mbar_arrive_expect_tx(&full_bar[s], kPair ? 2 * stage_bytes : stage_bytes);
+          tma_load_2d<kPair>(a, &map_h, kb * kGroup, m0, bar);
+          tma_load_2d<kPair>(a + a_bytes, &map_w, kb * kGroup, n0, bar);
+          if (kPair && n_half[1] > 0)
+            tma_load_2d<kPair>(a + a_bytes + w_own * kGroup, &map_w1, kb * kGroup, n1, bar);
+        }
+        __syncwarp();
+        if (++s == n_stages) { s = 0; ph ^= 1u; }
+      }
+    }
+    if (!ok) failed = 1;
+    if (rank == 0)      // the copies issued last have landed before the CTA may exit
+      for (uint32_t j = it > n_stages ? it - n_stages : 0u; j < it; ++j)
+        if (!wait_warp(&full_bar[j % n_stages], (j / n_stages) & 1)) failed = 1;
+  } else if (warp == 1 || warp == 3) {
+    // ---- tensor-core issue: each group's products into the accumulators in turn ----
+    // One warp for each half of the columns: a warp's own instructions (two waits, four
+    // products, two commits) take about 400 clocks a half, more than its products' 256.
+    const int half = warp >> 1;
+    if (rank == 0 && n_half[half] > 0) {
+      const uint32_t idesc = instr_desc(tile_rows, n_half[half]);
+      const uint64_t desc = smem_desc(smem);
+      const uint32_t desc_hi = (uint32_t)(desc >> 32), desc_lo = (uint32_t)desc;
+      const uint32_t b_off = (a_bytes + (uint32_t)(half * w_own * kGroup)) >> 4;
+      const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar);
+      const uint32_t acc_f = smem_u32(&acc_full[half]), acc_e = smem_u32(&acc_empty[half]);
+      const uint32_t d0 = tmem + (uint32_t)(kHalf * half);
+      uint32_t s = 0, lo = desc_lo, ph = 0;       // the stage, its descriptor, its phase
+      uint32_t buf = 0, aph = 1;                  // the buffer, its release's phase
+      bool ok = true;
+      const int tiles = first < n_total ? (n_total - first + step - 1) / step : 0;
+      for (int left = tiles * nkb; left > 0; --left) {
+        ok = wait_on(full0 + 8 * s, ph, ok);
+        // (the first use of a buffer waits for the phase before the first, which is over)
+        ok = wait_on(acc_e + 16 * buf, aph, ok);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        tc_fence_after();
+        if (elect_one()) {
+          issue<kPair>(d0 + 256 * buf, lo, lo + b_off, desc_hi, idesc);
+          commit_to<kPair>(acc_f + 16 * buf);
+          commit_to<kPair>(empty0 + 8 * s);
+        }
+        __syncwarp();
+        buf ^= 1u;
+        aph ^= buf ^ 1u;
+        lo += stage_bytes >> 4;
+        if (++s == n_stages) {
+          s = 0;
+          lo = desc_lo;
+          ph ^= 1u;
+        }
+      }
+      if (!ok) failed = 1;
+      // every MMA issued has finished before tensor memory is freed
+      if (elect_one()) umma_commit<kPair>(&drain_bar);
+      __syncwarp();
+    }
+    // (kPair, the peer: the leader's last signal)
+    if (!wait_warp(&drain_bar, 0)) failed = 1;
+  } else if (warp == 2) {
+    // ---- scales: a slot of groups ahead of the sums, straight to shared memory ----
+    const int w_blocks = (V + kGroup - 1) / kGroup;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int t = first; t < n_total && ok; t += step) {
+      int mt, nt;
+      tile_coords(t, m_tiles, n_tiles, group, mt, nt);
+      const int row0 = mt * tile_rows + (int)rank * kBM + lane, n0 = nt * bn;
+      const int blk = min((n0 + 32 * (lane & 7)) / kGroup, w_blocks - 1);
+      for (int kb0 = 0; kb0 < nkb; kb0 += kScaleGroups, ++it) {
+        const uint32_t slot = it % kScaleSlots;
+        if (it >= kScaleSlots && !wait_warp(&scale_empty[slot], ((it / kScaleSlots) - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        const int groups = min(kScaleGroups, nkb - kb0);
+#pragma unroll
+        for (int r = 0; r < kBM / 32; ++r) {
+          const float* src = h_scale + (size_t)min(row0 + 32 * r, M - 1) * nkb + kb0;
+          for (int k = 0; k < groups; ++k)
+            copy_async4(&scales[slot * kScaleGroups + k].row[lane + 32 * r], src + k);
+        }
+        for (int k = lane >> 3; k < groups; k += 4)
+          copy_async4(&scales[slot * kScaleGroups + k].chunk[lane & 7],
+                      w_scale + (size_t)blk * nkb + kb0 + k);
+        copy_async_arrive(&scale_full[slot]);
+      }
+    }
+    if (!ok) failed = 1;
+    // the copies issued last have landed before the CTA may exit
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  }
   }
   tc_fence_before();
   __syncthreads();
@@ -451,7 +625,8 @@ int tile_width(size_t m_tiles, int V, int units, int extra) {
 }
 
 template <bool kPair, bool kStats>
-cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const float* h_scale,
+cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w,
+                   const CUtensorMap& map_w1, const float* h_scale,
                    const float* w_scale, int M, int V, int K, const Shape& shape, float c_hi,
                    float c_lo, void* logits, float2* part, int m_tiles, int n_tiles, int group,
                    int units, uint32_t* status, cudaStream_t stream) {
@@ -471,7 +646,7 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w, const flo
   const int store = V % 8 ? kStore2
                     : V % 16 == 0 && (reinterpret_cast<uintptr_t>(logits) & 31u) == 0 ? kStore32
                                                                                      : kStore16;
-  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, h_scale, w_scale,
+  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, map_w1, h_scale, w_scale,
                             M, V, K, shape, c_hi, c_lo, static_cast<__nv_bfloat16*>(logits), part,
                             m_tiles, n_tiles, group, store, status);
 }
@@ -567,15 +742,17 @@ int tv_launch_lm_head_scaled(const void* hidden, const float* hidden_scales, con
   shape.bn = width_for(M, V, g);
   shape.stages = (int)std::min<size_t>(
       kMaxStages, kRingBytes / (shape.a_bytes() + shape.b_bytes(pair)));
-  CUtensorMap map_h, map_w;
+  CUtensorMap map_h, map_w, map_w1;
+  const int w1 = pair && shape.bn > kHalf ? (shape.bn - kHalf) / 2 : kHalf;
   if (!make_map(&map_h, hidden, M, K, shape.a_box) ||
-      !make_map(&map_w, weight, V, K, pair ? shape.bn / 2 : shape.bn))
+      !make_map(&map_w, weight, V, K, pair ? std::min(shape.bn, kHalf) / 2 : shape.bn) ||
+      !make_map(&map_w1, weight, V, K, w1))
     return -5;
   const int n_tiles = (V + shape.bn - 1) / shape.bn;
   const int group = (int)std::max<size_t>(1, kGroupBytes / ((size_t)tile_rows * K));
   auto run = pair ? (row_stats ? launch<true, true> : launch<true, false>)
                   : (row_stats ? launch<false, true> : launch<false, false>);
-  if (run(map_h, map_w, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo, logits, part,
+  if (run(map_h, map_w, map_w1, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo, logits, part,
           m_tiles, n_tiles, group, units, status, stream) != cudaSuccess) {
     cudaGetLastError();
     return -5;
