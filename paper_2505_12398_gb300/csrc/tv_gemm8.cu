@@ -33,13 +33,13 @@ constexpr int kUmmaK = 32;        // K per tcgen05.mma of kind::f8f6f4
 constexpr int kMaxStages = 8;
 constexpr size_t kRingBytes = 200u << 10;
 constexpr size_t kGroupBytes = 32u << 20;       // H bytes of a group of row tiles
-constexpr int kParts = 2;                       // epilogue warps per TMEM lane quarter, one for
+constexpr int kParts = 4;                       // epilogue warps per TMEM lane quarter, two for
 constexpr int kEpiWarps = 4 * kParts;           // each half of the tile's columns
 constexpr int kThreads = 128 + 32 * kEpiWarps;  // TMA, scale and two MMA warps, epilogue
 constexpr int kScaleGroups = 8;                 // groups of K in a slot of scales
 constexpr int kScaleSlots = 4;
-constexpr int kRegsFew = 40, kRegsMany = 232;   // registers per thread after the split
-static_assert(128 * kRegsFew + 32 * kEpiWarps * kRegsMany <= kThreads * 168,
+constexpr int kRegsFew = 32, kRegsMany = 112;   // registers per thread after the split
+static_assert(128 * kRegsFew + 32 * kEpiWarps * kRegsMany <= kThreads * 96,
               "the warpgroups' registers fit what the block was launched with");
 // The scales of one group: of a tile's rows, and of the weight block of each of its
 // 32-column chunks.
@@ -52,7 +52,7 @@ constexpr size_t kSmemBytes =
 constexpr int kHalf = 128;                      // columns of a product: a tile has one or two
 constexpr int kBufs = 4;                        // products in tensor memory
 constexpr int kHalves = kBN / kHalf;            // = 32-column chunks of a thread at most
-constexpr int kChunks = 4;                      // 32-column chunks of a thread
+constexpr int kChunks = 2;                      // 32-column chunks of a thread
 static_assert(kHalf == 32 * kChunks * kParts / kHalves && kBufs * kHalf == (int)kTmemCols, "");
 
 // Instruction descriptor of tcgen05.mma kind::f8f6f4: fp32 accumulator (bits 4-5 =
@@ -139,34 +139,12 @@ __device__ __forceinline__ void arrive_read(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// tmem_ld32 and tmem_wait of 16 columns.
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
-      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-        "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
-                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
-                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-
-// sum[at .. at + 8) += s * (16 columns).
-__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], int at, const uint32_t (&r)[16],
-                                           float s) {
+// sum += s * (32 columns).
+__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], const uint32_t (&r)[32], float s) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    sum[at + i] =
-        __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])),
-                   make_float2(s, s), sum[at + i]);
+  for (int i = 0; i < 16; ++i)
+    sum[i] = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])),
+                        make_float2(s, s), sum[i]);
 }
 
 // 4 bytes from global to shared memory, asynchronously.
@@ -350,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q = warp & 3;                       // the TMEM lane quarter of this warp
     const int mine = (warp - 4) >> 2;
     const float2 ch = make_float2(c_hi, c_hi), cl = make_float2(c_lo, c_lo);
-    const int half = mine, col = kHalf * half;
+    const int half = mine >> 1, col = 32 * kChunks * mine;
     const uint32_t full0 = smem_u32(&acc_full[half]);
     uint32_t empty0 = smem_u32(&acc_empty[half]);
     if constexpr (kPair) empty0 = map_shared(&acc_empty[half], 0);
@@ -379,28 +357,23 @@ __global__ void __launch_bounds__(kThreads, 1)
           const Scales* end = sc + min(kScaleGroups, nkb - kb0);
           for (; sc < end; ++sc) {
             const float sa = sc->row[q * 32 + lane];
-            const float4 sw = *reinterpret_cast<const float4*>(&sc->chunk[kChunks * half]);
+            const float2 sw = *reinterpret_cast<const float2*>(&sc->chunk[kChunks * mine]);
             ok = wait_on(full0 + 16 * buf, ph, ok);
             tc_fence_after();
             if (live) {
-              // 16 columns are on their way from tensor memory while 16 are summed (all of
-              // a product's, whatever the tile's width: those past it are not stored)
-              uint32_t r[2][16];
+              // (all columns of a product, whatever the tile's width: those past it are
+              // not stored)
+              uint32_t r[32];
               const uint32_t at = tbase + 256 * buf;
-              const float scale[kChunks] = {sa * sw.x, sa * sw.y, sa * sw.z, sa * sw.w};
-              tmem_ld16(at, r[0]);
-#pragma unroll
-              for (int k = 0; k < 2 * kChunks; ++k) {
-                tmem_wait16(r[k & 1]);
-                if (k + 1 < 2 * kChunks) {
-                  tmem_ld16(at + 16 * (k + 1), r[(k + 1) & 1]);
-                } else {
-                  tc_fence_before();
-                  // (every lane's part is read: the load and its wait are the warp's)
-                  if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
-                }
-                scaled_sum(sum[k >> 1], 8 * (k & 1), r[k & 1], scale[k >> 1]);
-              }
+              tmem_ld32(at, r);
+              tmem_wait(r);
+              scaled_sum(sum[0], r, sa * sw.x);
+              tmem_ld32(at + 32, r);
+              tmem_wait(r);
+              tc_fence_before();
+              // (every lane's part is read: the load and its wait are the warp's)
+              if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
+              scaled_sum(sum[1], r, sa * sw.y);
             } else {
               if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
             }
