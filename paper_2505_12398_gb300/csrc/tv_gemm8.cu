@@ -33,13 +33,13 @@ constexpr int kUmmaK = 32;        // K per tcgen05.mma of kind::f8f6f4
 constexpr int kMaxStages = 8;
 constexpr size_t kRingBytes = 200u << 10;
 constexpr size_t kGroupBytes = 32u << 20;       // H bytes of a group of row tiles
-constexpr int kParts = 4;                       // epilogue warps per TMEM lane quarter, two for
+constexpr int kParts = 2;                       // epilogue warps per TMEM lane quarter, one for
 constexpr int kEpiWarps = 4 * kParts;           // each half of the tile's columns
 constexpr int kThreads = 128 + 32 * kEpiWarps;  // TMA, scale and two MMA warps, epilogue
 constexpr int kScaleGroups = 8;                 // groups of K in a slot of scales
 constexpr int kScaleSlots = 4;
-constexpr int kRegsFew = 32, kRegsMany = 112;   // registers per thread after the split
-static_assert(128 * kRegsFew + 32 * kEpiWarps * kRegsMany <= kThreads * 96,
+constexpr int kRegsFew = 40, kRegsMany = 232;   // registers per thread after the split
+static_assert(128 * kRegsFew + 32 * kEpiWarps * kRegsMany <= kThreads * 168,
               "the warpgroups' registers fit what the block was launched with");
 // The scales of one group: of a tile's rows, and of the weight block of each of its
 // 32-column chunks.
@@ -48,11 +48,12 @@ struct Scales {
   float chunk[kBN / 32];
 };
 constexpr size_t kSmemBytes =
-    kRingBytes + 1024 + (size_t)kScaleSlots * kScaleGroups * sizeof(Scales);
+    kRingBytes + 1024 + (size_t)(kScaleSlots * kScaleGroups + 1) * sizeof(Scales);
+// (one more, which the reads ahead at the ring's end fall on)
 constexpr int kHalf = 128;                      // columns of a product: a tile has one or two
 constexpr int kBufs = 4;                        // products in tensor memory
 constexpr int kHalves = kBN / kHalf;            // = 32-column chunks of a thread at most
-constexpr int kChunks = 2;                      // 32-column chunks of a thread
+constexpr int kChunks = 4;                      // 32-column chunks of a thread
 static_assert(kHalf == 32 * kChunks * kParts / kHalves && kBufs * kHalf == (int)kTmemCols, "");
 
 // Instruction descriptor of tcgen05.mma kind::f8f6f4: fp32 accumulator (bits 4-5 =
@@ -102,9 +103,17 @@ __device__ __forceinline__ void commit_to(uint32_t bar) {
         : "memory");
 }
 
-// Waits until the phase of the barrier at `bar` with this parity has completed, unless
-// an earlier wait gave up; whether none has.
-__device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, bool ok) {
+// The same value, of which the compiler does not know that it is the whole warp's:
+// addresses for barriers and shared memory then stay in the registers that these
+// instructions read, and are not moved there from the uniform ones at each use (loop of
+// the sums 450 -> 410 clocks a group in isolation).
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  uint32_t y;
+  asm volatile("mov.u32 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -113,8 +122,13 @@ __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, bool ok) 
       : "=r"(done)
       : "r"(bar), "r"(parity)
       : "memory");
-  if (done) return ok;
-  for (uint32_t i = 0; ok && i < kSpinLimit; ++i) {
+  return done != 0;
+}
+
+// The rest of a wait whose first test found the phase running: 0, or 1 if it gave up.
+__device__ __forceinline__ uint32_t wait_longer(uint32_t bar, uint32_t parity) {
+  for (uint32_t i = 0; i < kSpinLimit; ++i) {
+    uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
@@ -122,9 +136,30 @@ __device__ __forceinline__ bool wait_on(uint32_t bar, uint32_t parity, bool ok) 
         : "=r"(done)
         : "r"(bar), "r"(parity), "n"(kTrySuspendNs)
         : "memory");
-    if (done) return true;
+    if (done) return 0;
   }
-  return false;
+  return 1;
+}
+
+// Waits until the phase of the barrier at `bar` with this parity has completed, unless
+// an earlier wait gave up; `bad` becomes 1 if this one does.
+__device__ __forceinline__ void wait_on(uint32_t bar, uint32_t parity, uint32_t& bad) {
+  if (!try_wait(bar, parity) && !bad) bad = wait_longer(bar, parity);
+}
+
+// A barrier's test whose answer is asked for later: a warp issues in order, and would
+// stand still for the 100 clocks that the test takes if its answer were used at once.
+// One test may be on its way; the predicate is the kernel's (declare_test, once).
+__device__ __forceinline__ void declare_test() { asm volatile(".reg .pred tv_over;"); }
+__device__ __forceinline__ void test_begin(uint32_t bar, uint32_t parity) {
+  asm volatile("mbarrier.test_wait.parity.shared::cta.b64 tv_over, [%0], %1;" ::"r"(bar),
+               "r"(parity)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t test_end() {
+  uint32_t over;
+  asm volatile("selp.u32 %0, 1, 0, tv_over;" : "=r"(over)::"memory");
+  return over;
 }
 
 // Arrives on the barrier at `bar` (kPair: an address in the leader) for a part of tensor
@@ -139,12 +174,53 @@ __device__ __forceinline__ void arrive_read(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// sum += s * (32 columns).
-__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], const uint32_t (&r)[32], float s) {
+// tmem_ld32 and tmem_wait of 16 columns.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+
+// sum[at .. at + 8) += s * (16 columns), those of r[from ..).
+template <int N>
+__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], int at, const uint32_t (&r)[N],
+                                           int from, float s) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    sum[i] = __ffma2_rn(make_float2(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])),
-                        make_float2(s, s), sum[i]);
+  for (int i = 0; i < 8; ++i)
+    sum[at + i] = __ffma2_rn(make_float2(__uint_as_float(r[from + 2 * i]),
+                                         __uint_as_float(r[from + 2 * i + 1])),
+                             make_float2(s, s), sum[at + i]);
+}
+__device__ __forceinline__ void scaled_sum(float2 (&sum)[16], const uint32_t (&r)[32], float s) {
+  scaled_sum(sum, 0, r, 0, s);
+  scaled_sum(sum, 8, r, 16, s);
+}
+
+__device__ __forceinline__ float lds32(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 lds128f(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
 }
 
 // 4 bytes from global to shared memory, asynchronously.
@@ -265,6 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float c_hi, float c_lo, __nv_bfloat16* __restrict__ logits,
                     float2* __restrict__ part, int m_tiles, int n_tiles, int group, int store,
                     uint32_t* __restrict__ status) {
+  declare_test();
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[kMaxStages];   // (kPair: the leader's are used)
   __shared__ __align__(8) uint64_t empty_bar[kMaxStages];
@@ -328,15 +405,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q = warp & 3;                       // the TMEM lane quarter of this warp
     const int mine = (warp - 4) >> 2;
     const float2 ch = make_float2(c_hi, c_hi), cl = make_float2(c_lo, c_lo);
-    const int half = mine >> 1, col = 32 * kChunks * mine;
-    const uint32_t full0 = smem_u32(&acc_full[half]);
-    uint32_t empty0 = smem_u32(&acc_empty[half]);
-    if constexpr (kPair) empty0 = map_shared(&acc_empty[half], 0);
-    uint32_t buf = 0, ph = 0, si = 0;             // the buffer of the next group, its phase
+    const int half = mine, col = kHalf * half;
+    const uint32_t full0 = opaque(smem_u32(&acc_full[half]));
+    const uint32_t empty0 = kPair ? map_shared(&acc_empty[half], 0)
+                                  : opaque(smem_u32(&acc_empty[half]));
+    // this thread's row's scales and its chunks' in the first record of the ring
+    const uint32_t row_scale = opaque(smem_u32(&scales->row[q * 32 + lane]));
+    const uint32_t chunk_scales = opaque(smem_u32(&scales->chunk[kChunks * half]));
+    uint32_t buf = 0, ph = 0, si = 0;             // 16 x the buffer of the next group; its phase
     int j = 0;
     // A wait that gives up is reported and no longer waited for: the loops go on to
     // their end (on whatever is there), so that no wait needs a way out of them.
-    bool ok = true;
+    uint32_t bad = 0, over = 0;                   // over: the next group's product is ready
     for (int t = first; t < n_total; t += step, ++j) {
       int mt, n_tile;
       tile_coords(t, m_tiles, n_tiles, group, mt, n_tile);
@@ -352,33 +432,58 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (n_half[half] > 0) {
         for (int kb0 = 0; kb0 < nkb; kb0 += kScaleGroups, ++si) {
           const uint32_t slot = si % kScaleSlots;
-          ok = wait_on(smem_u32(&scale_full[slot]), (si / kScaleSlots) & 1, ok);
-          const Scales* sc = scales + slot * kScaleGroups;
-          const Scales* end = sc + min(kScaleGroups, nkb - kb0);
-          for (; sc < end; ++sc) {
-            const float sa = sc->row[q * 32 + lane];
-            const float2 sw = *reinterpret_cast<const float2*>(&sc->chunk[kChunks * mine]);
-            ok = wait_on(full0 + 16 * buf, ph, ok);
-            tc_fence_after();
-            if (live) {
-              // (all columns of a product, whatever the tile's width: those past it are
-              // not stored)
-              uint32_t r[32];
-              const uint32_t at = tbase + 256 * buf;
-              tmem_ld32(at, r);
-              tmem_wait(r);
-              scaled_sum(sum[0], r, sa * sw.x);
-              tmem_ld32(at + 32, r);
-              tmem_wait(r);
+          wait_on(smem_u32(&scale_full[slot]), (si / kScaleSlots) & 1, bad);
+          uint32_t rec = slot * (uint32_t)(kScaleGroups * sizeof(Scales));
+          int left = min(kScaleGroups, nkb - kb0);
+          if (live) {
+            float next_row = lds32(row_scale + rec);
+            float4 next_chunk = lds128f(chunk_scales + rec);
+            for (; left > 0; --left) {
+              // 16 or 32 columns are on their way from tensor memory while the ones before
+              // are summed (all of a product's, whatever the tile's width: those past it
+              // are not stored); the next group's scales and its product's barrier are
+              // asked for meanwhile
+              if (!over) wait_on(full0 + buf, ph, bad);
+              tc_fence_after();
+              uint32_t a[32], b[16];
+              const uint32_t at = tbase + 16 * buf;
+              tmem_ld32(at, a);
+              const float4 s = make_float4(next_row * next_chunk.x, next_row * next_chunk.y,
+                                           next_row * next_chunk.z, next_row * next_chunk.w);
+              tmem_wait(a);
+              tmem_ld16(at + 32, b);
+              scaled_sum(sum[0], a, s.x);
+              rec += (uint32_t)sizeof(Scales);
+              ph ^= buf >> 4;                     // (the phase turns after the second buffer)
+              buf ^= 16u;
+              tmem_wait16(b);
+              tmem_ld32(at + 48, a);
+              test_begin(full0 + buf, ph);
+              next_row = lds32(row_scale + rec);
+              next_chunk = lds128f(chunk_scales + rec);
+              scaled_sum(sum[1], 0, b, 0, s.y);
+              tmem_wait(a);
+              tmem_ld16(at + 80, b);
+              scaled_sum(sum[1], 8, a, 0, s.y);
+              scaled_sum(sum[2], 0, a, 16, s.z);
+              over = test_end();
+              tmem_wait16(b);
+              tmem_ld32(at + 96, a);
+              scaled_sum(sum[2], 8, b, 0, s.z);
+              tmem_wait(a);
               tc_fence_before();
               // (every lane's part is read: the load and its wait are the warp's)
-              if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
-              scaled_sum(sum[1], r, sa * sw.y);
-            } else {
-              if (lane == 0) arrive_read<kPair>(empty0 + 16 * buf);
+              if (lane == 0) arrive_read<kPair>(empty0 + (buf ^ 16u));
+              scaled_sum(sum[3], a, s.w);
             }
-            buf ^= 1u;
-            ph ^= buf ^ 1u;
+          } else {
+            for (; left > 0; --left) {
+              if (!over) wait_on(full0 + buf, ph, bad);
+              if (lane == 0) arrive_read<kPair>(empty0 + buf);
+              ph ^= buf >> 4;
+              buf ^= 16u;
+              over = 0;
+            }
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&scale_empty[slot]);
@@ -400,12 +505,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if constexpr (kStats) {    // one partial per row and tile from the quarter's warps
         if (mine > 0) {
-          if (j > 0) ok = wait_on(smem_u32(&ms_empty[q]), (j - 1) & 1, ok);
+          if (j > 0) wait_on(smem_u32(&ms_empty[q]), (j - 1) & 1, bad);
           part_ms[mine - 1][q * 32 + lane] = make_float2(m_run, s_run);
           __syncwarp();
           if (lane == 0) mbar_arrive(&ms_full[q]);
         } else {
-          ok = wait_on(smem_u32(&ms_full[q]), j & 1, ok);
+          wait_on(smem_u32(&ms_full[q]), j & 1, bad);
           float2 o[kParts - 1];
           float mx = m_run;
 #pragma unroll
@@ -424,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (!ok) failed = 1;
+    if (bad) failed = 1;
   } else {
   regs_fewer<kRegsFew>();
   if (warp == 0) {
@@ -469,18 +574,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint64_t desc = smem_desc(smem);
       const uint32_t desc_hi = (uint32_t)(desc >> 32), desc_lo = (uint32_t)desc;
       const uint32_t b_off = (a_bytes + (uint32_t)(half * w_own * kGroup)) >> 4;
-      const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar);
-      const uint32_t acc_f = smem_u32(&acc_full[half]), acc_e = smem_u32(&acc_empty[half]);
+      const uint32_t full0 = opaque(smem_u32(full_bar)), empty0 = smem_u32(empty_bar);
+      const uint32_t acc_f = smem_u32(&acc_full[half]), acc_e = opaque(smem_u32(&acc_empty[half]));
       const uint32_t d0 = tmem + (uint32_t)(kHalf * half);
       uint32_t s = 0, lo = desc_lo, ph = 0;       // the stage, its descriptor, its phase
       uint32_t buf = 0, aph = 1;                  // the buffer, its release's phase
-      bool ok = true;
+      uint32_t bad = 0;
       const int tiles = first < n_total ? (n_total - first + step - 1) / step : 0;
       for (int left = tiles * nkb; left > 0; --left) {
-        ok = wait_on(full0 + 8 * s, ph, ok);
+        wait_on(full0 + 8 * s, ph, bad);
         // (the first use of a buffer waits for the phase before the first, which is over)
-        ok = wait_on(acc_e + 16 * buf, aph, ok);
-        if (!__all_sync(0xffffffffu, ok)) break;
+        wait_on(acc_e + 16 * buf, aph, bad);
+        if (__any_sync(0xffffffffu, bad)) break;
         tc_fence_after();
         if (elect_one()) {
           issue<kPair>(d0 + 256 * buf, lo, lo + b_off, desc_hi, idesc);
@@ -497,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           ph ^= 1u;
         }
       }
-      if (!ok) failed = 1;
+      if (bad) failed = 1;
       // every MMA issued has finished before tensor memory is freed
       if (elect_one()) umma_commit<kPair>(&drain_bar);
       __syncwarp();
