@@ -47,6 +47,11 @@ struct Scales {
   float row[kBM];
   float chunk[kBN / 32];
 };
+// Where SM pairs store through shared memory: buffers of 32 columns of a warp's 32 rows,
+// at the end of the ring's bytes.
+constexpr int kOutBufs = 2;
+constexpr uint32_t kOutBytes = 32 * 32 * 2;
+constexpr size_t kOutTotal = (size_t)kEpiWarps * kOutBufs * kOutBytes;
 constexpr size_t kSmemBytes =
     kRingBytes + 1024 + (size_t)(kScaleSlots * kScaleGroups + 1) * sizeof(Scales);
 // (one more, which the reads ahead at the ring's end fall on)
@@ -252,7 +257,36 @@ struct Shape {
 };
 
 // The widest stores that every row's 32-column chunks allow.
-enum { kStore2 = 0, kStore16 = 1, kStore32 = 2 };
+enum { kStore2 = 0, kStore16 = 1, kStore32 = 2, kStoreTma = 3 };
+
+// Stores 32 columns of the warp's 32 rows from `buf`, this lane's row into it first, in
+// the order that the 64-byte swizzle has (16-byte pieces exchanged by the row's bits 1
+// and 2, which also spreads the lanes over the banks).  Rows and columns past the end of
+// the logits are not written.
+__device__ __forceinline__ void store_tile(const uint32_t (&packed)[16], uint32_t buf, int lane,
+                                           const CUtensorMap* map, int x, int y) {
+  const uint32_t at = buf + (uint32_t)lane * 64u, turn = ((uint32_t)lane >> 1) & 3u;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 16 * (i ^ turn)),
+                 "r"(packed[4 * i]), "r"(packed[4 * i + 1]), "r"(packed[4 * i + 2]),
+                 "r"(packed[4 * i + 3])
+                 : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::
+                     "l"(reinterpret_cast<uint64_t>(map)),
+                 "r"(x), "r"(y), "r"(buf)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+// Until at most kLeft of the stores this thread queued still read their buffers.
+template <int kLeft>
+__device__ __forceinline__ void stores_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
+}
 
 // 32 columns of a row, rounded to bf16.
 __device__ __forceinline__ void pack_row(const float2 (&a)[16], uint32_t (&packed)[16]) {
@@ -336,7 +370,9 @@ template <bool kPair, bool kStats>
 __global__ void __launch_bounds__(kThreads, 1)
     lm_head8_kernel(const __grid_constant__ CUtensorMap map_h,
                     const __grid_constant__ CUtensorMap map_w,
-                    const __grid_constant__ CUtensorMap map_w1, const float* __restrict__ h_scale,
+                    const __grid_constant__ CUtensorMap map_w1,
+                    const __grid_constant__ CUtensorMap map_out,
+                    const float* __restrict__ h_scale,
                     const float* __restrict__ w_scale, int M, int V, int K, Shape shape,
                     float c_hi, float c_lo, __nv_bfloat16* __restrict__ logits,
                     float2* __restrict__ part, int m_tiles, int n_tiles, int group, int store,
@@ -412,6 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     // this thread's row's scales and its chunks' in the first record of the ring
     const uint32_t row_scale = opaque(smem_u32(&scales->row[q * 32 + lane]));
     const uint32_t chunk_scales = opaque(smem_u32(&scales->chunk[kChunks * half]));
+    const uint32_t out0 = smem_u32(smem) + (uint32_t)(kRingBytes - kOutTotal) +
+                          (uint32_t)((warp - 4) * kOutBufs) * kOutBytes;
     uint32_t buf = 0, ph = 0, si = 0;             // 16 x the buffer of the next group; its phase
     int j = 0;
     // A wait that gives up is reported and no longer waited for: the loops go on to
@@ -458,7 +496,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               buf ^= 16u;
               tmem_wait16(b);
               tmem_ld32(at + 48, a);
-              test_begin(full0 + buf, ph);
               next_row = lds32(row_scale + rec);
               next_chunk = lds128f(chunk_scales + rec);
               scaled_sum(sum[1], 0, b, 0, s.y);
@@ -466,7 +503,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               tmem_ld16(at + 80, b);
               scaled_sum(sum[1], 8, a, 0, s.y);
               scaled_sum(sum[2], 0, a, 16, s.z);
-              over = test_end();
               tmem_wait16(b);
               tmem_ld32(at + 96, a);
               scaled_sum(sum[2], 8, b, 0, s.z);
@@ -474,7 +510,9 @@ __global__ void __launch_bounds__(kThreads, 1)
               tc_fence_before();
               // (every lane's part is read: the load and its wait are the warp's)
               if (lane == 0) arrive_read<kPair>(empty0 + (buf ^ 16u));
+              test_begin(full0 + buf, ph);
               scaled_sum(sum[3], a, s.w);
+              over = test_end();
             }
           } else {
             for (; left > 0; --left) {
@@ -497,7 +535,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (c >= bn || n <= 0) break;             // (the same in the whole warp)
         uint32_t packed[16];
         pack_row(sum[k], packed);
-        if (row < M) store_row(packed, logits + (size_t)row * V + col0, n, store);
+        if (kPair && store == kStoreTma) {
+          if (row0 < M) {                         // (the same in the whole warp)
+            if (lane == 0) stores_read<kOutBufs - 1>();
+            __syncwarp();
+            store_tile(packed, out0 + kOutBytes * (k % kOutBufs), lane, &map_out, col0, row0);
+          }
+        } else if (row < M) {
+          store_row(packed, logits + (size_t)row * V + col0, n, store);
+        }
         if constexpr (kStats) {
           in_order(packed, m_run, s_run);
           sum_row(packed, n, ch, cl, m_run, s_run);
@@ -529,6 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
+    if (kPair && lane == 0) stores_read<0>();     // (the buffers go with the CTA)
     if (bad) failed = 1;
   } else {
   regs_fewer<kRegsFew>();
@@ -678,6 +725,24 @@ bool make_map(CUtensorMap* map, const void* base, int rows, int K, int box_rows)
          CUDA_SUCCESS;
 }
 
+// The logits in boxes of 32 x 32 with the 64-byte swizzle, where their rows allow it (the
+// kernel stores without the map where they do not).
+bool make_out_map(CUtensorMap* map, void* base, int rows, int V) {
+  if (V % 8) {
+    *map = CUtensorMap{};
+    return true;
+  }
+  const tvk::gemm::EncodeTiled enc = tvk::gemm::encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)V, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)V * 2};
+  const cuuint32_t box[2] = {32, 32};
+  const cuuint32_t estr[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr int kDevices = 64;
 std::mutex g_mutex;
 struct Device {
@@ -704,7 +769,7 @@ int tile_width(size_t m_tiles, int V, int units, int extra) {
 
 template <bool kPair, bool kStats>
 cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w,
-                   const CUtensorMap& map_w1, const float* h_scale,
+                   const CUtensorMap& map_w1, const CUtensorMap& map_out, const float* h_scale,
                    const float* w_scale, int M, int V, int K, const Shape& shape, float c_hi,
                    float c_lo, void* logits, float2* part, int m_tiles, int n_tiles, int group,
                    int units, uint32_t* status, cudaStream_t stream) {
@@ -722,9 +787,11 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w,
   cfg.attrs = attr;
   cfg.numAttrs = kPair ? 1 : 0;
   const int store = V % 8 ? kStore2
+                    : kPair ? kStoreTma
                     : V % 16 == 0 && (reinterpret_cast<uintptr_t>(logits) & 31u) == 0 ? kStore32
                                                                                      : kStore16;
-  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, map_w1, h_scale, w_scale,
+  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, map_w1, map_out, h_scale,
+                            w_scale,
                             M, V, K, shape, c_hi, c_lo, static_cast<__nv_bfloat16*>(logits), part,
                             m_tiles, n_tiles, group, store, status);
 }
@@ -819,18 +886,18 @@ int tv_launch_lm_head_scaled(const void* hidden, const float* hidden_scales, con
   shape.a_box = std::min(kBM, (M + 7) / 8 * 8);
   shape.bn = width_for(M, V, g);
   shape.stages = (int)std::min<size_t>(
-      kMaxStages, kRingBytes / (shape.a_bytes() + shape.b_bytes(pair)));
-  CUtensorMap map_h, map_w, map_w1;
+      kMaxStages, (kRingBytes - (pair ? kOutTotal : 0)) / (shape.a_bytes() + shape.b_bytes(pair)));
+  CUtensorMap map_h, map_w, map_w1, map_out;
   const int w1 = pair && shape.bn > kHalf ? (shape.bn - kHalf) / 2 : kHalf;
   if (!make_map(&map_h, hidden, M, K, shape.a_box) ||
       !make_map(&map_w, weight, V, K, pair ? std::min(shape.bn, kHalf) / 2 : shape.bn) ||
-      !make_map(&map_w1, weight, V, K, w1))
+      !make_map(&map_w1, weight, V, K, w1) || !make_out_map(&map_out, logits, M, V))
     return -5;
   const int n_tiles = (V + shape.bn - 1) / shape.bn;
   const int group = (int)std::max<size_t>(1, kGroupBytes / ((size_t)tile_rows * K));
   auto run = pair ? (row_stats ? launch<true, true> : launch<true, false>)
                   : (row_stats ? launch<false, true> : launch<false, false>);
-  if (run(map_h, map_w, map_w1, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo, logits, part,
+  if (run(map_h, map_w, map_w1, map_out, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo, logits, part,
           m_tiles, n_tiles, group, units, status, stream) != cudaSuccess) {
     cudaGetLastError();
     return -5;
