@@ -444,7 +444,6 @@ int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
  *                  aligned, of what is stored; a row whose mask leaves nothing gets
  *                  (-inf, 0), which verification reports as TV_STATUS_BAD_ROW if it
  *                  needs the row.
- * The first call allocates the handle's scratch.
  * Errors: TV_ERR_INVALID_ARG, TV_ERR_CAPACITY, TV_ERR_TEMPERATURE, TV_ERR_CUDA.
  */
 int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,

@@ -128,10 +128,22 @@ def _check_out(t, dtype, shape, device):
 
 
 def _check_in(t, dtype, shape, device, name):
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() \
-            or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected a contiguous {dtype} {shape} tensor on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _at(t):
+    """A tensor's address as an argument of the library (0 for None)."""
+    return 0 if t is None else t.data_ptr()
+
+
+def _raw_stream(index):
+    """The current stream of a device as a cudaStream_t, without the object that
+    torch.cuda.current_stream builds (3 us of a small call's 13)."""
+    import torch
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(index) if get is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 class Verifier:
@@ -278,6 +290,18 @@ class Verifier:
             raise LibraryError("tv_draft_children", rc, self.lib)
         return tokens
 
+    def _stream(self, stream):
+        return _raw_stream(self.device.index or 0) if stream is None else stream.cuda_stream
+
+    def _empty(self, stream, shape, dtype):
+        """A new output, of the stream that writes it: memory of another stream's might
+        still be in use there."""
+        import torch
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
     def _float_code(self, t, name):
         import torch
         if t.dtype == torch.bfloat16:
@@ -303,10 +327,9 @@ class Verifier:
         kind = torch.float8_e4m3fn if quantize else torch.bfloat16
         groups = (K + GROUP - 1) // GROUP
         if out is None:
-            y = torch.empty(M, K, dtype=kind, device=self.device)
-            scales = torch.empty(M, groups, dtype=torch.float32, device=self.device) \
-                if quantize else None
-            total = torch.empty_like(x) if residual is not None else None
+            y = self._empty(stream, (M, K), kind)
+            scales = self._empty(stream, (M, groups), torch.float32) if quantize else None
+            total = self._empty(stream, (M, K), x.dtype) if residual is not None else None
         else:
             y, scales, total = out if quantize else (out[0], None, out[1])
             _check_out(y, kind, (M, K), self.device)
@@ -316,9 +339,9 @@ class Verifier:
                 raise ValueError("output: a residual is written where one is given")
             if total is not None:
                 _check_out(total, x.dtype, (M, K), self.device)
-        rc = self.lib.tv_rms_norm(self.handle, M, K, code, _ptr(x), _ptr(residual), wcode,
-                                  _ptr(weight), float(eps), _ptr(total), _ptr(y), _ptr(scales),
-                                  _stream_ptr(stream))
+        rc = self.lib.tv_rms_norm(self.handle, M, K, code, _at(x), _at(residual), wcode,
+                                  _at(weight), float(eps), _at(total), _at(y), _at(scales),
+                                  self._stream(stream))
         if rc != 0:
             raise LibraryError("tv_rms_norm", rc, self.lib)
         return (y, scales, total) if quantize else (y, total)
@@ -332,14 +355,14 @@ class Verifier:
         _check_in(weight, weight.dtype, (rows, K), self.device, "weight")
         blocks = ((rows + GROUP - 1) // GROUP, (K + GROUP - 1) // GROUP)
         if out is None:
-            q = torch.empty(rows, K, dtype=torch.float8_e4m3fn, device=self.device)
-            scales = torch.empty(blocks, dtype=torch.float32, device=self.device)
+            q = self._empty(stream, (rows, K), torch.float8_e4m3fn)
+            scales = self._empty(stream, blocks, torch.float32)
         else:
             q, scales = out
             _check_out(q, torch.float8_e4m3fn, (rows, K), self.device)
             _check_out(scales, torch.float32, blocks, self.device)
-        rc = self.lib.tv_quantize_weight(self.handle, rows, K, code, _ptr(weight), _ptr(q),
-                                         _ptr(scales), _stream_ptr(stream))
+        rc = self.lib.tv_quantize_weight(self.handle, rows, K, code, _at(weight), _at(q),
+                                         _at(scales), self._stream(stream))
         if rc != 0:
             raise LibraryError("tv_quantize_weight", rc, self.lib)
         return q, scales
@@ -360,8 +383,8 @@ class Verifier:
         _check_in(weight_scales, torch.float32, ((V + GROUP - 1) // GROUP, groups), self.device,
                   "weight_scales")
         if out is None:
-            logits = torch.empty(M, V, dtype=torch.bfloat16, device=self.device)
-            row_stats = torch.empty(M, 2, dtype=torch.float32, device=self.device) \
+            logits = self._empty(stream, (M, V), torch.bfloat16)
+            row_stats = self._empty(stream, (M, 2), torch.float32) \
                 if temperature is not None else None
         else:
             logits, row_stats = out
@@ -371,9 +394,9 @@ class Verifier:
             if row_stats is not None:
                 _check_out(row_stats, torch.float32, (M, 2), self.device)
         rc = self.lib.tv_lm_head_scaled(
-            self.handle, M, K, _ptr(hidden), _ptr(hidden_scales), _ptr(weight),
-            _ptr(weight_scales), float(temperature) if temperature is not None else 0.0,
-            _ptr(logits), _ptr(row_stats), _stream_ptr(stream))
+            self.handle, M, K, _at(hidden), _at(hidden_scales), _at(weight),
+            _at(weight_scales), float(temperature) if temperature is not None else 0.0,
+            _at(logits), _at(row_stats), self._stream(stream))
         if rc != 0:
             raise LibraryError("tv_lm_head_scaled", rc, self.lib)
         return logits, row_stats
@@ -408,16 +431,16 @@ class Verifier:
         if context is not None and (context.vocab != V or context.device != self.device):
             raise ValueError("the context is for another vocabulary or device")
         if out is None:
-            res = torch.empty_like(logits)
-            row_stats = torch.empty(B, R, 2, dtype=torch.float32, device=self.device)
+            res = self._empty(stream, (B, R, V), self.logit_dtype)
+            row_stats = self._empty(stream, (B, R, 2), torch.float32)
         else:
             res, row_stats = out
             _check_out(res, self.logit_dtype, (B, R, V), self.device)
             _check_out(row_stats, torch.float32, (B, R, 2), self.device)
         rc = self.lib.tv_process_logits(
-            self.handle, context.ref if context is not None else None, B, R - 1, _ptr(slots),
-            _ptr(parents), _ptr(tokens), _ptr(penalties), _ptr(masks), _ptr(mask_index), n_masks,
-            float(temperature), _ptr(logits), _ptr(res), _ptr(row_stats), _stream_ptr(stream))
+            self.handle, context.ref if context is not None else None, B, R - 1, _at(slots),
+            _at(parents), _at(tokens), _at(penalties), _at(masks), _at(mask_index), n_masks,
+            float(temperature), _at(logits), _at(res), _at(row_stats), self._stream(stream))
         if rc != 0:
             raise LibraryError("tv_process_logits", rc, self.lib)
         return res, row_stats
@@ -544,7 +567,7 @@ class TokenContext:
         import torch
         if slots is not None:
             _check_in(slots, torch.int32, (B,), self.device, "slots")
-        return _ptr(slots)
+        return _at(slots)
 
     def _call(self, name, *args):
         rc = getattr(self.verifier.lib, name)(self.verifier.handle, self.ref, *args)
@@ -554,7 +577,7 @@ class TokenContext:
     def clear(self, slots, stream=None):
         """Empties the given slots ([n] int32, distinct)."""
         self._call("tv_context_clear", slots.numel(), self._slots(slots, slots.numel()),
-                   _stream_ptr(stream))
+                   self.verifier._stream(stream))
 
     def _add(self, kind, tokens, values, slots, stream):
         import torch
@@ -562,8 +585,8 @@ class TokenContext:
         _check_in(tokens, torch.int32, (B, n), self.device, "tokens")
         if values is not None:
             _check_in(values, torch.float32, (B, n), self.device, "values")
-        self._call("tv_context_add", kind, B, n, self._slots(slots, B), _ptr(tokens),
-                   _ptr(values), _stream_ptr(stream))
+        self._call("tv_context_add", kind, B, n, self._slots(slots, B), _at(tokens),
+                   _at(values), self.verifier._stream(stream))
 
     def add_prompt(self, tokens, slots=None, stream=None):
         """Prompt tokens [B, n] int32 of B requests; negative entries are skipped."""
@@ -585,5 +608,5 @@ class TokenContext:
         _check_in(tokens, torch.int32, (B, R), self.device, "tokens")
         _check_in(path, torch.int32, (B, R - 1), self.device, "path")
         _check_in(bonus, torch.int32, (B,), self.device, "bonus")
-        self._call("tv_context_accept", B, R - 1, self._slots(slots, B), _ptr(tokens),
-                   _ptr(path), _ptr(bonus), _stream_ptr(stream))
+        self._call("tv_context_accept", B, R - 1, self._slots(slots, B), _at(tokens),
+                   _at(path), _at(bonus), self.verifier._stream(stream))

@@ -37,9 +37,7 @@ struct tv_handle {
   int withhold_tree = -1;        // test hook for the next persistent call (-1: none)
   // per-(row, tile) scratch of tv_lm_head (allocated on first use)
   float2* lmh_part = nullptr;
-  // the same of tv_lm_head_scaled, and per-(row, chunk) scratch of tv_process_logits
-  float2* lmh8_part = nullptr;
-  float2* proc_part = nullptr;
+  float2* lmh8_part = nullptr;   // the same of tv_lm_head_scaled
   // staging for tv_verify_batch_host (allocated on first use), and the bytes
   // its last call copied each way
   char* stage = nullptr;
@@ -824,10 +822,6 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
     return TV_ERR_INVALID_ARG;
   DeviceGuard guard(h->device);
   if (!guard.ok()) return TV_ERR_CUDA;
-  if (!h->proc_part &&
-      !scratch(&h->proc_part,
-               tv_process_scratch((size_t)h->max_batch * (h->max_nodes + 1), h->vocab)))
-    return TV_ERR_CUDA;
   a.B = B;
   a.N = N;
   a.V = h->vocab;
@@ -840,11 +834,11 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
   a.n_masks = n_masks;
   a.logits = logits;
   a.out = out_logits;
-  a.part = h->proc_part;
   a.row_stats = reinterpret_cast<float2*>(out_row_stats);
   split_scale(temperature, &a.c_hi, &a.c_lo);
   a.status = h->status;
-  const int rc = tv_launch_process(a, h->dtype == TV_BF16, static_cast<cudaStream_t>(cuda_stream));
+  const int rc = tv_launch_process(a, h->dtype == TV_BF16, h->dev.sm_count,
+                                   static_cast<cudaStream_t>(cuda_stream));
   return rc == 0 ? TV_OK : TV_ERR_CUDA;
 }
 
@@ -932,7 +926,6 @@ int tv_destroy(tv_handle* h) {
     if (h->stage) cudaFree(h->stage);
     if (h->lmh_part) cudaFree(h->lmh_part);
     if (h->lmh8_part) cudaFree(h->lmh8_part);
-    if (h->proc_part) cudaFree(h->proc_part);
     cudaGetLastError();
   }
   delete h;

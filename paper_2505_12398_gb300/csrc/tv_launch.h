@@ -220,16 +220,14 @@ struct ProcessArgs {
   int n_masks;
   const void* logits;          // [B][N+1][V]
   void* out;
-  float2* part;                // tv_process_scratch(B (N+1), V) entries
   float2* row_stats;           // [B][N+1]
   float c_hi, c_lo;            // log2(e) / temperature
   uint32_t* status;
 };
 
-// Partial normalisers (float2) that calls of up to `rows` rows need.
-size_t tv_process_scratch(size_t rows, int V);
 // 0 or -5 (launch failed), as for the three after it.
-int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, cudaStream_t stream);
+int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
+                      cudaStream_t stream);
 int tv_launch_context_clear(const ContextArgs& c, int n, const int32_t* slots, int V,
                             uint32_t* status, cudaStream_t stream);
 int tv_launch_context_add(const ContextArgs& c, int kind, int B, int n, const int32_t* slots,

@@ -22,78 +22,191 @@
 
 #include "tv_device.cuh"
 #include "tv_launch.h"
+#include "tv_ptx.cuh"
 
 namespace tvk {
 namespace logits {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 8192;              // tokens of a CTA
-constexpr int kMaxPath = 1024;           // rows of a tree at most
+constexpr int kSegment = 65536;          // tokens whose bitmaps are in shared memory at a time
+constexpr int kSegWords = kSegment / 32;
+constexpr int kMaxCluster = 8;
 constexpr uint32_t kBadTree = 1u, kBadToken = 2u, kBadSlot = 256u, kBadMask = 512u;
+
+// A block of 8 logits, and how many blocks a thread has on its way (64 bytes).
+template <typename L> struct Block;
+template <> struct Block<Bf16Logits> {
+  using elem = __nv_bfloat16;
+  static constexpr int kBlocks = 4, kWords = 4;
+};
+template <> struct Block<F32Logits> {
+  using elem = float;
+  static constexpr int kBlocks = 2, kWords = 8;
+};
 
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float get(const float* p) { return *p; }
+
+// The logits may be processed in place, so that they are not read-only for the kernel.
+__device__ __forceinline__ uint4 ld16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p)
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ void st16(void* p, const uint32_t* w) {
+  asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+               "r"(w[2]), "r"(w[3])
+               : "memory");
+}
 
 struct Row {
   const uint32_t* counts;   // of the request's slot, or nullptr
   const float* bias;
   float rep, freq, pres;
-  int n_path;
 };
 
-// The logit of a marked token.
-__device__ __forceinline__ float penalised(float l, int x, const Row& r, const int* path) {
-  uint32_t c = 0;
-  float bias = 0.f;
-  if (r.counts) {
-    c = r.counts[x];
-    bias = r.bias[x];
-  }
-  uint32_t n = c >> 1;
-  for (int i = 0; i < r.n_path; ++i) n += path[i] == x;
-  if (n > 0 || (c & 1u)) l = l > 0.f ? __fdiv_rn(l, r.rep) : __fmul_rn(l, r.rep);
+// The logit of a marked token, on the path `times` times.
+__device__ __forceinline__ float penalised(float l, uint32_t count, float bias, uint32_t times,
+                                           const Row& r) {
+  const uint32_t n = (count >> 1) + times;
+  if (n > 0 || (count & 1u)) l = l > 0.f ? __fdiv_rn(l, r.rep) : __fmul_rn(l, r.rep);
   if (n > 0) l = __fsub_rn(__fsub_rn(l, __fmul_rn(r.freq, (float)n)), r.pres);
   return __fadd_rn(l, bias);
 }
 
-template <typename L> struct Elem;
-template <> struct Elem<Bf16Logits> { using type = __nv_bfloat16; };
-template <> struct Elem<F32Logits> { using type = float; };
+// All ones in the halves of a word whose bits (0: low, 1: high) are set: bits 0 and 1 as the
+// signs of bytes 0 and 1, and each sign through a half.
+__device__ __forceinline__ uint32_t halves(uint32_t bits) {
+  uint32_t w;
+  asm("prmt.b32 %0, %1, %1, 0x9988;" : "=r"(w) : "r"((bits & 3u) * 0x4080u));
+  return w;
+}
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
-  uint32_t w[4];
+// Blocks outside the allowed bits become -inf.
+template <typename L, int W>
+__device__ __forceinline__ void mask_block(uint32_t (&w)[W], uint32_t allowed) {
+  if constexpr (W == 4) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-    w[k] = *reinterpret_cast<const uint32_t*>(&h);
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t keep = halves(allowed >> (2 * k));
+      w[k] = (w[k] & keep) | (0xff80ff80u & ~keep);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (!(allowed >> k & 1u)) w[k] = 0xff800000u;
   }
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-}
-__device__ __forceinline__ float rounded(__nv_bfloat16*, float v) {
-  return __bfloat162float(__float2bfloat16_rn(v));
-}
-__device__ __forceinline__ float rounded(float*, float v) { return v; }
 
-// CTA (chunk, row): tokens [chunk * kTile, + kTile) of a row.
-template <typename L, bool VEC>
-__global__ void __launch_bounds__(kThreads)
+// Adds blocks to a thread's running (max, sum of 2^((v - max) c)).
+template <int N>
+__device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][4], float2 ch, float2 cl,
+                                           float& m_run, float& s_run) {
+  __nv_bfloat162 hm = *reinterpret_cast<const __nv_bfloat162*>(&w[0][0]);
+#pragma unroll
+  for (int i = 1; i < 4 * N; ++i)
+    hm = __hmax2(hm, *reinterpret_cast<const __nv_bfloat162*>(&w[i >> 2][i & 3]));
+  const float m = fmaxf(__low2float(hm), __high2float(hm));
+  if (m > m_run) {
+    if (m_run != TV_NEG_INF) s_run *= exp2_split(m_run - m, 0.f, ch.x, cl.x);
+    m_run = m;
+  }
+  if (m == TV_NEG_INF) return;           // (all masked)
+  const float2 nm = make_float2(-m_run, -m_run);
+  float2 acc[4];
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i) {
+    const uint32_t u = w[i >> 2][i & 3];
+    float2 e = exp2_corrected_x2(__fadd2_rn(make_float2(bf16_lo(u), bf16_hi(u)), nm), ch, cl);
+    e.x = fmaxf(e.x, 0.f);               // (-inf and NaN weigh nothing)
+    e.y = fmaxf(e.y, 0.f);
+    acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
+  }
+  const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
+  s_run += s2.x + s2.y;
+}
+template <int N>
+__device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][8], float2 ch, float2 cl,
+                                           float& m_run, float& s_run) {
+  float m = TV_NEG_INF;
+#pragma unroll
+  for (int i = 0; i < 8 * N; ++i) m = fmaxf(m, __uint_as_float(w[i >> 3][i & 7]));
+  if (m > m_run) {
+    if (m_run != TV_NEG_INF) s_run *= F32Logits::exp_rel(m_run, m, ch.x, cl.x);
+    m_run = m;
+  }
+  if (m == TV_NEG_INF) return;
+  float2 acc[4];
+#pragma unroll
+  for (int i = 0; i < 4 * N; ++i) {
+    const float2 v = make_float2(__uint_as_float(w[i >> 2][2 * (i & 3)]),
+                                 __uint_as_float(w[i >> 2][2 * (i & 3) + 1]));
+    const float2 e = F32Logits::exp_rel_x2(v, m_run, ch, cl);
+    acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
+  }
+  const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
+  s_run += s2.x + s2.y;
+}
+
+__device__ __forceinline__ float rescale(const Bf16Logits&, float v, float m, float2 ch,
+                                         float2 cl) {
+  return exp2_split(v - m, 0.f, ch.x, cl.x);
+}
+__device__ __forceinline__ float rescale(const F32Logits&, float v, float m, float2 ch,
+                                         float2 cl) {
+  return F32Logits::exp_rel(v, m, ch.x, cl.x);
+}
+
+// 32 bits of a bitmap row of `words` words from bit 32 w - shift on (bits before the row
+// and past it are 0).
+__device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long long w,
+                                            int shift) {
+  const uint32_t hi = w < words ? row[w] : 0u;
+  if (shift == 0) return hi;
+  const uint32_t lo = w > 0 && w - 1 < words ? row[w - 1] : 0u;
+  return __funnelshift_r(lo, hi, 32 - shift);
+}
+
+// One cluster of CTAs per row.  A row is taken in blocks of 8 logits at 8-element
+// boundaries of the whole array (16-byte loads wherever the row starts; the first and last
+// block may hold elements of other rows, which are neither read nor written): position p
+// of a row is its token p - off.  Bitmaps in shared memory hold a bit per position, so a
+// block's are one byte: `mark` the tokens with a count, a bias or a place on the path,
+// `allow` those that the grammar and the row's ends leave.  What bounds it: the logits'
+// bytes, read and written once, with the loads of the next blocks on their way while
+// these are worked on; the marked tokens' counts and biases are gathered where a block
+// has any.
+template <typename L, int kThreads>
+__global__ void __launch_bounds__(kThreads, 768 / kThreads)
     process_kernel(ProcessArgs a) {
-  using E = typename Elem<L>::type;
-  __shared__ uint32_t bits[kTile / 32];
-  __shared__ int path[kMaxPath];
+  using E = typename Block<L>::elem;
+  constexpr int NB = Block<L>::kBlocks, W = Block<L>::kWords;
+  extern __shared__ __align__(16) uint32_t dyn[];
   __shared__ int n_path_s;
   __shared__ float red[2][kThreads / 32];
+  __shared__ float2 joined[kMaxCluster];
   const int R = a.N + 1, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int b = blockIdx.y / R, i = blockIdx.y - b * R;
-  const size_t row = blockIdx.y;
-  const int lo = blockIdx.x * kTile, hi = min(a.V, lo + kTile);
+  uint4* stage = reinterpret_cast<uint4*>(dyn);                    // [NB * W / 4][kThreads]
+  uint32_t* mark = dyn + NB * W * kThreads;
+  uint32_t* allow = mark + kSegWords;
+  int* path = reinterpret_cast<int*>(allow + kSegWords);           // [R], then the tree's
+  int* par = path + R;                                             // parents and tokens
+  int* tok = par + R;
+  uint32_t C, rank;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int row_id = blockIdx.x / C, b = row_id / R, node = row_id - b * R;
+  const size_t row = row_id, start = row * a.V;
+  const int off = (int)(start & 7);
   const int words = (a.V + 31) / 32;
+  const long long positions = (long long)a.V + off;
   uint32_t found = 0;
 
+  // the request
   int slot = a.slots ? a.slots[b] : a.slot0 + b;
   if (a.counts && (slot < 0 || slot >= a.n_slots)) {
     found |= kBadSlot;
@@ -101,7 +214,7 @@ __global__ void __launch_bounds__(kThreads)
   }
   Row r;
   r.counts = a.counts && slot >= 0 ? a.counts + (size_t)slot * a.V : nullptr;
-  r.bias = a.bias + (size_t)max(slot, 0) * a.V;
+  r.bias = r.counts ? a.bias + (size_t)slot * a.V : nullptr;
   r.rep = a.penalties ? a.penalties[3 * b] : 1.f;
   r.freq = a.penalties ? a.penalties[3 * b + 1] : 0.f;
   r.pres = a.penalties ? a.penalties[3 * b + 2] : 0.f;
@@ -111,15 +224,18 @@ __global__ void __launch_bounds__(kThreads)
     found |= kBadMask;
     mi = -1;
   }
-  const uint32_t* allow = mi >= 0 ? a.masks + (size_t)mi * words : nullptr;
-
-  for (int w = tid; w < kTile / 32; w += kThreads)
-    bits[w] = marks && lo / 32 + w < words ? marks[lo / 32 + w] : 0u;
-  if (tid == 0) {       // the drafted path to this row
+  const uint32_t* grammar = mi >= 0 ? a.masks + (size_t)mi * words : nullptr;
+  if (node > 0) {       // the tree, for the drafted path to this row
+    for (int k = tid; k < node + 1; k += kThreads) {
+      par[k] = a.parents[(size_t)b * R + k];
+      tok[k] = a.tokens[(size_t)b * R + k];
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
     int n = 0;
-    const int32_t* par = a.parents + (size_t)b * R;
-    for (int k = i; k > 0;) {
-      const int p = par[k], t = a.tokens[(size_t)b * R + k];
+    for (int k = node; k > 0;) {
+      const int p = par[k], t = tok[k];
       if (t < 0 || t >= a.V) found |= kBadToken;
       else path[n++] = t;
       if (p < 0 || p >= k) {
@@ -131,67 +247,165 @@ __global__ void __launch_bounds__(kThreads)
     n_path_s = n;
   }
   __syncthreads();
-  r.n_path = n_path_s;
-  for (int k = tid; k < r.n_path; k += kThreads)
-    if (path[k] >= lo && path[k] < hi) atomicOr(&bits[(path[k] - lo) / 32], 1u << (path[k] & 31));
-  __syncthreads();
+  const int n_path = n_path_s;
 
-  const E* in = static_cast<const E*>(a.logits) + row * a.V;
-  E* out = static_cast<E*>(a.out) + row * a.V;
+  const E* in = static_cast<const E*>(a.logits) + (start - off);
+  E* out = static_cast<E*>(a.out) + (start - off);
   const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
   float m_run = TV_NEG_INF, s_run = 0.f;
-  for (int x0 = lo + tid * 8; x0 < hi; x0 += kThreads * 8) {
-    float v[8];
-    load_logits<L, VEC>(reinterpret_cast<const typename L::elem*>(in), x0, a.V, v);
-    const uint32_t mk = (bits[(x0 - lo) / 32] >> (x0 & 31)) & 0xffu;
-    const uint32_t ok = allow ? (allow[x0 / 32] >> (x0 & 31)) & 0xffu : 0xffu;
-    if (mk) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if ((mk >> k & 1u) && (VEC || x0 + k < a.V)) v[k] = penalised(v[k], x0 + k, r, path);
+  // this CTA's positions, whole steps of the block
+  constexpr int kStep = 8 * NB * kThreads;
+  const long long steps = (positions + kStep - 1) / kStep, per = (steps + C - 1) / C;
+  const long long p_lo = rank * per * kStep, p_hi = min(positions, p_lo + per * kStep);
+  for (long long s0 = p_lo; s0 < p_hi; s0 += kSegment) {
+    const long long s1 = min(p_hi, s0 + kSegment);
+    if (s0 > p_lo) __syncthreads();      // (the bitmaps before are done with)
+    const int n_words = (int)((s1 - s0 + 31) / 32);
+    for (int w = tid; w < n_words; w += kThreads) {
+      const long long at = s0 / 32 + w;
+      mark[w] = marks ? shifted(marks, words, at, off) : 0u;
+      uint32_t ok = grammar ? shifted(grammar, words, at, off) : 0xffffffffu;
+      if (at == 0) ok &= 0xffffffffu << off;                       // the row's ends
+      const long long left = positions - 32 * at;
+      if (left < 32) ok &= (1u << left) - 1u;
+      allow[w] = ok;
     }
-    float m = TV_NEG_INF;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      if (!(ok >> k & 1u)) v[k] = TV_NEG_INF;
-      v[k] = rounded(out, v[k]);
+    __syncthreads();
+    if (n_path > 0) {
+      for (int k = tid; k < n_path; k += kThreads) {
+        const long long p = (long long)path[k] + off;
+        if (p >= s0 && p < s1) atomicOr(&mark[(p - s0) / 32], 1u << (p & 31));
+      }
+      __syncthreads();
     }
-    if (VEC) {
-      store8(out + x0, v);
-    } else {
+    const uint8_t* mark8 = reinterpret_cast<const uint8_t*>(mark);
+    const uint8_t* allow8 = reinterpret_cast<const uint8_t*>(allow);
+    // this segment's blocks, where the row starts and ends in it, and its elements (a
+    // block at one of the ends is read and written element by element)
+    const int blocks = (int)((s1 - s0 + 7) / 8);
+    const int first = s0 == 0 ? off : 0, last = (int)(s1 - s0);
+    const E* const in_s = in + s0;
+    E* const out_s = out + s0;
+    const int x0 = (int)(s0 - off);      // the token at its first position
+    auto whole = [&](int blk) { return 8 * blk >= first && 8 * blk + 8 <= last; };
+    auto load = [&](int blk, uint32_t (&w)[W]) {
+      if (blk >= blocks) return;
+      const E* src = in_s + 8 * blk;
+      if (whole(blk)) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (x0 + k < a.V) put(out + x0 + k, v[k]);
-        else v[k] = TV_NEG_INF;
-    }
+        for (int k = 0; k < W; k += 4) {
+          const uint4 u = ld16(reinterpret_cast<const char*>(src) + 4 * k);
+          w[k] = u.x; w[k + 1] = u.y; w[k + 2] = u.z; w[k + 3] = u.w;
+        }
+      } else {
+        E v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m = fmaxf(m, v[k]);
-    if (m > m_run) {
-      if (m_run != TV_NEG_INF) s_run *= L::exp_rel(m_run, m, ch.x, cl.x);
-      m_run = m;
-    }
-    if (m_run != TV_NEG_INF) {
-      float t[8];
+        for (int k = 0; k < 8; ++k) {
+          const int p = 8 * blk + k;
+          put(&v[k], p >= first && p < last ? get(src + k) : 0.f);
+        }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) t[k] = L::exp_rel(v[k], m_run, ch.x, cl.x);
-      s_run += sum8(t);
+        for (int k = 0; k < W; ++k) w[k] = reinterpret_cast<const uint32_t*>(v)[k];
+      }
+    };
+    uint32_t next[NB][W];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) load(tid + j * kThreads, next[j]);
+    for (int b0 = 0; b0 < blocks; b0 += NB * kThreads) {
+      uint32_t w[NB][W];
+      uint32_t mk = 0;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int blk = b0 + tid + j * kThreads;
+#pragma unroll
+        for (int k = 0; k < W; ++k) w[j][k] = next[j][k];
+        if (blk < blocks) mk |= (uint32_t)(mark8[blk] & allow8[blk]) << (8 * j);
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) load(b0 + NB * kThreads + tid + j * kThreads, next[j]);
+      if (mk) {         // marked tokens, through this thread's place in shared memory
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int k = 0; k < W; k += 4)
+            stage[(j * (W / 4) + k / 4) * kThreads + tid] =
+                make_uint4(w[j][k], w[j][k + 1], w[j][k + 2], w[j][k + 3]);
+        while (mk) {
+          const int bit = __ffs(mk) - 1, j = bit >> 3, k = bit & 7;
+          mk &= mk - 1;
+          const int x = x0 + 8 * (b0 + tid + j * kThreads) + k;
+          const uint32_t c = r.counts ? r.counts[x] : 0u;
+          const float bias = r.counts ? r.bias[x] : 0.f;
+          uint32_t times = 0;
+          for (int i = 0; i < n_path; ++i) times += path[i] == x;
+          E* e = reinterpret_cast<E*>(
+                     stage + (j * (W / 4) + k * (int)sizeof(E) / 16) * kThreads + tid) +
+                 k % (16 / (int)sizeof(E));
+          put(e, penalised(get(e), c, bias, times, r));
+        }
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int k = 0; k < W; k += 4) {
+            const uint4 u = stage[(j * (W / 4) + k / 4) * kThreads + tid];
+            w[j][k] = u.x; w[j][k + 1] = u.y; w[j][k + 2] = u.z; w[j][k + 3] = u.w;
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int blk = b0 + tid + j * kThreads;
+        const uint32_t ok = blk < blocks ? allow8[blk] : 0u;
+        if (ok != 0xffu) mask_block<L>(w[j], ok);
+        if (blk < blocks) {
+          E* dst = out_s + 8 * blk;
+          if (whole(blk)) {
+#pragma unroll
+            for (int k = 0; k < W; k += 4) st16(reinterpret_cast<char*>(dst) + 4 * k, &w[j][k]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const int p = 8 * blk + k;
+              if (p >= first && p < last) dst[k] = reinterpret_cast<const E*>(w[j])[k];
+            }
+          }
+        }
+      }
+      add_blocks(w, ch, cl, m_run, s_run);
     }
   }
+
+  // the threads' (max, sum), then the cluster's CTAs' in their order
   const float wm = warp_max(m_run);
   if (lane == 0) red[0][wid] = wm;
   __syncthreads();
   float m = red[0][0];
 #pragma unroll
   for (int k = 1; k < kThreads / 32; ++k) m = fmaxf(m, red[0][k]);
-  float s = m_run == TV_NEG_INF ? 0.f : s_run * L::exp_rel(m_run, m, ch.x, cl.x);
+  float s = m_run == TV_NEG_INF ? 0.f : s_run * rescale(L(), m_run, m, ch, cl);
   s = warp_sum(s);
   if (lane == 0) red[1][wid] = s;
   __syncthreads();
   if (tid == 0) {
     s = 0.f;
     for (int k = 0; k < kThreads / 32; ++k) s += red[1][k];
-    a.part[row * gridDim.x + blockIdx.x] = make_float2(m, s);
+    if (C == 1) a.row_stats[row] = make_float2(m, s);
+    else {
+      const uint32_t to = map_shared(&joined[rank], 0);
+      st_cluster_f32(to, m);
+      st_cluster_f32(to + 4, s);
+    }
     if (found) atomicOr(a.status, found);
+  }
+  if (C > 1) {
+    cluster_sync_all();
+    if (rank == 0 && tid == 0) {
+      m = TV_NEG_INF;
+      for (uint32_t k = 0; k < C; ++k) m = fmaxf(m, joined[k].x);
+      s = 0.f;
+      for (uint32_t k = 0; k < C; ++k)
+        if (joined[k].x != TV_NEG_INF) s += joined[k].y * rescale(L(), joined[k].x, m, ch, cl);
+      a.row_stats[row] = make_float2(m, s);
+    }
   }
 }
 
@@ -272,43 +486,71 @@ __global__ void accept_kernel(ContextArgs c, int B, int N, const int32_t* __rest
 }  // namespace logits
 }  // namespace tvk
 
-size_t tv_process_scratch(size_t rows, int V) {
-  return rows * ((V + tvk::logits::kTile - 1) / tvk::logits::kTile);
+namespace {
+
+template <typename L, int kThreads>
+cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
+  using namespace tvk::logits;
+  const size_t smem =
+      4 * ((size_t)Block<L>::kBlocks * Block<L>::kWords * kThreads + 2 * kSegWords +
+           3 * (size_t)(a.N + 1));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.B * (a.N + 1) * C), 1, 1);
+  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)C;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (smem > 48u << 10) {
+    const cudaError_t e = cudaFuncSetAttribute(process_kernel<L, kThreads>,
+                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               64 << 10);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaLaunchKernelEx(&cfg, process_kernel<L, kThreads>, a);
 }
 
-int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, cudaStream_t stream) {
-  using namespace tvk;
-  using namespace tvk::logits;
-  const int rows = a.B * (a.N + 1), chunks = (a.V + kTile - 1) / kTile;
-  // (a grid has at most 65535 rows of blocks)
-  for (int r0 = 0; r0 < rows;) {
-    const int trees = std::max(1, std::min(a.B - r0 / (a.N + 1), 65535 / (a.N + 1)));
+}  // namespace
+
+int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
+                      cudaStream_t stream) {
+  // CTAs per row: enough for four an SM, as far as each has a step of its own
+  const long long rows = (long long)a.B * (a.N + 1);
+  int C = 1;
+  while (C < tvk::logits::kMaxCluster && rows * C < 4ll * sm_count && a.V > 8192 * C) C *= 2;
+  const bool few = rows * C <= sm_count;
+  // (a grid has at most 2^31 - 1 CTAs; the trees of one launch)
+  const long long most = std::max(1ll, 0x7fffffffll / ((long long)(a.N + 1) * C));
+  for (long long b0 = 0; b0 < a.B; b0 += most) {
+    const size_t r0 = (size_t)b0 * (a.N + 1);
     ProcessArgs p = a;
-    const int b0 = r0 / (a.N + 1);
-    const size_t off = (size_t)r0 * a.V * (logit_is_bf16 ? 2 : 4);
-    p.B = trees;
+    const size_t at = r0 * a.V * (logit_is_bf16 ? 2 : 4);
+    p.B = (int)std::min(most, a.B - b0);
     p.slots = a.slots ? a.slots + b0 : nullptr;
-    p.slot0 = a.slot0 + b0;
+    p.slot0 = a.slot0 + (int)b0;
     p.parents = a.parents + r0;
     p.tokens = a.tokens + r0;
     p.penalties = a.penalties ? a.penalties + 3 * (size_t)b0 : nullptr;
     p.mask_index = a.mask_index ? a.mask_index + r0 : nullptr;
-    p.logits = static_cast<const char*>(a.logits) + off;
-    p.out = static_cast<char*>(a.out) + off;
-    p.part = a.part + (size_t)r0 * chunks;
-    const dim3 grid(chunks, trees * (a.N + 1));
-    const bool vec = a.V % 8 == 0;
-    if (logit_is_bf16) {
-      if (vec) process_kernel<Bf16Logits, true><<<grid, kThreads, 0, stream>>>(p);
-      else process_kernel<Bf16Logits, false><<<grid, kThreads, 0, stream>>>(p);
-    } else {
-      if (vec) process_kernel<F32Logits, true><<<grid, kThreads, 0, stream>>>(p);
-      else process_kernel<F32Logits, false><<<grid, kThreads, 0, stream>>>(p);
+    p.logits = static_cast<const char*>(a.logits) + at;
+    p.out = static_cast<char*>(a.out) + at;
+    p.row_stats = a.row_stats + r0;
+    const cudaError_t e =
+        logit_is_bf16 ? (few ? launch_process<tvk::Bf16Logits, 512>(p, C, stream)
+                             : launch_process<tvk::Bf16Logits, 256>(p, C, stream))
+                      : (few ? launch_process<tvk::F32Logits, 512>(p, C, stream)
+                             : launch_process<tvk::F32Logits, 256>(p, C, stream));
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      return -5;
     }
-    if (cudaGetLastError() != cudaSuccess) return -5;
-    r0 += trees * (a.N + 1);
   }
-  return tv_launch_merge(a.part, chunks, rows, a.c_hi, a.c_lo, a.row_stats, stream);
+  return 0;
 }
 
 int tv_launch_context_clear(const ContextArgs& c, int n, const int32_t* slots, int V,
