@@ -803,6 +803,7 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
   NvtxRange range("tv_process_logits");
   if (!h || B < 0 || N < 0 || n_masks < 0) return TV_ERR_INVALID_ARG;
   if (B > h->max_batch || N > h->max_nodes) return TV_ERR_CAPACITY;
+  if ((long long)B * (N + 1) > 0x7fff0000ll) return TV_ERR_CAPACITY;   // (rows are an int)
   if (!temperature_ok(temperature)) return TV_ERR_TEMPERATURE;
   if (B == 0) return TV_OK;
   ProcessArgs a = {};

@@ -66,92 +66,99 @@ __device__ __forceinline__ void st16(void* p, const uint32_t* w) {
 struct Row {
   const uint32_t* counts;   // of the request's slot, or nullptr
   const float* bias;
-  float rep, freq, pres;
+  float rep, inv_rep, freq, pres;
 };
 
-// The logit of a marked token, on the path `times` times.
+// The logit of a marked token, on the path `times` times.  (A positive one is multiplied by
+// 1 / rep: one more rounding in 32 bits than the division, below the one to the logits'
+// type, for a tenth of its instructions.)
 __device__ __forceinline__ float penalised(float l, uint32_t count, float bias, uint32_t times,
                                            const Row& r) {
   const uint32_t n = (count >> 1) + times;
-  if (n > 0 || (count & 1u)) l = l > 0.f ? __fdiv_rn(l, r.rep) : __fmul_rn(l, r.rep);
+  if (n > 0 || (count & 1u)) l = __fmul_rn(l, l > 0.f ? r.inv_rep : r.rep);
   if (n > 0) l = __fsub_rn(__fsub_rn(l, __fmul_rn(r.freq, (float)n)), r.pres);
   return __fadd_rn(l, bias);
 }
 
-// All ones in the halves of a word whose bits (0: low, 1: high) are set: bits 0 and 1 as the
-// signs of bytes 0 and 1, and each sign through a half.
-__device__ __forceinline__ uint32_t halves(uint32_t bits) {
-  uint32_t w;
-  asm("prmt.b32 %0, %1, %1, 0x9988;" : "=r"(w) : "r"((bits & 3u) * 0x4080u));
-  return w;
-}
-
-// Blocks outside the allowed bits become -inf.
-template <typename L, int W>
-__device__ __forceinline__ void mask_block(uint32_t (&w)[W], uint32_t allowed) {
-  if constexpr (W == 4) {
+// Blocks outside the allowed bits become -inf.  bf16: four bits at a time, each first to
+// the sign of a byte of its own (their products with 2^7, 2^14, 2^21 and 2^28 do not
+// overlap), the signs then through the bytes of two words.
+__device__ __forceinline__ void mask_block(uint32_t (&w)[4], uint32_t allowed) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t keep = halves(allowed >> (2 * k));
-      w[k] = (w[k] & keep) | (0xff80ff80u & ~keep);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (!(allowed >> k & 1u)) w[k] = 0xff800000u;
+  for (int k = 0; k < 4; k += 2) {
+    const uint32_t signs = (allowed >> (2 * k) & 0xfu) * 0x10204080u;
+    uint32_t lo, hi;
+    asm("prmt.b32 %0, %1, %1, 0x9988;" : "=r"(lo) : "r"(signs));
+    asm("prmt.b32 %0, %1, %1, 0xbbaa;" : "=r"(hi) : "r"(signs));
+    w[k] = (w[k] & lo) | (0xff80ff80u & ~lo);
+    w[k + 1] = (w[k + 1] & hi) | (0xff80ff80u & ~hi);
   }
 }
+__device__ __forceinline__ void mask_block(uint32_t (&w)[8], uint32_t allowed) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (!(allowed >> k & 1u)) w[k] = 0xff800000u;
+}
 
-// Adds blocks to a thread's running (max, sum of 2^((v - max) c)).  bf16: the exponent d c
-// = d c_lo + d c_hi (d = v - max is exact) is rounded once, which leaves each weight within
-// 2^-24 |d c| ln 2 of the exact one, to either side: of a sum, whose weights lie at 2^0 to
-// 2^-17 of the largest for the most part, below 7e-7 at the very worst and 1e-7 as it
-// goes.  (exp2_corrected's three more operations a pair cost 1057 -> TIME us at 128 x
-// 61 x 128256.)
+// The i-th pair of logits of a thread's blocks, and the largest of all.
 template <int N>
-__device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][4], float2 ch, float2 cl,
-                                           float& m_run, float& s_run) {
+__device__ __forceinline__ float2 pair_of(const uint32_t (&w)[N][4], int i) {
+  const uint32_t u = w[i >> 2][i & 3];
+  return make_float2(bf16_lo(u), bf16_hi(u));
+}
+template <int N>
+__device__ __forceinline__ float2 pair_of(const uint32_t (&w)[N][8], int i) {
+  return make_float2(__uint_as_float(w[i >> 2][2 * (i & 3)]),
+                     __uint_as_float(w[i >> 2][2 * (i & 3) + 1]));
+}
+template <int N>
+__device__ __forceinline__ float largest(const uint32_t (&w)[N][4]) {
   __nv_bfloat162 hm = *reinterpret_cast<const __nv_bfloat162*>(&w[0][0]);
 #pragma unroll
   for (int i = 1; i < 4 * N; ++i)
     hm = __hmax2(hm, *reinterpret_cast<const __nv_bfloat162*>(&w[i >> 2][i & 3]));
-  const float m = fmaxf(__low2float(hm), __high2float(hm));
+  return fmaxf(__low2float(hm), __high2float(hm));
+}
+template <int N>
+__device__ __forceinline__ float largest(const uint32_t (&w)[N][8]) {
+  float m = __uint_as_float(w[0][0]);
+#pragma unroll
+  for (int i = 1; i < 8 * N; ++i) m = fmaxf(m, __uint_as_float(w[i >> 3][i & 7]));
+  return m;
+}
+
+__device__ __forceinline__ float rescale(const Bf16Logits&, float v, float m, float2 ch,
+                                         float2 cl);
+__device__ __forceinline__ float rescale(const F32Logits&, float v, float m, float2 ch,
+                                         float2 cl);
+
+// Adds blocks to a thread's running (max, sum of 2^((v - max) c)).  bf16: d = v - max is
+// exact, and the exponent d c_lo + d c_hi is rounded once, which leaves each weight within
+// 2^-24 |d c| ln 2 of the exact one, to either side: of a sum, whose weights lie at 2^0 to
+// 2^-17 of the largest for the most part, below 7e-7 at the very worst and 1e-7 as it
+// goes.  (exp2_corrected's three more operations a pair: 1057 us for 1016 with three CTAs
+// an SM, at 128 x 61 x 128256.)
+template <typename L, int N, int W>
+__device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch, float2 cl,
+                                           float& m_run, float& s_run) {
+  const float m = largest(w);
   if (m > m_run) {
-    if (m_run != TV_NEG_INF) s_run *= exp2_split(m_run - m, 0.f, ch.x, cl.x);
+    if (m_run != TV_NEG_INF) s_run *= rescale(L(), m_run, m, ch, cl);
     m_run = m;
   }
   if (!(m > TV_NEG_INF)) return;         // (all masked)
-  const float2 nm = make_float2(-m_run, -m_run);
   float2 acc[4];
 #pragma unroll
   for (int i = 0; i < 4 * N; ++i) {
-    const uint32_t u = w[i >> 2][i & 3];
-    const float2 d = __fadd2_rn(make_float2(bf16_lo(u), bf16_hi(u)), nm);
-    const float2 x = __ffma2_rn(d, ch, __fmul2_rn(d, cl));
-    // (-inf and NaN weigh nothing, at any temperature)
-    const float2 e = make_float2(fmaxf(ex2(x.x), 0.f), fmaxf(ex2(x.y), 0.f));
-    acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
-  }
-  const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
-  s_run += s2.x + s2.y;
-}
-template <int N>
-__device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][8], float2 ch, float2 cl,
-                                           float& m_run, float& s_run) {
-  float m = TV_NEG_INF;
-#pragma unroll
-  for (int i = 0; i < 8 * N; ++i) m = fmaxf(m, __uint_as_float(w[i >> 3][i & 7]));
-  if (m > m_run) {
-    if (m_run != TV_NEG_INF) s_run *= F32Logits::exp_rel(m_run, m, ch.x, cl.x);
-    m_run = m;
-  }
-  if (m == TV_NEG_INF) return;
-  float2 acc[4];
-#pragma unroll
-  for (int i = 0; i < 4 * N; ++i) {
-    const float2 v = make_float2(__uint_as_float(w[i >> 2][2 * (i & 3)]),
-                                 __uint_as_float(w[i >> 2][2 * (i & 3) + 1]));
-    const float2 e = F32Logits::exp_rel_x2(v, m_run, ch, cl);
+    float2 e;
+    if constexpr (W == 4) {
+      const float2 d = __fadd2_rn(pair_of(w, i), make_float2(-m_run, -m_run));
+      const float2 x = __ffma2_rn(d, ch, __fmul2_rn(d, cl));
+      // (-inf and NaN weigh nothing, at any temperature)
+      e = make_float2(fmaxf(ex2(x.x), 0.f), fmaxf(ex2(x.y), 0.f));
+    } else {
+      e = F32Logits::exp_rel_x2(pair_of(w, i), m_run, ch, cl);
+    }
     acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
   }
   const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
@@ -193,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   constexpr int NB = Block<L>::kBlocks, W = Block<L>::kWords;
   extern __shared__ __align__(16) uint32_t dyn[];
   __shared__ int n_path_s;
+  __shared__ uint32_t path_bits_s;
   __shared__ float red[2][kThreads / 32];
   __shared__ float2 joined[kMaxCluster];
   const int R = a.N + 1, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -222,6 +230,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   r.counts = a.counts && slot >= 0 ? a.counts + (size_t)slot * a.V : nullptr;
   r.bias = r.counts ? a.bias + (size_t)slot * a.V : nullptr;
   r.rep = a.penalties ? a.penalties[3 * b] : 1.f;
+  r.inv_rep = 1.f / r.rep;
   r.freq = a.penalties ? a.penalties[3 * b + 1] : 0.f;
   r.pres = a.penalties ? a.penalties[3 * b + 2] : 0.f;
   const uint32_t* marks = r.counts ? a.marks + (size_t)slot * words : nullptr;
@@ -240,10 +249,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   }
   if (tid == 0) {
     int n = 0;
+    uint32_t bits = 0;
     for (int k = node; k > 0;) {
       const int p = par[k], t = tok[k];
-      if (t < 0 || t >= a.V) found |= kBadToken;
-      else path[n++] = t;
+      if (t < 0 || t >= a.V) {
+        found |= kBadToken;
+      } else {
+        path[n++] = t;
+        bits |= 1u << (t & 31);
+      }
       if (p < 0 || p >= k) {
         found |= kBadTree;
         break;
@@ -251,9 +265,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       k = p;
     }
     n_path_s = n;
+    path_bits_s = bits;                  // (which residues the path's tokens have)
   }
   __syncthreads();
   const int n_path = n_path_s;
+  const uint32_t path_bits = path_bits_s;
 
   const E* in = static_cast<const E*>(a.logits) + (start - off);
   E* out = static_cast<E*>(a.out) + (start - off);
@@ -314,21 +330,44 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         for (int k = 0; k < W; ++k) w[k] = reinterpret_cast<const uint32_t*>(v)[k];
       }
     };
-    uint32_t next[NB][W];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) load(tid + j * kThreads, next[j]);
-    for (int b0 = 0; b0 < blocks; b0 += NB * kThreads) {
-      uint32_t w[NB][W];
-      uint32_t mk = 0;
+    // the marked tokens of a thread's blocks from b0 on, 8 bits a block, and the count
+    // and bias of the first, asked for a step ahead of their use
+    auto marked = [&](int b0) {
+      uint32_t m = 0;
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const int blk = b0 + tid + j * kThreads;
+        if (blk < blocks) m |= (uint32_t)(mark8[blk] & allow8[blk]) << (8 * j);
+      }
+      return m;
+    };
+    auto token = [&](int b0, uint32_t m) {
+      const int bit = __ffs(m) - 1;
+      return x0 + 8 * (b0 + tid + (bit >> 3) * kThreads) + (bit & 7);
+    };
+    uint32_t next[NB][W], next_mk = marked(0), next_c = 0;
+    float next_b = 0.f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) load(tid + j * kThreads, next[j]);
+    if (next_mk && r.counts) {
+      next_c = r.counts[token(0, next_mk)];
+      next_b = r.bias[token(0, next_mk)];
+    }
+    for (int b0 = 0; b0 < blocks; b0 += NB * kThreads) {
+      uint32_t w[NB][W], mk = next_mk, c = next_c;
+      float bias = next_b;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int k = 0; k < W; ++k) w[j][k] = next[j][k];
-        if (blk < blocks) mk |= (uint32_t)(mark8[blk] & allow8[blk]) << (8 * j);
-      }
+      const int b1 = b0 + NB * kThreads;
 #pragma unroll
-      for (int j = 0; j < NB; ++j) load(b0 + NB * kThreads + tid + j * kThreads, next[j]);
+      for (int j = 0; j < NB; ++j) load(b1 + tid + j * kThreads, next[j]);
+      next_mk = marked(b1);
+      if (next_mk && r.counts) {
+        next_c = r.counts[token(b1, next_mk)];
+        next_b = r.bias[token(b1, next_mk)];
+      }
       if (mk) {         // marked tokens, through this thread's place in shared memory
 #pragma unroll
         for (int j = 0; j < NB; ++j)
@@ -336,18 +375,21 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
           for (int k = 0; k < W; k += 4)
             stage[(j * (W / 4) + k / 4) * kThreads + tid] =
                 make_uint4(w[j][k], w[j][k + 1], w[j][k + 2], w[j][k + 3]);
-        while (mk) {
-          const int bit = __ffs(mk) - 1, j = bit >> 3, k = bit & 7;
-          mk &= mk - 1;
-          const int x = x0 + 8 * (b0 + tid + j * kThreads) + k;
-          const uint32_t c = r.counts ? r.counts[x] : 0u;
-          const float bias = r.counts ? r.bias[x] : 0.f;
+        for (;;) {
+          const int bit = __ffs(mk) - 1, j = bit >> 3, k = bit & 7, x = token(b0, mk);
           uint32_t times = 0;
-          for (int i = 0; i < n_path; ++i) times += path[i] == x;
+          if (path_bits >> (x & 31) & 1u)
+            for (int i = 0; i < n_path; ++i) times += path[i] == x;
           E* e = reinterpret_cast<E*>(
                      stage + (j * (W / 4) + k * (int)sizeof(E) / 16) * kThreads + tid) +
                  k % (16 / (int)sizeof(E));
           put(e, penalised(get(e), c, bias, times, r));
+          mk &= mk - 1;
+          if (!mk) break;
+          if (r.counts) {
+            c = r.counts[token(b0, mk)];
+            bias = r.bias[token(b0, mk)];
+          }
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j)
@@ -361,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       for (int j = 0; j < NB; ++j) {
         const int blk = b0 + tid + j * kThreads;
         const uint32_t ok = blk < blocks ? allow8[blk] : 0u;
-        if (ok != 0xffu) mask_block<L>(w[j], ok);
+        if (ok != 0xffu) mask_block(w[j], ok);
         if (blk < blocks) {
           E* dst = out_s + 8 * blk;
           if (whole(blk)) {
@@ -376,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
           }
         }
       }
-      add_blocks(w, ch, cl, m_run, s_run);
+      add_blocks<L>(w, ch, cl, m_run, s_run);
     }
   }
 
