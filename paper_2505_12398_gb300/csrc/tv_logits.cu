@@ -27,8 +27,7 @@
 namespace tvk {
 namespace logits {
 
-constexpr int kSegment = 65536;          // tokens whose bitmaps are in shared memory at a time
-constexpr int kSegWords = kSegment / 32;
+constexpr int kSegment = 65536;          // tokens whose bits are in shared memory at a time
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kBadTree = 1u, kBadToken = 2u, kBadSlot = 256u, kBadMask = 512u;
 
@@ -174,6 +173,18 @@ __device__ __forceinline__ float rescale(const F32Logits&, float v, float m, flo
   return F32Logits::exp_rel(v, m, ch.x, cl.x);
 }
 
+// Adds one logit to a running (max, sum).
+template <typename L>
+__device__ __forceinline__ void add_one(const L&, float v, float2 ch, float2 cl, float& m_run,
+                                        float& s_run) {
+  if (v > m_run) {
+    s_run = 1.f + (m_run == TV_NEG_INF ? 0.f : s_run * rescale(L(), m_run, v, ch, cl));
+    m_run = v;
+  } else if (m_run != TV_NEG_INF) {
+    s_run += rescale(L(), v, m_run, ch, cl);
+  }
+}
+
 // 32 bits of a bitmap row of `words` words from bit 32 w - shift on (bits before the row
 // and past it are 0).
 __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long long w,
@@ -187,9 +198,9 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
 // One cluster of CTAs per row.  A row is taken in blocks of 8 logits at 8-element
 // boundaries of the whole array (16-byte loads wherever the row starts; the first and last
 // block may hold elements of other rows, which are neither read nor written): position p
-// of a row is its token p - off.  Bitmaps in shared memory hold a bit per position, so a
-// block's are one byte: `mark` the tokens with a count, a bias or a place on the path,
-// `allow` those that the grammar and the row's ends leave.  What bounds it: the logits'
+// of a row is its token p - off.  Shared memory holds two bytes for each block: a bit for
+// each token that the grammar and the row's ends leave, and for each of those that has a
+// count, a bias or a place on the path.  What bounds it: the logits'
 // bytes, read and written once, with the loads of the next blocks on their way while
 // these are worked on; the marked tokens' counts and biases are gathered where a block
 // has any.
@@ -205,9 +216,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   __shared__ float2 joined[kMaxCluster];
   const int R = a.N + 1, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   uint4* stage = reinterpret_cast<uint4*>(dyn);                    // [NB * W / 4][kThreads]
-  uint32_t* mark = dyn + NB * W * kThreads;
-  uint32_t* allow = mark + kSegWords;
-  int* path = reinterpret_cast<int*>(allow + kSegWords);           // [R], then the tree's
+  uint16_t* bits = reinterpret_cast<uint16_t*>(dyn + NB * W * kThreads);   // [kSegment / 8]
+  int* path = reinterpret_cast<int*>(bits + kSegment / 8);         // [R], then the tree's
   int* par = path + R;                                             // parents and tokens
   int* tok = par + R;
   uint32_t C, rank;
@@ -275,99 +285,95 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   E* out = static_cast<E*>(a.out) + (start - off);
   const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
   float m_run = TV_NEG_INF, s_run = 0.f;
+  // how often a token is on the path
+  auto times = [&](int x) {
+    uint32_t n = 0;
+    if (path_bits >> (x & 31) & 1u)
+      for (int i = 0; i < n_path; ++i) n += path[i] == x;
+    return n;
+  };
   // this CTA's positions, whole steps of the block
-  constexpr int kStep = 8 * NB * kThreads;
+  constexpr int kBlocks = NB * kThreads, kStep = 8 * kBlocks;
   const long long steps = (positions + kStep - 1) / kStep, per = (steps + C - 1) / C;
   const long long p_lo = rank * per * kStep, p_hi = min(positions, p_lo + per * kStep);
   for (long long s0 = p_lo; s0 < p_hi; s0 += kSegment) {
     const long long s1 = min(p_hi, s0 + kSegment);
     if (s0 > p_lo) __syncthreads();      // (the bitmaps before are done with)
-    const int n_words = (int)((s1 - s0 + 31) / 32);
-    for (int w = tid; w < n_words; w += kThreads) {
+    // this segment's whole blocks [lo, hi), and the steps that hold them (what is left at the
+    // row's ends is taken element by element further down)
+    const int lo = s0 == 0 && off > 0 ? 1 : 0, hi = (int)((s1 - s0) / 8);
+    const int blocks = (hi + kBlocks - 1) / kBlocks * kBlocks;
+    const E* const in_s = in + s0 + 8 * tid;
+    E* const out_s = out + s0 + 8 * tid;
+    const int x0 = (int)(s0 - off) + 8 * tid;      // the token at this thread's first position
+    // a byte of allowed and one of marked tokens for each block
+    for (int w = tid; w < blocks / 4; w += kThreads) {
       const long long at = s0 / 32 + w;
-      mark[w] = marks ? shifted(marks, words, at, off) : 0u;
       uint32_t ok = grammar ? shifted(grammar, words, at, off) : 0xffffffffu;
-      if (at == 0) ok &= 0xffffffffu << off;                       // the row's ends
-      const long long left = positions - 32 * at;
-      if (left < 32) ok &= (1u << left) - 1u;
-      allow[w] = ok;
+      if (w == 0 && lo) ok &= 0xffffff00u;
+      const int left = 8 * hi - 32 * w;
+      if (left < 32) ok &= left > 0 ? (1u << left) - 1u : 0u;
+      const uint32_t mk = marks ? shifted(marks, words, at, off) & ok : 0u;
+      reinterpret_cast<uint2*>(bits)[w] =
+          make_uint2(__byte_perm(ok, mk, 0x5140), __byte_perm(ok, mk, 0x7362));
     }
     __syncthreads();
     if (n_path > 0) {
       for (int k = tid; k < n_path; k += kThreads) {
-        const long long p = (long long)path[k] + off;
-        if (p >= s0 && p < s1) atomicOr(&mark[(p - s0) / 32], 1u << (p & 31));
+        const long long p = (long long)path[k] + off - s0;
+        if (p >= 0 && p < 8 * hi && (bits[p >> 3] >> (p & 7) & 1u))
+          atomicOr(reinterpret_cast<uint32_t*>(bits) + (p >> 4),
+                   1u << ((p & 7) + 8 + 16 * (int)(p >> 3 & 1)));
       }
       __syncthreads();
     }
-    const uint8_t* mark8 = reinterpret_cast<const uint8_t*>(mark);
-    const uint8_t* allow8 = reinterpret_cast<const uint8_t*>(allow);
-    // this segment's blocks, where the row starts and ends in it, and its elements (a
-    // block at one of the ends is read and written element by element)
-    const int blocks = (int)((s1 - s0 + 7) / 8);
-    const int first = s0 == 0 ? off : 0, last = (int)(s1 - s0);
-    const E* const in_s = in + s0;
-    E* const out_s = out + s0;
-    const int x0 = (int)(s0 - off);      // the token at its first position
-    auto whole = [&](int blk) { return 8 * blk >= first && 8 * blk + 8 <= last; };
-    auto load = [&](int blk, uint32_t (&w)[W]) {
-      if (blk >= blocks) return;
-      const E* src = in_s + 8 * blk;
-      if (whole(blk)) {
-#pragma unroll
-        for (int k = 0; k < W; k += 4) {
-          const uint4 u = ld16(reinterpret_cast<const char*>(src) + 4 * k);
-          w[k] = u.x; w[k + 1] = u.y; w[k + 2] = u.z; w[k + 3] = u.w;
-        }
-      } else {
-        E v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int p = 8 * blk + k;
-          put(&v[k], p >= first && p < last ? get(src + k) : 0.f);
-        }
-#pragma unroll
-        for (int k = 0; k < W; ++k) w[k] = reinterpret_cast<const uint32_t*>(v)[k];
-      }
+    // A step's blocks of this thread: their logits, the bits of their allowed tokens and of
+    // those that are marked as well (8 a block), and the first marked one's count and bias.
+    auto token = [&](int b0, uint32_t m) {
+      const int bit = __ffs(m) - 1;
+      return x0 + 8 * (b0 + (bit >> 3) * kThreads) + (bit & 7);
     };
-    // the marked tokens of a thread's blocks from b0 on, 8 bits a block, and the count
-    // and bias of the first, asked for a step ahead of their use
-    auto marked = [&](int b0) {
-      uint32_t m = 0;
+    uint32_t next[NB][W], next_ok = 0, next_mk = 0, next_count = 0;
+    float next_bias = 0.f;
+    auto fetch = [&](int b0) {
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const int blk = b0 + tid + j * kThreads;
-        if (blk < blocks) m |= (uint32_t)(mark8[blk] & allow8[blk]) << (8 * j);
-      }
-      return m;
-    };
-    auto token = [&](int b0, uint32_t m) {
-      const int bit = __ffs(m) - 1;
-      return x0 + 8 * (b0 + tid + (bit >> 3) * kThreads) + (bit & 7);
-    };
-    uint32_t next[NB][W], next_mk = marked(0), next_c = 0;
-    float next_b = 0.f;
+        if (blk >= lo && blk < hi) {
 #pragma unroll
-    for (int j = 0; j < NB; ++j) load(tid + j * kThreads, next[j]);
-    if (next_mk && r.counts) {
-      next_c = r.counts[token(0, next_mk)];
-      next_b = r.bias[token(0, next_mk)];
-    }
-    for (int b0 = 0; b0 < blocks; b0 += NB * kThreads) {
-      uint32_t w[NB][W], mk = next_mk, c = next_c;
-      float bias = next_b;
+          for (int k = 0; k < W; k += 4) {
+            const uint4 u = ld16(reinterpret_cast<const char*>(in_s + 8 * b0) +
+                                 j * kThreads * 8 * (int)sizeof(E) + 4 * k);
+            next[j][k] = u.x;
+            next[j][k + 1] = u.y;
+            next[j][k + 2] = u.z;
+            next[j][k + 3] = u.w;
+          }
+        }
+      }
+      if (b0 >= blocks) return;
+      next_ok = next_mk = 0;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const uint32_t both = bits[b0 + tid + j * kThreads];
+        next_ok |= (both & 0xffu) << (8 * j);
+        next_mk |= (both >> 8) << (8 * j);
+      }
+      if (next_mk && r.counts) {
+        next_count = r.counts[token(b0, next_mk)];
+        next_bias = r.bias[token(b0, next_mk)];
+      }
+    };
+    fetch(0);
+    for (int b0 = 0; b0 < blocks; b0 += kBlocks) {
+      uint32_t w[NB][W], mk = next_mk, count = next_count;
+      const uint32_t ok = next_ok;
+      float bias = next_bias;
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int k = 0; k < W; ++k) w[j][k] = next[j][k];
-      const int b1 = b0 + NB * kThreads;
-#pragma unroll
-      for (int j = 0; j < NB; ++j) load(b1 + tid + j * kThreads, next[j]);
-      next_mk = marked(b1);
-      if (next_mk && r.counts) {
-        next_c = r.counts[token(b1, next_mk)];
-        next_b = r.bias[token(b1, next_mk)];
-      }
+      fetch(b0 + kBlocks);
       if (mk) {         // marked tokens, through this thread's place in shared memory
 #pragma unroll
         for (int j = 0; j < NB; ++j)
@@ -377,17 +383,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
                 make_uint4(w[j][k], w[j][k + 1], w[j][k + 2], w[j][k + 3]);
         for (;;) {
           const int bit = __ffs(mk) - 1, j = bit >> 3, k = bit & 7, x = token(b0, mk);
-          uint32_t times = 0;
-          if (path_bits >> (x & 31) & 1u)
-            for (int i = 0; i < n_path; ++i) times += path[i] == x;
           E* e = reinterpret_cast<E*>(
                      stage + (j * (W / 4) + k * (int)sizeof(E) / 16) * kThreads + tid) +
                  k % (16 / (int)sizeof(E));
-          put(e, penalised(get(e), c, bias, times, r));
+          put(e, penalised(get(e), count, bias, times(x), r));
           mk &= mk - 1;
           if (!mk) break;
           if (r.counts) {
-            c = r.counts[token(b0, mk)];
+            count = r.counts[token(b0, mk)];
             bias = r.bias[token(b0, mk)];
           }
         }
@@ -399,26 +402,45 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
             w[j][k] = u.x; w[j][k + 1] = u.y; w[j][k + 2] = u.z; w[j][k + 3] = u.w;
           }
       }
+      if (ok != (NB == 4 ? 0xffffffffu : 0xffffu)) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) mask_block(w[j], ok >> (8 * j) & 0xffu);
+      }
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const int blk = b0 + tid + j * kThreads;
-        const uint32_t ok = blk < blocks ? allow8[blk] : 0u;
-        if (ok != 0xffu) mask_block(w[j], ok);
-        if (blk < blocks) {
-          E* dst = out_s + 8 * blk;
-          if (whole(blk)) {
+        if (blk >= lo && blk < hi) {
 #pragma unroll
-            for (int k = 0; k < W; k += 4) st16(reinterpret_cast<char*>(dst) + 4 * k, &w[j][k]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const int p = 8 * blk + k;
-              if (p >= first && p < last) dst[k] = reinterpret_cast<const E*>(w[j])[k];
-            }
-          }
+          for (int k = 0; k < W; k += 4)
+            st16(reinterpret_cast<char*>(out_s + 8 * b0) + j * kThreads * 8 * (int)sizeof(E) +
+                     4 * k,
+                 &w[j][k]);
         }
       }
       add_blocks<L>(w, ch, cl, m_run, s_run);
+    }
+    // the blocks at the row's ends, an element a thread
+    // (one block, where the row starts and ends in the same)
+    if ((lo && tid < 8) || (s1 == positions && hi >= lo && tid >= 8 && tid < 16)) {
+      const long long p = tid < 8 ? tid : s0 + 8ll * hi + (tid - 8);
+      const int x = (int)(p - off);
+      if (x >= 0 && p < positions) {
+        uint32_t n = 0, marked = 0;
+        float bias = 0.f;
+        if (marks && (marks[x >> 5] >> (x & 31) & 1u)) {
+          n = r.counts[x];
+          bias = r.bias[x];
+          marked = 1;
+        }
+        const uint32_t on_path = times(x);
+        float v = get(in + p);
+        if (marked || on_path) v = penalised(v, n, bias, on_path, r);
+        if (grammar && !(grammar[x >> 5] >> (x & 31) & 1u)) v = TV_NEG_INF;
+        E e;
+        put(&e, v);
+        out[p] = e;
+        add_one(L(), get(&e), ch, cl, m_run, s_run);
+      }
     }
   }
 
@@ -540,7 +562,7 @@ template <typename L, int kThreads>
 cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
   using namespace tvk::logits;
   const size_t smem =
-      4 * ((size_t)Block<L>::kBlocks * Block<L>::kWords * kThreads + 2 * kSegWords +
+      4 * ((size_t)Block<L>::kBlocks * Block<L>::kWords * kThreads + kSegment / 16 +
            3 * (size_t)(a.N + 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.B * (a.N + 1) * C), 1, 1);
