@@ -206,8 +206,7 @@ struct ContextArgs {
 
 struct ProcessArgs {
   int B, N, V;
-  const int32_t* slots;        // [B] or nullptr: slot0 + b
-  int slot0;
+  const int32_t* slots;        // [B] or nullptr: b
   int n_slots;
   const uint32_t* counts;      // a context's arrays, or nullptr
   const float* bias;

@@ -27,7 +27,7 @@
 namespace tvk {
 namespace logits {
 
-constexpr int kSegment = 65536;          // tokens whose bits are in shared memory at a time
+constexpr int kSegment = 65536;         // tokens whose bits are in shared memory at a time
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kBadTree = 1u, kBadToken = 2u, kBadSlot = 256u, kBadMask = 512u;
 
@@ -50,14 +50,14 @@ __device__ __forceinline__ float get(const float* p) { return *p; }
 // The logits may be processed in place, so that they are not read-only for the kernel.
 __device__ __forceinline__ uint4 ld16(const void* p) {
   uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+  asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                : "l"(p)
                : "memory");
   return v;
 }
 __device__ __forceinline__ void st16(void* p, const uint32_t* w) {
-  asm volatile("st.global.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+  asm volatile("st.global.cs.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]),
                "r"(w[2]), "r"(w[3])
                : "memory");
 }
@@ -227,64 +227,108 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   const size_t row = row_id, start = row * a.V;
   const int off = (int)(start & 7);
   const int words = (a.V + 31) / 32;
-  const long long positions = (long long)a.V + off;
   uint32_t found = 0;
 
-  // the request
-  int slot = a.slots ? a.slots[b] : a.slot0 + b;
-  if (a.counts && (slot < 0 || slot >= a.n_slots)) {
-    found |= kBadSlot;
-    slot = -1;
+  // this CTA's positions [p_lo, p_hi), whole steps of the block, and its whole blocks [lo,
+  // hi) (what is left at the row's ends is taken element by element at the end)
+  constexpr int kBlocks = NB * kThreads, kStep = 8 * kBlocks;
+  const long long positions = (long long)a.V + off;
+  const long long steps = (positions + kStep - 1) / kStep, per = (steps + C - 1) / C;
+  const long long p_lo = min(positions, rank * per * kStep);
+  const long long p_hi = min(positions, p_lo + per * kStep);
+  const int lo = p_lo == 0 && off > 0 ? 1 : 0, hi = (int)((p_hi - p_lo) / 8);
+  const int blocks = (hi + kBlocks - 1) / kBlocks * kBlocks;
+  const E* const in = static_cast<const E*>(a.logits) + (start - off + p_lo) + 8 * tid;
+  E* const out = static_cast<E*>(a.out) + (start - off + p_lo) + 8 * tid;
+  const int x0 = (int)(p_lo - off) + 8 * tid;      // the token at this thread's first position
+  // the first step's logits are on their way while all of the rest is looked up
+  uint32_t next[NB][W];
+  auto fetch = [&](int b0) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const int blk = b0 + tid + j * kThreads;
+      if (blk >= lo && blk < hi) {
+#pragma unroll
+        for (int k = 0; k < W; k += 4) {
+          const uint4 u = ld16(reinterpret_cast<const char*>(in + 8 * b0) +
+                               j * kThreads * 8 * (int)sizeof(E) + 4 * k);
+          next[j][k] = u.x;
+          next[j][k + 1] = u.y;
+          next[j][k + 2] = u.z;
+          next[j][k + 3] = u.w;
+        }
+      }
+    }
+  };
+  fetch(0);
+
+  // the request, and the tree for the drafted path to this row
+  int slot = a.slots ? a.slots[b] : b;
+  int mi = a.mask_index ? a.mask_index[row] : -1;
+  if (node > 0) {
+    for (int k = tid; k < node + 1; k += kThreads) {
+      par[k] = a.parents[(size_t)b * R + k];
+      tok[k] = a.tokens[(size_t)b * R + k];
+    }
   }
   Row r;
-  r.counts = a.counts && slot >= 0 ? a.counts + (size_t)slot * a.V : nullptr;
-  r.bias = r.counts ? a.bias + (size_t)slot * a.V : nullptr;
   r.rep = a.penalties ? a.penalties[3 * b] : 1.f;
   r.inv_rep = 1.f / r.rep;
   r.freq = a.penalties ? a.penalties[3 * b + 1] : 0.f;
   r.pres = a.penalties ? a.penalties[3 * b + 2] : 0.f;
+  if (a.counts && (slot < 0 || slot >= a.n_slots)) {
+    found |= kBadSlot;
+    slot = -1;
+  }
+  r.counts = a.counts && slot >= 0 ? a.counts + (size_t)slot * a.V : nullptr;
+  r.bias = r.counts ? a.bias + (size_t)slot * a.V : nullptr;
   const uint32_t* marks = r.counts ? a.marks + (size_t)slot * words : nullptr;
-  int mi = a.mask_index ? a.mask_index[row] : -1;
   if (mi < -1 || mi >= a.n_masks) {
     found |= kBadMask;
     mi = -1;
   }
   const uint32_t* grammar = mi >= 0 ? a.masks + (size_t)mi * words : nullptr;
-  if (node > 0) {       // the tree, for the drafted path to this row
-    for (int k = tid; k < node + 1; k += kThreads) {
-      par[k] = a.parents[(size_t)b * R + k];
-      tok[k] = a.tokens[(size_t)b * R + k];
+  // a byte of allowed and one of marked tokens for each block of a segment
+  auto look_up = [&](int seg) {
+    const int n = min(kSegment / 8, blocks - seg) / 4;
+    for (int w = tid; w < n; w += kThreads) {
+      const long long at = (p_lo + 8ll * seg) / 32 + w;
+      uint32_t ok = grammar ? shifted(grammar, words, at, off) : 0xffffffffu;
+      if (seg == 0 && w == 0 && lo) ok &= 0xffffff00u;
+      const int left = 8 * (hi - seg) - 32 * w;
+      if (left < 32) ok &= left > 0 ? (1u << left) - 1u : 0u;
+      const uint32_t mk = marks ? shifted(marks, words, at, off) & ok : 0u;
+      reinterpret_cast<uint2*>(bits)[w] =
+          make_uint2(__byte_perm(ok, mk, 0x5140), __byte_perm(ok, mk, 0x7362));
+    }
+  };
+  look_up(0);
+  __syncthreads();
+  if (node > 0) {
+    if (tid == 0) {
+      int n = 0;
+      uint32_t residues = 0;
+      for (int k = node; k > 0;) {
+        const int p = par[k], t = tok[k];
+        if (t < 0 || t >= a.V) {
+          found |= kBadToken;
+        } else {
+          path[n++] = t;
+          residues |= 1u << (t & 31);
+        }
+        if (p < 0 || p >= k) {
+          found |= kBadTree;
+          break;
+        }
+        k = p;
+      }
+      n_path_s = n;
+      path_bits_s = residues;            // (which residues the path's tokens have)
     }
     __syncthreads();
   }
-  if (tid == 0) {
-    int n = 0;
-    uint32_t bits = 0;
-    for (int k = node; k > 0;) {
-      const int p = par[k], t = tok[k];
-      if (t < 0 || t >= a.V) {
-        found |= kBadToken;
-      } else {
-        path[n++] = t;
-        bits |= 1u << (t & 31);
-      }
-      if (p < 0 || p >= k) {
-        found |= kBadTree;
-        break;
-      }
-      k = p;
-    }
-    n_path_s = n;
-    path_bits_s = bits;                  // (which residues the path's tokens have)
-  }
-  __syncthreads();
-  const int n_path = n_path_s;
-  const uint32_t path_bits = path_bits_s;
-
-  const E* in = static_cast<const E*>(a.logits) + (start - off);
-  E* out = static_cast<E*>(a.out) + (start - off);
-  const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
-  float m_run = TV_NEG_INF, s_run = 0.f;
+  const int n_path = node > 0 ? n_path_s : 0;
+  const uint32_t path_bits = node > 0 ? path_bits_s : 0u;
   // how often a token is on the path
   auto times = [&](int x) {
     uint32_t n = 0;
@@ -292,70 +336,39 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       for (int i = 0; i < n_path; ++i) n += path[i] == x;
     return n;
   };
-  // this CTA's positions, whole steps of the block
-  constexpr int kBlocks = NB * kThreads, kStep = 8 * kBlocks;
-  const long long steps = (positions + kStep - 1) / kStep, per = (steps + C - 1) / C;
-  const long long p_lo = rank * per * kStep, p_hi = min(positions, p_lo + per * kStep);
-  for (long long s0 = p_lo; s0 < p_hi; s0 += kSegment) {
-    const long long s1 = min(p_hi, s0 + kSegment);
-    if (s0 > p_lo) __syncthreads();      // (the bitmaps before are done with)
-    // this segment's whole blocks [lo, hi), and the steps that hold them (what is left at the
-    // row's ends is taken element by element further down)
-    const int lo = s0 == 0 && off > 0 ? 1 : 0, hi = (int)((s1 - s0) / 8);
-    const int blocks = (hi + kBlocks - 1) / kBlocks * kBlocks;
-    const E* const in_s = in + s0 + 8 * tid;
-    E* const out_s = out + s0 + 8 * tid;
-    const int x0 = (int)(s0 - off) + 8 * tid;      // the token at this thread's first position
-    // a byte of allowed and one of marked tokens for each block
-    for (int w = tid; w < blocks / 4; w += kThreads) {
-      const long long at = s0 / 32 + w;
-      uint32_t ok = grammar ? shifted(grammar, words, at, off) : 0xffffffffu;
-      if (w == 0 && lo) ok &= 0xffffff00u;
-      const int left = 8 * hi - 32 * w;
-      if (left < 32) ok &= left > 0 ? (1u << left) - 1u : 0u;
-      const uint32_t mk = marks ? shifted(marks, words, at, off) & ok : 0u;
-      reinterpret_cast<uint2*>(bits)[w] =
-          make_uint2(__byte_perm(ok, mk, 0x5140), __byte_perm(ok, mk, 0x7362));
+
+  const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
+  float m_run = TV_NEG_INF, s_run = 0.f;
+  for (int seg = 0; seg < blocks; seg += kSegment / 8) {
+    if (seg > 0) {
+      __syncthreads();                   // (the bits before are done with)
+      look_up(seg);
+      __syncthreads();
     }
-    __syncthreads();
+    const int seg_end = min(blocks, seg + kSegment / 8);
     if (n_path > 0) {
       for (int k = tid; k < n_path; k += kThreads) {
-        const long long p = (long long)path[k] + off - s0;
-        if (p >= 0 && p < 8 * hi && (bits[p >> 3] >> (p & 7) & 1u))
+        const long long p = (long long)path[k] + off - p_lo - 8ll * seg;
+        if (p >= 0 && p < 8 * (seg_end - seg) && (bits[p >> 3] >> (p & 7) & 1u))
           atomicOr(reinterpret_cast<uint32_t*>(bits) + (p >> 4),
                    1u << ((p & 7) + 8 + 16 * (int)(p >> 3 & 1)));
       }
       __syncthreads();
     }
-    // A step's blocks of this thread: their logits, the bits of their allowed tokens and of
-    // those that are marked as well (8 a block), and the first marked one's count and bias.
+    // The bits of a step's tokens of this thread (8 a block), those that are allowed and
+    // those that are marked as well, and the first marked one's count and bias.
     auto token = [&](int b0, uint32_t m) {
       const int bit = __ffs(m) - 1;
       return x0 + 8 * (b0 + (bit >> 3) * kThreads) + (bit & 7);
     };
-    uint32_t next[NB][W], next_ok = 0, next_mk = 0, next_count = 0;
+    uint32_t next_ok = 0, next_mk = 0, next_count = 0;
     float next_bias = 0.f;
-    auto fetch = [&](int b0) {
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const int blk = b0 + tid + j * kThreads;
-        if (blk >= lo && blk < hi) {
-#pragma unroll
-          for (int k = 0; k < W; k += 4) {
-            const uint4 u = ld16(reinterpret_cast<const char*>(in_s + 8 * b0) +
-                                 j * kThreads * 8 * (int)sizeof(E) + 4 * k);
-            next[j][k] = u.x;
-            next[j][k + 1] = u.y;
-            next[j][k + 2] = u.z;
-            next[j][k + 3] = u.w;
-          }
-        }
-      }
-      if (b0 >= blocks) return;
+    auto ask = [&](int b0) {
+      if (b0 >= seg_end) return;
       next_ok = next_mk = 0;
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const uint32_t both = bits[b0 + tid + j * kThreads];
+        const uint32_t both = bits[b0 - seg + tid + j * kThreads];
         next_ok |= (both & 0xffu) << (8 * j);
         next_mk |= (both >> 8) << (8 * j);
       }
@@ -364,8 +377,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         next_bias = r.bias[token(b0, next_mk)];
       }
     };
-    fetch(0);
-    for (int b0 = 0; b0 < blocks; b0 += kBlocks) {
+    ask(seg);
+    for (int b0 = seg; b0 < seg_end; b0 += kBlocks) {
       uint32_t w[NB][W], mk = next_mk, count = next_count;
       const uint32_t ok = next_ok;
       float bias = next_bias;
@@ -374,6 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 #pragma unroll
         for (int k = 0; k < W; ++k) w[j][k] = next[j][k];
       fetch(b0 + kBlocks);
+      ask(b0 + kBlocks);
       if (mk) {         // marked tokens, through this thread's place in shared memory
 #pragma unroll
         for (int j = 0; j < NB; ++j)
@@ -412,35 +426,35 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         if (blk >= lo && blk < hi) {
 #pragma unroll
           for (int k = 0; k < W; k += 4)
-            st16(reinterpret_cast<char*>(out_s + 8 * b0) + j * kThreads * 8 * (int)sizeof(E) +
+            st16(reinterpret_cast<char*>(out + 8 * b0) + j * kThreads * 8 * (int)sizeof(E) +
                      4 * k,
                  &w[j][k]);
         }
       }
       add_blocks<L>(w, ch, cl, m_run, s_run);
     }
-    // the blocks at the row's ends, an element a thread
-    // (one block, where the row starts and ends in the same)
-    if ((lo && tid < 8) || (s1 == positions && hi >= lo && tid >= 8 && tid < 16)) {
-      const long long p = tid < 8 ? tid : s0 + 8ll * hi + (tid - 8);
-      const int x = (int)(p - off);
-      if (x >= 0 && p < positions) {
-        uint32_t n = 0, marked = 0;
-        float bias = 0.f;
-        if (marks && (marks[x >> 5] >> (x & 31) & 1u)) {
-          n = r.counts[x];
-          bias = r.bias[x];
-          marked = 1;
-        }
-        const uint32_t on_path = times(x);
-        float v = get(in + p);
-        if (marked || on_path) v = penalised(v, n, bias, on_path, r);
-        if (grammar && !(grammar[x >> 5] >> (x & 31) & 1u)) v = TV_NEG_INF;
-        E e;
-        put(&e, v);
-        out[p] = e;
-        add_one(L(), get(&e), ch, cl, m_run, s_run);
+  }
+  // the blocks at the row's ends, an element a thread (one block, where the row starts and
+  // ends in the same)
+  if ((lo && tid < 8) || (p_hi == positions && p_lo < p_hi && hi >= lo && tid >= 8 && tid < 16)) {
+    const int p = (tid < 8 ? tid : 8 * hi + (tid - 8)) - 8 * tid;   // from this thread's first
+    const int x = x0 + p;
+    if (x >= 0 && x < a.V) {
+      uint32_t n = 0;
+      float bias = 0.f;
+      const bool marked = marks && (marks[x >> 5] >> (x & 31) & 1u);
+      if (marked) {
+        n = r.counts[x];
+        bias = r.bias[x];
       }
+      const uint32_t on_path = times(x);
+      float v = get(in + p);
+      if (marked || on_path) v = penalised(v, n, bias, on_path, r);
+      if (grammar && !(grammar[x >> 5] >> (x & 31) & 1u)) v = TV_NEG_INF;
+      E e;
+      put(&e, v);
+      out[p] = e;
+      add_one(L(), get(&e), ch, cl, m_run, s_run);
     }
   }
 
@@ -589,36 +603,30 @@ cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
 
 int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
                       cudaStream_t stream) {
-  // CTAs per row: enough for four an SM, as far as each has a step of its own
-  const long long rows = (long long)a.B * (a.N + 1);
+  // CTAs per row: those whose rounds (four CTAs an SM) take the least time, counted in steps
+  // of a CTA with one and a half more for its start and end.  At V = 128256: 8 for one row
+  // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves), 1 for 7808 (where 2
+  // took 889 us for 846).
+  const long long rows = (long long)a.B * (a.N + 1), ctas = 4ll * sm_count;
+  const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2), steps = ((long long)a.V + step - 1) / step;
   int C = 1;
-  while (C < tvk::logits::kMaxCluster && rows * C < 4ll * sm_count && a.V > 8192 * C) C *= 2;
-  const bool few = rows * C <= sm_count;
-  // (a grid has at most 2^31 - 1 CTAs; the trees of one launch)
-  const long long most = std::max(1ll, 0x7fffffffll / ((long long)(a.N + 1) * C));
-  for (long long b0 = 0; b0 < a.B; b0 += most) {
-    const size_t r0 = (size_t)b0 * (a.N + 1);
-    ProcessArgs p = a;
-    const size_t at = r0 * a.V * (logit_is_bf16 ? 2 : 4);
-    p.B = (int)std::min(most, a.B - b0);
-    p.slots = a.slots ? a.slots + b0 : nullptr;
-    p.slot0 = a.slot0 + (int)b0;
-    p.parents = a.parents + r0;
-    p.tokens = a.tokens + r0;
-    p.penalties = a.penalties ? a.penalties + 3 * (size_t)b0 : nullptr;
-    p.mask_index = a.mask_index ? a.mask_index + r0 : nullptr;
-    p.logits = static_cast<const char*>(a.logits) + at;
-    p.out = static_cast<char*>(a.out) + at;
-    p.row_stats = a.row_stats + r0;
-    const cudaError_t e =
-        logit_is_bf16 ? (few ? launch_process<tvk::Bf16Logits, 512>(p, C, stream)
-                             : launch_process<tvk::Bf16Logits, 256>(p, C, stream))
-                      : (few ? launch_process<tvk::F32Logits, 512>(p, C, stream)
-                             : launch_process<tvk::F32Logits, 256>(p, C, stream));
-    if (e != cudaSuccess) {
-      cudaGetLastError();
-      return -5;
+  double least = 0;
+  for (int c = 1; c <= tvk::logits::kMaxCluster; c *= 2) {
+    const double cost = (double)((rows * c + ctas - 1) / ctas) * ((steps + c - 1) / c + 1.5);
+    if (c == 1 || cost < least) {
+      least = cost;
+      C = c;
     }
+  }
+  const bool few = rows * C <= sm_count;
+  const cudaError_t e =
+      logit_is_bf16 ? (few ? launch_process<tvk::Bf16Logits, 512>(a, C, stream)
+                           : launch_process<tvk::Bf16Logits, 256>(a, C, stream))
+                    : (few ? launch_process<tvk::F32Logits, 512>(a, C, stream)
+                           : launch_process<tvk::F32Logits, 256>(a, C, stream));
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return -5;
   }
   return 0;
 }
