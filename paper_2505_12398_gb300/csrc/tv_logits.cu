@@ -28,6 +28,7 @@ namespace tvk {
 namespace logits {
 
 constexpr int kSegment = 65536;         // tokens whose bits are in shared memory at a time
+constexpr int kListed = 96;              // marked tokens of a warp's step that it shares out
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kBadTree = 1u, kBadToken = 2u, kBadSlot = 256u, kBadMask = 512u;
 
@@ -217,7 +218,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   const int R = a.N + 1, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   uint4* stage = reinterpret_cast<uint4*>(dyn);                    // [NB * W / 4][kThreads]
   uint16_t* bits = reinterpret_cast<uint16_t*>(dyn + NB * W * kThreads);   // [kSegment / 8]
-  int* path = reinterpret_cast<int*>(bits + kSegment / 8);         // [R], then the tree's
+  uint16_t* lists = bits + kSegment / 8;                           // [kThreads / 32][2][kListed]
+  int* path = reinterpret_cast<int*>(lists + kThreads / 32 * 2 * kListed);   // [R], the tree's
   int* par = path + R;                                             // parents and tokens
   int* tok = par + R;
   uint32_t C, rank;
@@ -356,14 +358,19 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       __syncthreads();
     }
     // The bits of a step's tokens of this thread (8 a block), those that are allowed and
-    // those that are marked as well, and the first marked one's count and bias.
-    auto token = [&](int b0, uint32_t m) {
-      const int bit = __ffs(m) - 1;
-      return x0 + 8 * (b0 + (bit >> 3) * kThreads) + (bit & 7);
+    // those that are marked as well.  The marked ones of a warp are shared out among its
+    // threads, whichever hold them: a list of (thread, bit) codes, of which thread i has
+    // the i-th, the (32 + i)-th and so on.  The first one's count and bias are asked for
+    // with the logits, a step ahead of their use.
+    auto token = [&](int b0, int code) {           // (code: owner lane << 5 | bit)
+      return x0 + 8 * ((code >> 5) - lane) + 8 * (b0 + ((code >> 3) & 3) * kThreads) + (code & 7);
     };
     uint32_t next_ok = 0, next_mk = 0, next_count = 0;
+    int next_total = 0, next_code = 0;
     float next_bias = 0.f;
+    uint16_t* const list = lists + wid * 2 * kListed;
     auto ask = [&](int b0) {
+      next_total = 0;
       if (b0 >= seg_end) return;
       next_ok = next_mk = 0;
 #pragma unroll
@@ -372,15 +379,41 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         next_ok |= (both & 0xffu) << (8 * j);
         next_mk |= (both >> 8) << (8 * j);
       }
-      if (next_mk && r.counts) {
-        next_count = r.counts[token(b0, next_mk)];
-        next_bias = r.bias[token(b0, next_mk)];
+      if (!__any_sync(0xffffffffu, next_mk != 0)) return;
+      int upto = __popc(next_mk);
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += v;
       }
+      next_total = __shfl_sync(0xffffffffu, upto, 31);
+      if (next_total > kListed) return;            // (each thread takes its own)
+      uint16_t* const to = list + (b0 / kBlocks & 1) * kListed;
+      int at = upto - __popc(next_mk);
+      for (uint32_t m = next_mk; m; m &= m - 1)
+        to[at++] = (uint16_t)(lane << 5 | (__ffs(m) - 1));
+      __syncwarp();
+      if (lane < next_total) {
+        next_code = to[lane];
+        if (r.counts) {
+          next_count = r.counts[token(b0, next_code)];
+          next_bias = r.bias[token(b0, next_code)];
+        }
+      }
+    };
+    // the element of a code, in the owner's place in shared memory
+    auto element = [&](int code) {
+      const int j = code >> 3 & 3, k = code & 7;
+      return reinterpret_cast<E*>(stage + (j * (W / 4) + k * (int)sizeof(E) / 16) * kThreads +
+                                  wid * 32 + (code >> 5)) +
+             k % (16 / (int)sizeof(E));
     };
     ask(seg);
     for (int b0 = seg; b0 < seg_end; b0 += kBlocks) {
       uint32_t w[NB][W], mk = next_mk, count = next_count;
       const uint32_t ok = next_ok;
+      const int total = next_total;
+      int code = next_code;
       float bias = next_bias;
 #pragma unroll
       for (int j = 0; j < NB; ++j)
@@ -388,26 +421,31 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         for (int k = 0; k < W; ++k) w[j][k] = next[j][k];
       fetch(b0 + kBlocks);
       ask(b0 + kBlocks);
-      if (mk) {         // marked tokens, through this thread's place in shared memory
+      if (total > 0) {  // marked tokens, through shared memory
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
           for (int k = 0; k < W; k += 4)
             stage[(j * (W / 4) + k / 4) * kThreads + tid] =
                 make_uint4(w[j][k], w[j][k + 1], w[j][k + 2], w[j][k + 3]);
-        for (;;) {
-          const int bit = __ffs(mk) - 1, j = bit >> 3, k = bit & 7, x = token(b0, mk);
-          E* e = reinterpret_cast<E*>(
-                     stage + (j * (W / 4) + k * (int)sizeof(E) / 16) * kThreads + tid) +
-                 k % (16 / (int)sizeof(E));
-          put(e, penalised(get(e), count, bias, times(x), r));
-          mk &= mk - 1;
-          if (!mk) break;
-          if (r.counts) {
-            count = r.counts[token(b0, mk)];
-            bias = r.bias[token(b0, mk)];
+        __syncwarp();
+        const bool shared_out = total <= kListed;
+        const uint16_t* const from = list + (b0 / kBlocks & 1) * kListed;
+        bool asked = shared_out;
+        for (int i = lane; shared_out ? i < total : mk != 0; i += 32) {
+          if (!asked) {
+            code = shared_out ? from[i] : lane << 5 | (__ffs(mk) - 1);
+            if (r.counts) {
+              count = r.counts[token(b0, code)];
+              bias = r.bias[token(b0, code)];
+            }
           }
+          asked = false;
+          mk &= mk - 1;
+          E* const e = element(code);
+          put(e, penalised(get(e), count, bias, times(token(b0, code)), r));
         }
+        __syncwarp();
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -415,6 +453,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
             const uint4 u = stage[(j * (W / 4) + k / 4) * kThreads + tid];
             w[j][k] = u.x; w[j][k + 1] = u.y; w[j][k + 2] = u.z; w[j][k + 3] = u.w;
           }
+        __syncwarp();
       }
       if (ok != (NB == 4 ? 0xffffffffu : 0xffffu)) {
 #pragma unroll
@@ -577,7 +616,7 @@ cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
   using namespace tvk::logits;
   const size_t smem =
       4 * ((size_t)Block<L>::kBlocks * Block<L>::kWords * kThreads + kSegment / 16 +
-           3 * (size_t)(a.N + 1));
+           kThreads / 32 * kListed + 3 * (size_t)(a.N + 1));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(a.B * (a.N + 1) * C), 1, 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
