@@ -692,7 +692,7 @@ int tv_rms_norm(tv_handle* h, int M, int K, tv_dtype dtype, const void* x, const
   if (!guard.ok()) return TV_ERR_CUDA;
   const int rc = tv_launch_rms_norm(M, K, dtype == TV_BF16, x, residual, weight_dtype == TV_BF16,
                                     weight, eps, out_residual, out, out_scales,
-                                    static_cast<cudaStream_t>(cuda_stream));
+                                    h->dev.sm_count, static_cast<cudaStream_t>(cuda_stream));
   return rc == 0 ? TV_OK : TV_ERR_CUDA;
 }
 

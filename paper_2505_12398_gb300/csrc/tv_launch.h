@@ -189,7 +189,7 @@ int tv_norm_max_columns();
 // else in bf16.  residual and out_residual may be null.  0 or -5.
 int tv_launch_rms_norm(int M, int K, int x_is_bf16, const void* x, const void* residual,
                        int weight_is_bf16, const void* weight, float eps, void* out_residual,
-                       void* out, float* out_scales, cudaStream_t stream);
+                       void* out, float* out_scales, int sm_count, cudaStream_t stream);
 // weight[V][K] (K % 16 == 0) in e4m3 with a scale per 128 x 128 block.  0 or -5.
 int tv_launch_quantize_weight(int V, int K, int is_bf16, const void* weight, void* out,
                               float* out_scales, cudaStream_t stream);

@@ -19,6 +19,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "tv_device.cuh"
 #include "tv_launch.h"
@@ -629,11 +630,16 @@ cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (smem > 48u << 10) {
-    const cudaError_t e = cudaFuncSetAttribute(process_kernel<L, kThreads>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               96 << 10);
+  // the same limit for every launch, set once per device
+  static std::atomic<uint64_t> set{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  if (device >= 64 || !(set.load() >> device & 1u)) {
+    e = cudaFuncSetAttribute(process_kernel<L, kThreads>,
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, 96 << 10);
     if (e != cudaSuccess) return e;
+    if (device < 64) set.fetch_or(1ull << device);
   }
   return cudaLaunchKernelEx(&cfg, process_kernel<L, kThreads>, a);
 }

@@ -61,6 +61,18 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
   v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
   v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
 }
+// The same before it is widened, so that many can be on their way.
+template <typename X>
+struct Raw8 {
+  uint4 v[sizeof(X) / 2];
+  __device__ __forceinline__ void load(const X* p) {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(X) / 2); ++k) v[k] = reinterpret_cast<const uint4*>(p)[k];
+  }
+  __device__ __forceinline__ void widen(float (&f)[8]) const {
+    load8(reinterpret_cast<const X*>(v), f);
+  }
+};
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
   uint32_t w[4];
 #pragma unroll
@@ -78,7 +90,7 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 // One CTA per row.  Every element of the row is read before any is written, so
 // out_residual may be x or residual.  kSteps * blockDim.x * 8 >= K.
 template <typename X, typename W, bool kQuant, int kSteps>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(kSteps < kMaxSteps ? 512 : 1024)
     rms_norm_kernel(const X* x, const X* residual, const W* __restrict__ weight, int K, float eps,
                     X* out_residual, __nv_bfloat16* __restrict__ out_bf16,
                     uint8_t* __restrict__ out_e4m3, float* __restrict__ out_scales) {
@@ -87,24 +99,33 @@ __global__ void __launch_bounds__(1024)
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = blockDim.x >> 5;
   float h[kSteps][kVec];
   float sq = 0.f;
+  // all of a thread's loads at once (of the longest rows, more than the registers hold, a
+  // step's); columns past the end read the last ones
+  constexpr int kAtOnce = kSteps < kMaxSteps ? kSteps : 1;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int c = (i * (int)blockDim.x + tid) * kVec;
+  for (int i0 = 0; i0 < kSteps; i0 += kAtOnce) {
+    Raw8<X> rx[kAtOnce], rr[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) h[i][k] = 0.f;
-    if (c < K) {
-      load8(x + row * K + c, h[i]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int c = min(((i0 + i) * (int)blockDim.x + tid) * kVec, K - kVec);
+      rx[i].load(x + row * K + c);
+      if (residual) rr[i].load(residual + row * K + c);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      float (&hi)[kVec] = h[i0 + i];
+      rx[i].widen(hi);
       if (residual) {
         float r[kVec];
-        load8(residual + row * K + c, r);
+        rr[i].widen(r);
 #pragma unroll
-        for (int k = 0; k < kVec; ++k) h[i][k] += r[k];
+        for (int k = 0; k < kVec; ++k) hi[k] += r[k];
       }
-    }
-    float t[kVec];
+      float t[kVec];
 #pragma unroll
-    for (int k = 0; k < kVec; ++k) t[k] = h[i][k] * h[i][k];
-    sq += sum8(t);
+      for (int k = 0; k < kVec; ++k) t[k] = hi[k] * hi[k];
+      if (((i0 + i) * (int)blockDim.x + tid) * kVec < K) sq += sum8(t);
+    }
   }
   sq = warp_sum(sq);
   if (lane == 0) red[wid] = sq;
@@ -143,7 +164,7 @@ __global__ void __launch_bounds__(1024)
 
 // One CTA per 128 x 128 block: 8 threads a row (16 columns each), 32 rows a step.
 template <typename X>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, sizeof(X) == 2 ? 3 : 2)
     quantize_block_kernel(const X* __restrict__ w, int V, int K, uint8_t* __restrict__ out,
                           float* __restrict__ scales) {
   __shared__ float red[8];
@@ -195,11 +216,19 @@ __global__ void __launch_bounds__(256)
 
 template <typename X, typename W, bool kQuant>
 int launch_norm(int M, int K, const void* x, const void* residual, const void* weight, float eps,
-                void* out_residual, void* out, float* out_scales, cudaStream_t stream) {
-  // up to 1024 threads; more columns than they hold in one step take several
+                void* out_residual, void* out, float* out_scales, int sm_count,
+                cudaStream_t stream) {
+  // Few rows: a thread for every 8 columns, up to 512 (61 x 4096: 2.3 us, 2.7 with half as
+  // many).  Many: four steps of a thread in bf16, two in fp32, so that its loads are on
+  // their way at once and an SM holds more rows, whose waits for their sums and stores
+  // overlap (15625 x 4096: 79 us with 512 threads, 70 with 256, 68 with 128, where 66 is
+  // the floor).
   const int vecs = (K + kVec - 1) / kVec;
+  const int aim = M <= 2 * sm_count ? 1 : sizeof(X) == 2 ? 4 : 2;
   int steps = 1;
-  while (steps < kMaxSteps && (vecs + steps - 1) / steps > 512) steps *= 2;
+  while (steps < kMaxSteps && ((steps < aim && vecs > 64 * steps) ||
+                               (vecs + steps - 1) / steps > 512))
+    steps *= 2;
   const int threads = std::min(1024, ((vecs + steps - 1) / steps + 31) / 32 * 32);
   auto run = [&](auto kernel) {
     kernel<<<M, threads, 0, stream>>>(
@@ -219,12 +248,12 @@ int launch_norm(int M, int K, const void* x, const void* residual, const void* w
 template <typename X>
 int launch_norm_of(int M, int K, const void* x, const void* residual, const void* weight,
                    int weight_is_bf16, float eps, void* out_residual, void* out,
-                   float* out_scales, cudaStream_t stream) {
+                   float* out_scales, int sm_count, cudaStream_t stream) {
   auto run = weight_is_bf16
                  ? (out_scales ? launch_norm<X, __nv_bfloat16, true>
                                : launch_norm<X, __nv_bfloat16, false>)
                  : (out_scales ? launch_norm<X, float, true> : launch_norm<X, float, false>);
-  return run(M, K, x, residual, weight, eps, out_residual, out, out_scales, stream);
+  return run(M, K, x, residual, weight, eps, out_residual, out, out_scales, sm_count, stream);
 }
 
 }  // namespace norm
@@ -234,9 +263,10 @@ int tv_norm_max_columns() { return tvk::norm::kMaxSteps * 1024 * tvk::norm::kVec
 
 int tv_launch_rms_norm(int M, int K, int x_is_bf16, const void* x, const void* residual,
                        int weight_is_bf16, const void* weight, float eps, void* out_residual,
-                       void* out, float* out_scales, cudaStream_t stream) {
+                       void* out, float* out_scales, int sm_count, cudaStream_t stream) {
   auto run = x_is_bf16 ? tvk::norm::launch_norm_of<__nv_bfloat16> : tvk::norm::launch_norm_of<float>;
-  return run(M, K, x, residual, weight, weight_is_bf16, eps, out_residual, out, out_scales, stream);
+  return run(M, K, x, residual, weight, weight_is_bf16, eps, out_residual, out, out_scales,
+             sm_count, stream);
 }
 
 int tv_launch_quantize_weight(int V, int K, int is_bf16, const void* weight, void* out,
