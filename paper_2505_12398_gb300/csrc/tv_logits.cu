@@ -71,8 +71,7 @@ struct Row {
 };
 
 // The logit of a marked token, on the path `times` times.  (A positive one is multiplied by
-// 1 / rep: one more rounding in 32 bits than the division, below the one to the logits'
-// type, for a tenth of its instructions.)
+// 1 / rep: one more rounding of 2^-24 than the division, for a tenth of its instructions.)
 __device__ __forceinline__ float penalised(float l, uint32_t count, float bias, uint32_t times,
                                            const Row& r) {
   const uint32_t n = (count >> 1) + times;
@@ -226,6 +225,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   uint32_t C, rank;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  // (the CTAs write to the first one's shared memory at the end, by when it has to run)
+  if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   const int row_id = blockIdx.x / C, b = row_id / R, node = row_id - b * R;
   const size_t row = row_id, start = row * a.V;
   const int off = (int)(start & 7);
@@ -508,6 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   float s = m_run == TV_NEG_INF ? 0.f : s_run * rescale(L(), m_run, m, ch, cl);
   s = warp_sum(s);
   if (lane == 0) red[1][wid] = s;
+  if (C > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
   if (tid == 0) {
     s = 0.f;
