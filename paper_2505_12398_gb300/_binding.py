@@ -293,14 +293,15 @@ class Verifier:
     def _stream(self, stream):
         return _raw_stream(self.device.index or 0) if stream is None else stream.cuda_stream
 
-    def _empty(self, stream, shape, dtype):
-        """A new output, of the stream that writes it: memory of another stream's might
-        still be in use there."""
+    def _empty(self, stream, *outputs):
+        """New outputs ((shape, dtype) or None each), of the stream that writes them: memory
+        of another stream's might still be in use there."""
         import torch
-        if stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._empty(None, *outputs)
+        empty, dev = torch.empty, self.device
+        return [empty(o[0], dtype=o[1], device=dev) if o is not None else None for o in outputs]
 
     def _float_code(self, t, name):
         import torch
@@ -327,9 +328,9 @@ class Verifier:
         kind = torch.float8_e4m3fn if quantize else torch.bfloat16
         groups = (K + GROUP - 1) // GROUP
         if out is None:
-            y = self._empty(stream, (M, K), kind)
-            scales = self._empty(stream, (M, groups), torch.float32) if quantize else None
-            total = self._empty(stream, (M, K), x.dtype) if residual is not None else None
+            y, scales, total = self._empty(
+                stream, ((M, K), kind), ((M, groups), torch.float32) if quantize else None,
+                ((M, K), x.dtype) if residual is not None else None)
         else:
             y, scales, total = out if quantize else (out[0], None, out[1])
             _check_out(y, kind, (M, K), self.device)
@@ -355,8 +356,8 @@ class Verifier:
         _check_in(weight, weight.dtype, (rows, K), self.device, "weight")
         blocks = ((rows + GROUP - 1) // GROUP, (K + GROUP - 1) // GROUP)
         if out is None:
-            q = self._empty(stream, (rows, K), torch.float8_e4m3fn)
-            scales = self._empty(stream, blocks, torch.float32)
+            q, scales = self._empty(stream, ((rows, K), torch.float8_e4m3fn),
+                                    (blocks, torch.float32))
         else:
             q, scales = out
             _check_out(q, torch.float8_e4m3fn, (rows, K), self.device)
@@ -383,9 +384,9 @@ class Verifier:
         _check_in(weight_scales, torch.float32, ((V + GROUP - 1) // GROUP, groups), self.device,
                   "weight_scales")
         if out is None:
-            logits = self._empty(stream, (M, V), torch.bfloat16)
-            row_stats = self._empty(stream, (M, 2), torch.float32) \
-                if temperature is not None else None
+            logits, row_stats = self._empty(
+                stream, ((M, V), torch.bfloat16),
+                ((M, 2), torch.float32) if temperature is not None else None)
         else:
             logits, row_stats = out
             _check_out(logits, torch.bfloat16, (M, V), self.device)
@@ -431,8 +432,8 @@ class Verifier:
         if context is not None and (context.vocab != V or context.device != self.device):
             raise ValueError("the context is for another vocabulary or device")
         if out is None:
-            res = self._empty(stream, (B, R, V), self.logit_dtype)
-            row_stats = self._empty(stream, (B, R, 2), torch.float32)
+            res, row_stats = self._empty(stream, ((B, R, V), self.logit_dtype),
+                                         ((B, R, 2), torch.float32))
         else:
             res, row_stats = out
             _check_out(res, self.logit_dtype, (B, R, V), self.device)

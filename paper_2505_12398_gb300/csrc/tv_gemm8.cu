@@ -8,14 +8,39 @@
 // second.  The logits are rounded once to bf16; on request each stored row's
 // normaliser (max, sum of 2^((l - max) c)) comes with them.
 //
-// One persistent kernel, one CTA per SM (SM pairs above 128 rows), with the ring,
-// tile order and roles of the bf16 LM head.  What differs: the scales are general fp32
-// numbers, so the tensor cores' own block scaling (powers of two) does not serve.  A
-// stage holds one group of K (128 bytes of a row, one swizzle row); its four
-// tcgen05.mma of kind::f8f6f4 start from zero in one of two tensor-memory
-// accumulators of up to 256 columns, and 16 warps add s P_g to fp32 sums in their
-// registers (64 columns of a row per thread) while the tensor cores work on the next
-// group.  Every wait is bounded, as there.
+// The scales are general fp32 numbers, so the tensor cores' own block scaling (powers of
+// two) does not serve: every group's product P_g is made from zero (four tcgen05.mma of
+// kind::f8f6f4 on the group's 128 bytes a row) and added, times its scale, to fp32 sums
+// in registers.  A group of a 128 x 256 tile costs the tensor cores 512 clocks; its 32768
+// multiply-adds take 128 lanes 256, and bringing the product from tensor memory some 100
+// more.  The two have to run side by side all the time: that sets the layout.
+//
+// One persistent kernel, one CTA of 12 warps per SM (SM pairs above 128 rows, which halve
+// W's traffic through L2):
+//   warp 0       TMA into a ring of stages, one group of K each
+//   warps 1, 3   the products, one warp for each half of the tile's columns
+//   warp 2       the scales, by 4-byte asynchronous copies into a ring of their own
+//   warps 4-11   the sums: two warps for each quarter of the rows, one per half of the
+//                columns; 128 fp32 sums and one row a thread, in registers that the other
+//                warps give up (232 of them for 40)
+// Tensor memory holds four products of 128 columns, two for each half, so that one is
+// made while the one before is summed.  Each is read in pieces of 32 and 16 columns, one
+// on its way while the last is summed, two columns per multiply-add.  At the end of a
+// tile the sums are rounded once to bf16; pairs store them through shared memory and TMA,
+// in the shadow of the next tile's first products.
+//
+// Every wait is bounded; one that gives up raises the timeout status, and the loops go on
+// to their end.
+//
+// Measured, without row statistics (GB300, inputs from memory):
+//   7808 x 4096 x 128256   2937 us, 2790 TFLOP/s, under the power cap (2541 us, 3230
+//                          TFLOP/s, in bursts; the products alone 1732 us; twice the bf16
+//                          rate of a plain library product would be 2135 us)
+//   3904 x 4096 x  32000    386 us, 2650 TFLOP/s (348 us in bursts)
+//     61 x 4096 x 128256     87 us, 6.2 TB/s: the weight's bytes
+//      1 x 4096 x  32000     27 us, 4.9 TB/s: the same, with the launch and its ends
+// A group takes the sums' warps 630 clocks of which 370 are their loads and multiply-adds
+// in isolation; the tensor cores idle for the rest of 630 less 513.
 #include <limits.h>
 
 #include <algorithm>
@@ -57,7 +82,7 @@ constexpr size_t kSmemBytes =
 // (one more, which the reads ahead at the ring's end fall on)
 constexpr int kHalf = 128;                      // columns of a product: a tile has one or two
 constexpr int kBufs = 4;                        // products in tensor memory
-constexpr int kHalves = kBN / kHalf;            // = 32-column chunks of a thread at most
+constexpr int kHalves = kBN / kHalf;
 constexpr int kChunks = 4;                      // 32-column chunks of a thread
 static_assert(kHalf == 32 * kChunks * kParts / kHalves && kBufs * kHalf == (int)kTmemCols, "");
 
@@ -275,10 +300,11 @@ __device__ __forceinline__ void store_tile(const uint32_t (&packed)[16], uint32_
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
   if (lane == 0) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::
-                     "l"(reinterpret_cast<uint64_t>(map)),
-                 "r"(x), "r"(y), "r"(buf)
-                 : "memory");
+    asm volatile(
+        "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+            reinterpret_cast<uint64_t>(map)),
+        "r"(x), "r"(y), "r"(buf)
+        : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
@@ -437,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (warp >= 4) {
     regs_more<kRegsMany>();
-    // ---- scaled sums: one row per thread, every other 32-column chunk ----
+    // ---- scaled sums: one row and 128 columns (half of the tile's at most) a thread ----
     const int q = warp & 3;                       // the TMEM lane quarter of this warp
     const int mine = (warp - 4) >> 2;
     const float2 ch = make_float2(c_hi, c_hi), cl = make_float2(c_lo, c_lo);
@@ -578,117 +604,119 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (kPair && lane == 0) stores_read<0>();     // (the buffers go with the CTA)
     if (bad) failed = 1;
   } else {
-  regs_fewer<kRegsFew>();
-  if (warp == 0) {
-    // ---- TMA producer: one ring across all of this CTA's tiles ----
-    uint32_t it = 0, s = 0, ph = 0;
-    bool ok = true;
-    for (int t = first; t < n_total && ok; t += step) {
-      int mt, nt;
-      tile_coords(t, m_tiles, n_tiles, group, mt, nt);
-      const int m0 = mt * tile_rows + (int)rank * kBM, n0 = nt * bn + (int)rank * w_own;
-      const int n1 = nt * bn + kHalf + (int)rank * (n_half[1] / 2);
-      for (int kb = 0; kb < nkb; ++kb, ++it) {
-        if (it >= n_stages && !wait_warp(&empty_bar[s], ph ^ 1u)) {
-          ok = false;
-          break;
+    regs_fewer<kRegsFew>();
+    if (warp == 0) {
+      // ---- TMA producer: one ring across all of this CTA's tiles ----
+      uint32_t it = 0, s = 0, ph = 0;
+      bool ok = true;
+      for (int t = first; t < n_total && ok; t += step) {
+        int mt, nt;
+        tile_coords(t, m_tiles, n_tiles, group, mt, nt);
+        const int m0 = mt * tile_rows + (int)rank * kBM, n0 = nt * bn + (int)rank * w_own;
+        const int n1 = nt * bn + kHalf + (int)rank * (n_half[1] / 2);
+        for (int kb = 0; kb < nkb; ++kb, ++it) {
+          if (it >= n_stages && !wait_warp(&empty_bar[s], ph ^ 1u)) {
+            ok = false;
+            break;
+          }
+          uint8_t* a = smem + s * stage_bytes;
+          uint32_t bar = smem_u32(&full_bar[s]);
+          if constexpr (kPair) bar = map_shared(&full_bar[s], 0);
+          if (elect_one()) {
+            if (rank == 0)
+              mbar_arrive_expect_tx(&full_bar[s], kPair ? 2 * stage_bytes : stage_bytes);
+            tma_load_2d<kPair>(a, &map_h, kb * kGroup, m0, bar);
+            tma_load_2d<kPair>(a + a_bytes, &map_w, kb * kGroup, n0, bar);
+            if (kPair && n_half[1] > 0)
+              tma_load_2d<kPair>(a + a_bytes + w_own * kGroup, &map_w1, kb * kGroup, n1, bar);
+          }
+          __syncwarp();
+          if (++s == n_stages) { s = 0; ph ^= 1u; }
         }
-        uint8_t* a = smem + s * stage_bytes;
-        uint32_t bar = smem_u32(&full_bar[s]);
-        if constexpr (kPair) bar = map_shared(&full_bar[s], 0);
-        if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(&full_bar[s], kPair ? 2 * stage_bytes : stage_bytes);
-          tma_load_2d<kPair>(a, &map_h, kb * kGroup, m0, bar);
-          tma_load_2d<kPair>(a + a_bytes, &map_w, kb * kGroup, n0, bar);
-          if (kPair && n_half[1] > 0)
-            tma_load_2d<kPair>(a + a_bytes + w_own * kGroup, &map_w1, kb * kGroup, n1, bar);
+      }
+      if (!ok) failed = 1;
+      if (rank == 0)      // the copies issued last have landed before the CTA may exit
+        for (uint32_t j = it > n_stages ? it - n_stages : 0u; j < it; ++j)
+          if (!wait_warp(&full_bar[j % n_stages], (j / n_stages) & 1)) failed = 1;
+    } else if (warp == 1 || warp == 3) {
+      // ---- tensor-core issue: each group's products into the accumulators in turn ----
+      // One warp for each half of the columns: a warp's own instructions (two waits, four
+      // products, two commits) take about 400 clocks a half, more than its products' 256.
+      const int half = warp >> 1;
+      if (rank == 0 && n_half[half] > 0) {
+        const uint32_t idesc = instr_desc(tile_rows, n_half[half]);
+        const uint64_t desc = smem_desc(smem);
+        const uint32_t desc_hi = (uint32_t)(desc >> 32), desc_lo = (uint32_t)desc;
+        const uint32_t b_off = (a_bytes + (uint32_t)(half * w_own * kGroup)) >> 4;
+        const uint32_t full0 = opaque(smem_u32(full_bar)), empty0 = smem_u32(empty_bar);
+        const uint32_t acc_f = smem_u32(&acc_full[half]);
+        const uint32_t acc_e = opaque(smem_u32(&acc_empty[half]));
+        const uint32_t d0 = tmem + (uint32_t)(kHalf * half);
+        uint32_t s = 0, lo = desc_lo, ph = 0;       // the stage, its descriptor, its phase
+        uint32_t buf = 0, aph = 1;                  // the buffer, its release's phase
+        uint32_t bad = 0;
+        const int tiles = first < n_total ? (n_total - first + step - 1) / step : 0;
+        for (int left = tiles * nkb; left > 0; --left) {
+          wait_on(full0 + 8 * s, ph, bad);
+          // (the first use of a buffer waits for the phase before the first, which is over)
+          wait_on(acc_e + 16 * buf, aph, bad);
+          if (__any_sync(0xffffffffu, bad)) break;
+          tc_fence_after();
+          if (elect_one()) {
+            issue<kPair>(d0 + 256 * buf, lo, lo + b_off, desc_hi, idesc);
+            commit_to<kPair>(acc_f + 16 * buf);
+            commit_to<kPair>(empty0 + 8 * s);
+          }
+          __syncwarp();
+          buf ^= 1u;
+          aph ^= buf ^ 1u;
+          lo += stage_bytes >> 4;
+          if (++s == n_stages) {
+            s = 0;
+            lo = desc_lo;
+            ph ^= 1u;
+          }
         }
+        if (bad) failed = 1;
+        // every MMA issued has finished before tensor memory is freed
+        if (elect_one()) umma_commit<kPair>(&drain_bar);
         __syncwarp();
-        if (++s == n_stages) { s = 0; ph ^= 1u; }
       }
-    }
-    if (!ok) failed = 1;
-    if (rank == 0)      // the copies issued last have landed before the CTA may exit
-      for (uint32_t j = it > n_stages ? it - n_stages : 0u; j < it; ++j)
-        if (!wait_warp(&full_bar[j % n_stages], (j / n_stages) & 1)) failed = 1;
-  } else if (warp == 1 || warp == 3) {
-    // ---- tensor-core issue: each group's products into the accumulators in turn ----
-    // One warp for each half of the columns: a warp's own instructions (two waits, four
-    // products, two commits) take about 400 clocks a half, more than its products' 256.
-    const int half = warp >> 1;
-    if (rank == 0 && n_half[half] > 0) {
-      const uint32_t idesc = instr_desc(tile_rows, n_half[half]);
-      const uint64_t desc = smem_desc(smem);
-      const uint32_t desc_hi = (uint32_t)(desc >> 32), desc_lo = (uint32_t)desc;
-      const uint32_t b_off = (a_bytes + (uint32_t)(half * w_own * kGroup)) >> 4;
-      const uint32_t full0 = opaque(smem_u32(full_bar)), empty0 = smem_u32(empty_bar);
-      const uint32_t acc_f = smem_u32(&acc_full[half]), acc_e = opaque(smem_u32(&acc_empty[half]));
-      const uint32_t d0 = tmem + (uint32_t)(kHalf * half);
-      uint32_t s = 0, lo = desc_lo, ph = 0;       // the stage, its descriptor, its phase
-      uint32_t buf = 0, aph = 1;                  // the buffer, its release's phase
-      uint32_t bad = 0;
-      const int tiles = first < n_total ? (n_total - first + step - 1) / step : 0;
-      for (int left = tiles * nkb; left > 0; --left) {
-        wait_on(full0 + 8 * s, ph, bad);
-        // (the first use of a buffer waits for the phase before the first, which is over)
-        wait_on(acc_e + 16 * buf, aph, bad);
-        if (__any_sync(0xffffffffu, bad)) break;
-        tc_fence_after();
-        if (elect_one()) {
-          issue<kPair>(d0 + 256 * buf, lo, lo + b_off, desc_hi, idesc);
-          commit_to<kPair>(acc_f + 16 * buf);
-          commit_to<kPair>(empty0 + 8 * s);
-        }
-        __syncwarp();
-        buf ^= 1u;
-        aph ^= buf ^ 1u;
-        lo += stage_bytes >> 4;
-        if (++s == n_stages) {
-          s = 0;
-          lo = desc_lo;
-          ph ^= 1u;
+      // (kPair, the peer: the leader's last signal)
+      if (!wait_warp(&drain_bar, 0)) failed = 1;
+    } else if (warp == 2) {
+      // ---- scales: a slot of groups ahead of the sums, straight to shared memory ----
+      const int w_blocks = (V + kGroup - 1) / kGroup;
+      uint32_t it = 0;
+      bool ok = true;
+      for (int t = first; t < n_total && ok; t += step) {
+        int mt, nt;
+        tile_coords(t, m_tiles, n_tiles, group, mt, nt);
+        const int row0 = mt * tile_rows + (int)rank * kBM + lane, n0 = nt * bn;
+        const int blk = min((n0 + 32 * (lane & 7)) / kGroup, w_blocks - 1);
+        for (int kb0 = 0; kb0 < nkb; kb0 += kScaleGroups, ++it) {
+          const uint32_t slot = it % kScaleSlots;
+          if (it >= kScaleSlots && !wait_warp(&scale_empty[slot], ((it / kScaleSlots) - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          const int groups = min(kScaleGroups, nkb - kb0);
+  #pragma unroll
+          for (int r = 0; r < kBM / 32; ++r) {
+            const float* src = h_scale + (size_t)min(row0 + 32 * r, M - 1) * nkb + kb0;
+            for (int k = 0; k < groups; ++k)
+              copy_async4(&scales[slot * kScaleGroups + k].row[lane + 32 * r], src + k);
+          }
+          for (int k = lane >> 3; k < groups; k += 4)
+            copy_async4(&scales[slot * kScaleGroups + k].chunk[lane & 7],
+                        w_scale + (size_t)blk * nkb + kb0 + k);
+          copy_async_arrive(&scale_full[slot]);
         }
       }
-      if (bad) failed = 1;
-      // every MMA issued has finished before tensor memory is freed
-      if (elect_one()) umma_commit<kPair>(&drain_bar);
-      __syncwarp();
+      if (!ok) failed = 1;
+      // the copies issued last have landed before the CTA may exit
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    // (kPair, the peer: the leader's last signal)
-    if (!wait_warp(&drain_bar, 0)) failed = 1;
-  } else if (warp == 2) {
-    // ---- scales: a slot of groups ahead of the sums, straight to shared memory ----
-    const int w_blocks = (V + kGroup - 1) / kGroup;
-    uint32_t it = 0;
-    bool ok = true;
-    for (int t = first; t < n_total && ok; t += step) {
-      int mt, nt;
-      tile_coords(t, m_tiles, n_tiles, group, mt, nt);
-      const int row0 = mt * tile_rows + (int)rank * kBM + lane, n0 = nt * bn;
-      const int blk = min((n0 + 32 * (lane & 7)) / kGroup, w_blocks - 1);
-      for (int kb0 = 0; kb0 < nkb; kb0 += kScaleGroups, ++it) {
-        const uint32_t slot = it % kScaleSlots;
-        if (it >= kScaleSlots && !wait_warp(&scale_empty[slot], ((it / kScaleSlots) - 1) & 1)) {
-          ok = false;
-          break;
-        }
-        const int groups = min(kScaleGroups, nkb - kb0);
-#pragma unroll
-        for (int r = 0; r < kBM / 32; ++r) {
-          const float* src = h_scale + (size_t)min(row0 + 32 * r, M - 1) * nkb + kb0;
-          for (int k = 0; k < groups; ++k)
-            copy_async4(&scales[slot * kScaleGroups + k].row[lane + 32 * r], src + k);
-        }
-        for (int k = lane >> 3; k < groups; k += 4)
-          copy_async4(&scales[slot * kScaleGroups + k].chunk[lane & 7],
-                      w_scale + (size_t)blk * nkb + kb0 + k);
-        copy_async_arrive(&scale_full[slot]);
-      }
-    }
-    if (!ok) failed = 1;
-    // the copies issued last have landed before the CTA may exit
-    asm volatile("cp.async.wait_all;" ::: "memory");
-  }
   }
   tc_fence_before();
   __syncthreads();
@@ -790,10 +818,10 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w,
                     : kPair ? kStoreTma
                     : V % 16 == 0 && (reinterpret_cast<uintptr_t>(logits) & 31u) == 0 ? kStore32
                                                                                      : kStore16;
-  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, map_w1, map_out, h_scale,
-                            w_scale,
-                            M, V, K, shape, c_hi, c_lo, static_cast<__nv_bfloat16*>(logits), part,
-                            m_tiles, n_tiles, group, store, status);
+  return cudaLaunchKernelEx(&cfg, lm_head8_kernel<kPair, kStats>, map_h, map_w, map_w1, map_out,
+                            h_scale, w_scale, M, V, K, shape, c_hi, c_lo,
+                            static_cast<__nv_bfloat16*>(logits), part, m_tiles, n_tiles, group,
+                            store, status);
 }
 
 template <bool kPair, bool kStats>
@@ -897,8 +925,8 @@ int tv_launch_lm_head_scaled(const void* hidden, const float* hidden_scales, con
   const int group = (int)std::max<size_t>(1, kGroupBytes / ((size_t)tile_rows * K));
   auto run = pair ? (row_stats ? launch<true, true> : launch<true, false>)
                   : (row_stats ? launch<false, true> : launch<false, false>);
-  if (run(map_h, map_w, map_w1, map_out, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo, logits, part,
-          m_tiles, n_tiles, group, units, status, stream) != cudaSuccess) {
+  if (run(map_h, map_w, map_w1, map_out, hidden_scales, weight_scales, M, V, K, shape, c_hi, c_lo,
+          logits, part, m_tiles, n_tiles, group, units, status, stream) != cudaSuccess) {
     cudaGetLastError();
     return -5;
   }

@@ -196,15 +196,22 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
   return __funnelshift_r(lo, hi, 32 - shift);
 }
 
-// One cluster of CTAs per row.  A row is taken in blocks of 8 logits at 8-element
+// One cluster of CTAs per row.  What bounds it: the logits' bytes, read and written once,
+// with the loads of the next step on their way while this one is worked on, and about as
+// much issue: two exponentials, their sums, the bits and the conversions of each pair.  At
+// 128 x 61 x 128256 in bf16, 745 us, 5.4 TB/s (the copy's rate would be 600 us); at 32 x 26 x
+// 32003 in fp32, 74 us, 3.0 TB/s (rows that start at any element); one row of 128256 takes
+// about 8 us on a cluster of 8 CTAs, most of it the launch, the look-ups and the join.
+//
+// A row is taken in blocks of 8 logits at 8-element
 // boundaries of the whole array (16-byte loads wherever the row starts; the first and last
 // block may hold elements of other rows, which are neither read nor written): position p
 // of a row is its token p - off.  Shared memory holds two bytes for each block: a bit for
 // each token that the grammar and the row's ends leave, and for each of those that has a
-// count, a bias or a place on the path.  What bounds it: the logits'
-// bytes, read and written once, with the loads of the next blocks on their way while
-// these are worked on; the marked tokens' counts and biases are gathered where a block
-// has any.
+// count, a bias or a place on the path; only their counts and biases are gathered.
+// Tried and slower at 128 x 61 x 128256: bits of 131072 tokens at a time (833 us for 752),
+// the row's marked tokens listed beforehand (1152), loads by a warp of their own through
+// shared memory with persistent CTAs (1502).
 template <typename L, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     process_kernel(ProcessArgs a) {
@@ -655,7 +662,8 @@ int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
   // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves), 1 for 7808 (where 2
   // took 889 us for 846).
   const long long rows = (long long)a.B * (a.N + 1), ctas = 4ll * sm_count;
-  const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2), steps = ((long long)a.V + step - 1) / step;
+  const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2);
+  const long long steps = ((long long)a.V + step - 1) / step;
   int C = 1;
   double least = 0;
   for (int c = 1; c <= tvk::logits::kMaxCluster; c *= 2) {

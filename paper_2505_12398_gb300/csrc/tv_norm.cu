@@ -11,7 +11,11 @@
 // Both are bound by their bytes.  The norm keeps a row in the registers of one CTA (8
 // consecutive columns, 16 bytes of bf16, per thread and step), so x and r are read once;
 // 16 neighbouring threads hold a group, whose largest magnitude is four shuffles away.
-// The quantiser keeps a block in the registers of one CTA.
+// The quantiser keeps a block in the registers of one CTA.  Measured (GB300, bf16, e4m3
+// out): norm of 7808 x 4096, 38.6 us, 5.8 TB/s (floor 33.2); of 61 x 4096, 2.3 us of the
+// GPU; quantiser of 32000 x 2048, 34.9 us, 5.6 TB/s (29.0); of 128256 x 4096, 242 us, 6.5
+// TB/s (232.5).  A ring of TMA copies with persistent CTAs in the norm's place took 40.8 us
+// at 7808 x 4096 and 72 us for 36 at 30000 x 1024.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -264,7 +268,8 @@ int tv_norm_max_columns() { return tvk::norm::kMaxSteps * 1024 * tvk::norm::kVec
 int tv_launch_rms_norm(int M, int K, int x_is_bf16, const void* x, const void* residual,
                        int weight_is_bf16, const void* weight, float eps, void* out_residual,
                        void* out, float* out_scales, int sm_count, cudaStream_t stream) {
-  auto run = x_is_bf16 ? tvk::norm::launch_norm_of<__nv_bfloat16> : tvk::norm::launch_norm_of<float>;
+  auto run =
+      x_is_bf16 ? tvk::norm::launch_norm_of<__nv_bfloat16> : tvk::norm::launch_norm_of<float>;
   return run(M, K, x, residual, weight, weight_is_bf16, eps, out_residual, out, out_scales,
              sm_count, stream);
 }
