@@ -29,6 +29,7 @@ namespace tvk {
 namespace logits {
 
 constexpr int kSegment = 65536;         // tokens whose bits are in shared memory at a time
+constexpr int kPathBits = 4096;
 constexpr int kListed = 96;              // marked tokens of a warp's step that it shares out
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kBadTree = 1u, kBadToken = 2u, kBadSlot = 256u, kBadMask = 512u;
@@ -100,6 +101,15 @@ __device__ __forceinline__ void mask_block(uint32_t (&w)[8], uint32_t allowed) {
     if (!(allowed >> k & 1u)) w[k] = 0xff800000u;
 }
 
+// The larger value; kNan: NaN if either is, else the other one.
+template <bool kNan>
+__device__ __forceinline__ float max_of(float a, float b) {
+  if constexpr (!kNan) return fmaxf(a, b);
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
 // The i-th pair of logits of a thread's blocks, and the largest of all.
 template <int N>
 __device__ __forceinline__ float2 pair_of(const uint32_t (&w)[N][4], int i) {
@@ -111,19 +121,21 @@ __device__ __forceinline__ float2 pair_of(const uint32_t (&w)[N][8], int i) {
   return make_float2(__uint_as_float(w[i >> 2][2 * (i & 3)]),
                      __uint_as_float(w[i >> 2][2 * (i & 3) + 1]));
 }
-template <int N>
+template <bool kNan, int N>
 __device__ __forceinline__ float largest(const uint32_t (&w)[N][4]) {
   __nv_bfloat162 hm = *reinterpret_cast<const __nv_bfloat162*>(&w[0][0]);
 #pragma unroll
-  for (int i = 1; i < 4 * N; ++i)
-    hm = __hmax2(hm, *reinterpret_cast<const __nv_bfloat162*>(&w[i >> 2][i & 3]));
-  return fmaxf(__low2float(hm), __high2float(hm));
+  for (int i = 1; i < 4 * N; ++i) {
+    const __nv_bfloat162 h = *reinterpret_cast<const __nv_bfloat162*>(&w[i >> 2][i & 3]);
+    hm = kNan ? __hmax2_nan(hm, h) : __hmax2(hm, h);
+  }
+  return max_of<kNan>(__low2float(hm), __high2float(hm));
 }
-template <int N>
+template <bool kNan, int N>
 __device__ __forceinline__ float largest(const uint32_t (&w)[N][8]) {
   float m = __uint_as_float(w[0][0]);
 #pragma unroll
-  for (int i = 1; i < 8 * N; ++i) m = fmaxf(m, __uint_as_float(w[i >> 3][i & 7]));
+  for (int i = 1; i < 8 * N; ++i) m = max_of<kNan>(m, __uint_as_float(w[i >> 3][i & 7]));
   return m;
 }
 
@@ -132,34 +144,65 @@ __device__ __forceinline__ float rescale(const Bf16Logits&, float v, float m, fl
 __device__ __forceinline__ float rescale(const F32Logits&, float v, float m, float2 ch,
                                          float2 cl);
 
-// Adds blocks to a thread's running (max, sum of 2^((v - max) c)).  bf16: d = v - max is
-// exact, and the exponent d c_lo + d c_hi is rounded once, which leaves each weight within
-// 2^-24 |d c| ln 2 of the exact one, to either side: of a sum, whose weights lie at 2^0 to
-// 2^-17 of the largest for the most part, below 7e-7 at the very worst and 1e-7 as it
-// goes.  (exp2_corrected's three more operations a pair: 1057 us for 1016 with three CTAs
-// an SM, at 128 x 61 x 128256.)
+// What the product m ch leaves beside its rounding to fp32.
+__device__ __forceinline__ float beside(float m, float ch) {
+  return fmaf(m, ch, -__fmul_rn(m, ch));
+}
+// A thread's running sum, between the form in which it is kept where |m| < far (below) and
+// the sum of 2^((v - m) c).
+__device__ __forceinline__ float kept(float s, float m, float ch, float far) {
+  return fabsf(m) < far ? s * ex2(beside(m, ch)) : s;
+}
+__device__ __forceinline__ float settled(float s, float m, float ch, float far) {
+  return fabsf(m) < far ? s * ex2(-beside(m, ch)) : s;
+}
+
+// Adds blocks to a thread's running (max, sum).  Kept is the sum of 2^(v ch - round(max ch)),
+// one multiply-add and one exponential a logit; what the rounding left of max ch is put
+// right once at the end.  A weight is then off by the rounding of its exponent and by (v -
+// max) cl, together within 1.5 2^-24 |(v - max) c| ln 2: of a sum, whose weights lie at 2^0
+// to 2^-17 of the largest for the most part, below 1.1e-6 at the very worst and 1e-7 as it
+// goes.  Blocks with a NaN (which weighs nothing) or with a maximum too far out for the
+// product (|max| >= far = 2^20 / ch) are summed from exact differences instead.  (The exact
+// differences and a maximum with 0 for every logit: 742 us for 727 at 128 x 61 x 128256 in
+// bf16.)
 template <typename L, int N, int W>
 __device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch, float2 cl,
-                                           float& m_run, float& s_run) {
-  const float m = largest(w);
-  if (m > m_run) {
-    if (m_run != TV_NEG_INF) s_run *= rescale(L(), m_run, m, ch, cl);
-    m_run = m;
-  }
-  if (!(m > TV_NEG_INF)) return;         // (all masked)
+                                           float far, float& m_run, float& s_run) {
+  const float m = largest<true>(w);
+  if (m == TV_NEG_INF) return;           // (all masked)
   float2 acc[4];
+  if (fabsf(m) < far && (fabsf(m_run) < far || m_run == TV_NEG_INF)) {
+    if (m > m_run) {
+      if (m_run != TV_NEG_INF) s_run *= ex2(__fmul_rn(m_run, ch.x) - __fmul_rn(m, ch.x));
+      m_run = m;
+    }
+    const float mc = __fmul_rn(m_run, ch.x);
 #pragma unroll
-  for (int i = 0; i < 4 * N; ++i) {
-    float2 e;
-    if constexpr (W == 4) {
+    for (int i = 0; i < 4 * N; ++i) {
+      const float2 x = __ffma2_rn(pair_of(w, i), ch, make_float2(-mc, -mc));
+      const float2 e = make_float2(ex2(x.x), ex2(x.y));
+      acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
+    }
+  } else {
+    const float finite = largest<false>(w);
+    s_run = settled(s_run, m_run, ch.x, far);
+    if (finite > m_run) {
+      if (m_run != TV_NEG_INF) s_run *= rescale(L(), m_run, finite, ch, cl);
+      m_run = finite;
+    }
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) {
       const float2 d = __fadd2_rn(pair_of(w, i), make_float2(-m_run, -m_run));
       const float2 x = __ffma2_rn(d, ch, __fmul2_rn(d, cl));
       // (-inf and NaN weigh nothing, at any temperature)
-      e = make_float2(fmaxf(ex2(x.x), 0.f), fmaxf(ex2(x.y), 0.f));
-    } else {
-      e = F32Logits::exp_rel_x2(pair_of(w, i), m_run, ch, cl);
+      const float2 e = make_float2(fmaxf(ex2(x.x), 0.f), fmaxf(ex2(x.y), 0.f));
+      acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
     }
-    acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
+    s_run = kept(s_run, m_run, ch.x, far);
+    const float k = kept(1.f, m_run, ch.x, far);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = __fmul2_rn(acc[i], make_float2(k, k));
   }
   const float2 s2 = __fadd2_rn(__fadd2_rn(acc[0], acc[1]), __fadd2_rn(acc[2], acc[3]));
   s_run += s2.x + s2.y;
@@ -197,11 +240,12 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
 }
 
 // One cluster of CTAs per row.  What bounds it: the logits' bytes, read and written once,
-// with the loads of the next step on their way while this one is worked on, and about as
-// much issue: two exponentials, their sums, the bits and the conversions of each pair.  At
-// 128 x 61 x 128256 in bf16, 745 us, 5.4 TB/s (the copy's rate would be 600 us); at 32 x 26 x
-// 32003 in fp32, 74 us, 3.0 TB/s (rows that start at any element); one row of 128256 takes
-// about 8 us on a cluster of 8 CTAs, most of it the launch, the look-ups and the join.
+// with the loads of the next step on their way while this one is worked on, and the marked
+// tokens, whose counts and biases are gathered in 32-byte sectors and put through shared
+// memory.  At 128 x 61 x 128256 in bf16, 1 in 100 tokens marked, 725 us, 5.6 TB/s (642 us with
+// none marked; 600 at the copy's rate); at 32 x 26 x 32003 in fp32, rows that start at any
+// element and 1 in 7 tokens marked, 68 us, 3.3 TB/s (48 with none, 33); one row of 128256
+// takes about 8 us on a cluster of 8 CTAs, most of it the launch, the look-ups and the join.
 //
 // A row is taken in blocks of 8 logits at 8-element
 // boundaries of the whole array (16-byte loads wherever the row starts; the first and last
@@ -209,7 +253,7 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
 // of a row is its token p - off.  Shared memory holds two bytes for each block: a bit for
 // each token that the grammar and the row's ends leave, and for each of those that has a
 // count, a bias or a place on the path; only their counts and biases are gathered.
-// Tried and slower at 128 x 61 x 128256: bits of 131072 tokens at a time (833 us for 752),
+// Tried and slower at 128 x 61 x 128256: bits of 131072 tokens at a time (833 us for then 752),
 // the row's marked tokens listed beforehand (1152), loads by a warp of their own through
 // shared memory with persistent CTAs (1502).
 template <typename L, int kThreads>
@@ -219,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   constexpr int NB = Block<L>::kBlocks, W = Block<L>::kWords;
   extern __shared__ __align__(16) uint32_t dyn[];
   __shared__ int n_path_s;
-  __shared__ uint32_t path_bits_s;
+  __shared__ uint32_t path_bits[kPathBits / 32];     // (the path's tokens, modulo kPathBits)
   __shared__ float red[2][kThreads / 32];
   __shared__ float2 joined[kMaxCluster];
   const int R = a.N + 1, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -314,18 +358,18 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     }
   };
   look_up(0);
+  if (tid < kPathBits / 32) path_bits[tid] = 0u;
   __syncthreads();
   if (node > 0) {
     if (tid == 0) {
       int n = 0;
-      uint32_t residues = 0;
       for (int k = node; k > 0;) {
         const int p = par[k], t = tok[k];
         if (t < 0 || t >= a.V) {
           found |= kBadToken;
         } else {
           path[n++] = t;
-          residues |= 1u << (t & 31);
+          path_bits[t % kPathBits >> 5] |= 1u << (t & 31);
         }
         if (p < 0 || p >= k) {
           found |= kBadTree;
@@ -334,21 +378,21 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
         k = p;
       }
       n_path_s = n;
-      path_bits_s = residues;            // (which residues the path's tokens have)
     }
     __syncthreads();
   }
   const int n_path = node > 0 ? n_path_s : 0;
-  const uint32_t path_bits = node > 0 ? path_bits_s : 0u;
-  // how often a token is on the path
+  // how often a token is on the path (few pass the first test that are not: with 32 bits
+  // for it in place of 4096, some lane of nearly every warp did)
   auto times = [&](int x) {
     uint32_t n = 0;
-    if (path_bits >> (x & 31) & 1u)
+    if (path_bits[x % kPathBits >> 5] >> (x & 31) & 1u)
       for (int i = 0; i < n_path; ++i) n += path[i] == x;
     return n;
   };
 
   const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
+  const float far = 1048576.f / a.c_hi;
   float m_run = TV_NEG_INF, s_run = 0.f;
   for (int seg = 0; seg < blocks; seg += kSegment / 8) {
     if (seg > 0) {
@@ -479,9 +523,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
                  &w[j][k]);
         }
       }
-      add_blocks<L>(w, ch, cl, m_run, s_run);
+      add_blocks<L>(w, ch, cl, far, m_run, s_run);
     }
   }
+  s_run = settled(s_run, m_run, ch.x, far);
   // the blocks at the row's ends, an element a thread (one block, where the row starts and
   // ends in the same)
   if ((lo && tid < 8) || (p_hi == positions && p_lo < p_hi && hi >= lo && tid >= 8 && tid < 16)) {
@@ -658,16 +703,17 @@ cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
 int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
                       cudaStream_t stream) {
   // CTAs per row: those whose rounds (four CTAs an SM) take the least time, counted in steps
-  // of a CTA with one and a half more for its start and end.  At V = 128256: 8 for one row
-  // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves), 1 for 7808 (where 2
-  // took 889 us for 846).
+  // of a CTA with two and a half more for its start and end.  At V = 128256: 8 for one row
+  // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves: 194 us
+  // for 196), 1 for 7808 (where 2 took 889 us for 846); at 832 rows of 32003 in bf16 1 (53 us,
+  // 56 with 2), in fp32 2 (68, 69 with 1, 79 with 4).
   const long long rows = (long long)a.B * (a.N + 1), ctas = 4ll * sm_count;
   const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2);
   const long long steps = ((long long)a.V + step - 1) / step;
   int C = 1;
   double least = 0;
   for (int c = 1; c <= tvk::logits::kMaxCluster; c *= 2) {
-    const double cost = (double)((rows * c + ctas - 1) / ctas) * ((steps + c - 1) / c + 1.5);
+    const double cost = (double)((rows * c + ctas - 1) / ctas) * ((steps + c - 1) / c + 2.5);
     if (c == 1 || cost < least) {
       least = cost;
       C = c;
