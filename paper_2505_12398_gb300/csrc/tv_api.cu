@@ -226,6 +226,15 @@ void split_scale(float temperature, float* c_hi, float* c_lo) {
   *c_lo = static_cast<float>(c - static_cast<double>(*c_hi));
 }
 
+// The same with c_lo > 0 (c_hi below the value): -inf times either is then -inf.
+void split_scale_below(float temperature, float* c_hi, float* c_lo) {
+  split_scale(temperature, c_hi, c_lo);
+  if (*c_lo > 0.f) return;
+  const double c = 1.4426950408889634 / static_cast<double>(temperature);
+  *c_hi = std::nextafter(*c_hi, 0.f);
+  *c_lo = static_cast<float>(c - static_cast<double>(*c_hi));
+}
+
 // Per-row scratch of `entries` partial normalisers, allocated on first use.
 bool scratch(float2** p, size_t entries) {
   if (*p) return true;
@@ -836,7 +845,7 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
   a.logits = logits;
   a.out = out_logits;
   a.row_stats = reinterpret_cast<float2*>(out_row_stats);
-  split_scale(temperature, &a.c_hi, &a.c_lo);
+  split_scale_below(temperature, &a.c_hi, &a.c_lo);
   a.status = h->status;
   const int rc = tv_launch_process(a, h->dtype == TV_BF16, h->dev.sm_count,
                                    static_cast<cudaStream_t>(cuda_stream));

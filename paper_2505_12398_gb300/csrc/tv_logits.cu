@@ -144,28 +144,28 @@ __device__ __forceinline__ float rescale(const Bf16Logits&, float v, float m, fl
 __device__ __forceinline__ float rescale(const F32Logits&, float v, float m, float2 ch,
                                          float2 cl);
 
-// What the product m ch leaves beside its rounding to fp32.
-__device__ __forceinline__ float beside(float m, float ch) {
-  return fmaf(m, ch, -__fmul_rn(m, ch));
+// What m c = m (ch + cl) leaves beside the rounding of m ch to fp32.
+__device__ __forceinline__ float beside(float m, float ch, float cl) {
+  return fmaf(m, ch, -__fmul_rn(m, ch)) + m * cl;
 }
 // A thread's running sum, between the form in which it is kept where |m| < far (below) and
 // the sum of 2^((v - m) c).
-__device__ __forceinline__ float kept(float s, float m, float ch, float far) {
-  return fabsf(m) < far ? s * ex2(beside(m, ch)) : s;
+__device__ __forceinline__ float kept(float s, float m, float ch, float cl, float far) {
+  return fabsf(m) < far ? s * ex2(beside(m, ch, cl)) : s;
 }
-__device__ __forceinline__ float settled(float s, float m, float ch, float far) {
-  return fabsf(m) < far ? s * ex2(-beside(m, ch)) : s;
+__device__ __forceinline__ float settled(float s, float m, float ch, float cl, float far) {
+  return fabsf(m) < far ? s * ex2(-beside(m, ch, cl)) : s;
 }
 
-// Adds blocks to a thread's running (max, sum).  Kept is the sum of 2^(v ch - round(max ch)),
-// one multiply-add and one exponential a logit; what the rounding left of max ch is put
-// right once at the end.  A weight is then off by the rounding of its exponent and by (v -
-// max) cl, together within 1.5 2^-24 |(v - max) c| ln 2: of a sum, whose weights lie at 2^0
-// to 2^-17 of the largest for the most part, below 1.1e-6 at the very worst and 1e-7 as it
-// goes.  Blocks with a NaN (which weighs nothing) or with a maximum too far out for the
-// product (|max| >= far = 2^20 / ch) are summed from exact differences instead.  (The exact
-// differences and a maximum with 0 for every logit: 742 us for 727 at 128 x 61 x 128256 in
-// bf16.)
+// Adds blocks to a thread's running (max, sum).  Kept is the sum of 2^(v c - round(max ch)):
+// two multiply-adds and one exponential a logit; what the rounding left of max c is put
+// right once at the end.  A weight is then off by the two roundings of its exponent, within
+// 2^-23 |(v - max) c| ln 2 to either side: of a sum, whose weights lie at 2^0 to 2^-17 of the
+// largest for the most part, below 1.4e-6 at the very worst and 1e-7 as it goes.  (Without
+// the product with cl all weights would be off to the same side.)  Blocks with a NaN (which
+// weighs nothing) or with a maximum too far out for the product (|max| >= far = 2^20 / ch)
+// are summed from exact differences instead; those, and a maximum with 0 for every logit,
+// took 742 us for 734 at 128 x 61 x 128256 in bf16.
 template <typename L, int N, int W>
 __device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch, float2 cl,
                                            float far, float& m_run, float& s_run) {
@@ -180,13 +180,14 @@ __device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch,
     const float mc = __fmul_rn(m_run, ch.x);
 #pragma unroll
     for (int i = 0; i < 4 * N; ++i) {
-      const float2 x = __ffma2_rn(pair_of(w, i), ch, make_float2(-mc, -mc));
+      const float2 v = pair_of(w, i);      // (-inf: cl > 0, so that no infinities cancel)
+      const float2 x = __ffma2_rn(v, cl, __ffma2_rn(v, ch, make_float2(-mc, -mc)));
       const float2 e = make_float2(ex2(x.x), ex2(x.y));
       acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
     }
   } else {
     const float finite = largest<false>(w);
-    s_run = settled(s_run, m_run, ch.x, far);
+    s_run = settled(s_run, m_run, ch.x, cl.x, far);
     if (finite > m_run) {
       if (m_run != TV_NEG_INF) s_run *= rescale(L(), m_run, finite, ch, cl);
       m_run = finite;
@@ -199,8 +200,8 @@ __device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch,
       const float2 e = make_float2(fmaxf(ex2(x.x), 0.f), fmaxf(ex2(x.y), 0.f));
       acc[i & 3] = i < 4 ? e : __fadd2_rn(acc[i & 3], e);
     }
-    s_run = kept(s_run, m_run, ch.x, far);
-    const float k = kept(1.f, m_run, ch.x, far);
+    s_run = kept(s_run, m_run, ch.x, cl.x, far);
+    const float k = kept(1.f, m_run, ch.x, cl.x, far);
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] = __fmul2_rn(acc[i], make_float2(k, k));
   }
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       add_blocks<L>(w, ch, cl, far, m_run, s_run);
     }
   }
-  s_run = settled(s_run, m_run, ch.x, far);
+  s_run = settled(s_run, m_run, ch.x, cl.x, far);
   // the blocks at the row's ends, an element a thread (one block, where the row starts and
   // ends in the same)
   if ((lo && tid < 8) || (p_hi == positions && p_lo < p_hi && hi >= lo && tid >= 8 && tid < 16)) {
