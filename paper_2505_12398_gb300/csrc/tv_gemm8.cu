@@ -72,8 +72,8 @@ struct Scales {
   float row[kBM];
   float chunk[kBN / 32];
 };
-// Where SM pairs store through shared memory: buffers of 32 columns of a warp's 32 rows,
-// at the end of the ring's bytes.
+// Where logits are stored through shared memory (by SM pairs, and where rows are not whole
+// 16-byte pieces): buffers of 32 columns of a warp's 32 rows, at the end of the ring's bytes.
 constexpr int kOutBufs = 2;
 constexpr uint32_t kOutBytes = 32 * 32 * 2;
 constexpr size_t kOutTotal = (size_t)kEpiWarps * kOutBufs * kOutBytes;
@@ -281,8 +281,9 @@ struct Shape {
   }
 };
 
-// The widest stores that every row's 32-column chunks allow.
-enum { kStore2 = 0, kStore16 = 1, kStore32 = 2, kStoreTma = 3 };
+// The widest stores that every row's 32-column chunks allow (kStore4: 4 bytes, with 2 at the
+// ends of odd rows).
+enum { kStore4 = 0, kStore16 = 1, kStore32 = 2, kStoreTma = 3 };
 
 // Stores 32 columns of the warp's 32 rows from `buf`, this lane's row into it first, in
 // the order that the 64-byte swizzle has (16-byte pieces exchanged by the row's bits 1
@@ -332,27 +333,60 @@ __device__ __forceinline__ void in_order(uint32_t (&p)[16], float& m, float& s) 
                  "+r"(p[12]), "+r"(p[13]), "+r"(p[14]), "+r"(p[15]), "+f"(m), "+f"(s));
 }
 
-// Stores the first n of 32 columns.
+// Stores the first n of 32 columns (a multiple of 8).
 __device__ __forceinline__ void store_row(const uint32_t (&packed)[16], __nv_bfloat16* dst, int n,
                                           int mode) {
   if (mode == kStore32 && n >= 32) {
     st_global_32b(dst, packed);
     st_global_32b(dst + 16, packed + 8);
-  } else if (mode != kStore2) {          // (n is a multiple of 8)
+  } else {
     uint4* d4 = reinterpret_cast<uint4*>(dst);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (8 * i < n)
         d4[i] = make_uint4(packed[4 * i], packed[4 * i + 1], packed[4 * i + 2],
                            packed[4 * i + 3]);
-  } else {
-    uint16_t* d = reinterpret_cast<uint16_t*>(dst);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (2 * i < n) d[2 * i] = (uint16_t)packed[i];
-      if (2 * i + 1 < n) d[2 * i + 1] = (uint16_t)(packed[i] >> 16);
-    }
   }
+}
+
+// Rows of any length: 64 columns of the warp's 32 rows through 4 KB of shared memory, so that
+// a warp stores 128 bytes of one row at a time (2-byte stores of a column by 32 rows: 1162 us
+// at 3904 x 512 x 31997 for 173, 314 at 976 x 1024 x 31997 for 62, 52 at 61 x 4096 x 31997 for
+// 40).  Word j of a row holds
+// its columns 2 j - s and 2 j + 1 - s, s = 1 where the row starts at an odd element, so that
+// whole words are 4-byte aligned; of such a row the first column, and the last of a whole
+// chunk, are stored by the lane that has the row.
+//
+// Puts a chunk's words there; before: the last word of the chunk before it.
+__device__ __forceinline__ void stage_words(const uint32_t (&packed)[16], uint32_t before,
+                                            uint32_t buf, int lane, int second, int s) {
+  const uint32_t at = buf + (uint32_t)lane * 128u, order = s ? 0x5432u : 0x7654u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + 4u * (uint32_t)((16 * second + i) ^ lane)),
+                 "r"(__byte_perm(i > 0 ? packed[i > 0 ? i - 1 : 0] : before, packed[i], order))
+                 : "memory");
+}
+// Stores n columns of `rows` rows from there, of which the first starts at dst; chunks: how
+// many were put there.
+__device__ __forceinline__ void store_words(uint32_t buf, __nv_bfloat16* dst, int rows, int row0,
+                                            int V, int n, int chunks, int lane) {
+  __syncwarp();
+#pragma unroll 4
+  for (int r = 0; r < rows; ++r) {
+    const int s = (row0 + r) & V & 1, e = 2 * lane - s;
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];"
+                 : "=r"(v)
+                 : "r"(buf + 128u * (uint32_t)r + 4u * (uint32_t)(lane ^ r))
+                 : "memory");
+    __nv_bfloat16* const p = dst + (size_t)r * V + e;
+    if (e >= 0 && e + 1 < n)
+      *reinterpret_cast<uint32_t*>(p) = v;
+    else if (e >= 0 && e < (s && n == 32 * chunks ? n - 1 : n))
+      *reinterpret_cast<uint16_t*>(p) = (uint16_t)v;
+  }
+  __syncwarp();
 }
 
 // Adds the first n of 32 stored values to a row's running (max, sum).
@@ -554,6 +588,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       float m_run = TV_NEG_INF, s_run = 0.f;
+      uint32_t before = 0;                        // (kStore4: the last word of the chunk before)
 #pragma unroll
       for (int k = 0; k < kChunks; ++k) {
         const int c = col + 32 * k, col0 = n0 + c;
@@ -566,6 +601,21 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (lane == 0) stores_read<kOutBufs - 1>();
             __syncwarp();
             store_tile(packed, out0 + kOutBytes * (k % kOutBufs), lane, &map_out, col0, row0);
+          }
+        } else if (store == kStore4) {
+          if (row0 < M) {
+            const int odd = row & V & 1;          // (col0 is even)
+            __nv_bfloat16* const dst = logits + (size_t)row * V + col0;
+            uint16_t* const own = reinterpret_cast<uint16_t*>(dst);
+            stage_words(packed, before, out0, lane, k & 1, odd);
+            before = packed[15];
+            if (odd && row < M && !(k & 1)) own[0] = (uint16_t)packed[0];
+            if ((k & 1) || c + 32 >= bn || n < 32 || V - col0 <= 32) {   // no chunk to wait for
+              const int back = 32 * (k & 1);
+              if (odd && row < M && n == 32) own[31] = (uint16_t)(packed[15] >> 16);
+              store_words(out0, logits + (size_t)row0 * V + col0 - back, min(32, M - row0), row0,
+                          V, back + n, 1 + (k & 1), lane);
+            }
           }
         } else if (row < M) {
           store_row(packed, logits + (size_t)row * V + col0, n, store);
@@ -814,7 +864,7 @@ cudaError_t launch(const CUtensorMap& map_h, const CUtensorMap& map_w,
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = kPair ? 1 : 0;
-  const int store = V % 8 ? kStore2
+  const int store = V % 8 ? kStore4
                     : kPair ? kStoreTma
                     : V % 16 == 0 && (reinterpret_cast<uintptr_t>(logits) & 31u) == 0 ? kStore32
                                                                                      : kStore16;
@@ -914,7 +964,8 @@ int tv_launch_lm_head_scaled(const void* hidden, const float* hidden_scales, con
   shape.a_box = std::min(kBM, (M + 7) / 8 * 8);
   shape.bn = width_for(M, V, g);
   shape.stages = (int)std::min<size_t>(
-      kMaxStages, (kRingBytes - (pair ? kOutTotal : 0)) / (shape.a_bytes() + shape.b_bytes(pair)));
+      kMaxStages, (kRingBytes - (pair || V % 8 ? kOutTotal : 0)) /
+                      (shape.a_bytes() + shape.b_bytes(pair)));
   CUtensorMap map_h, map_w, map_w1, map_out;
   const int w1 = pair && shape.bn > kHalf ? (shape.bn - kHalf) / 2 : kHalf;
   if (!make_map(&map_h, hidden, M, K, shape.a_box) ||

@@ -59,6 +59,24 @@ def test_every_tile_width(tv, M, V):
     v.close()
 
 
+@pytest.mark.parametrize("M", [1, 31, 64, 129, 290])
+@pytest.mark.parametrize("V", [1, 7, 33, 63, 97, 130, 991, 1012, 2045, 2046])
+def test_rows_of_any_length(tv, M, V):
+    """Vocabularies that are not whole 16-byte pieces, from one token on: every logit, and
+    nothing written before or past them."""
+    K = 144
+    qa, sa, qw, sw = _operands(M, K, V, 3 * M + V)
+    v = tv.Verifier(V, 0, M, "bf16", path="three")
+    big = torch.full((M * V + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = big[32:32 + M * V].view(M, V)
+    v.lm_head_fp8(qa.to(torch.float8_e4m3fn), sa, qw.to(torch.float8_e4m3fn), sw, out=(out, None))
+    want = _rows_of(qa, sa, qw, sw, slice(None)).float().to(torch.bfloat16)
+    assert torch.equal(out, want)
+    assert bool((big[:32] == 7).all()) and bool((big[32 + M * V:] == 7).all())
+    assert v.status() == 0
+    v.close()
+
+
 def test_head_past_32_bit_offsets(tv):
     """18000 x 128256 logits: 2.3e9 of them; rows at both ends and across the middle."""
     M, K, V = 18000, 64, 128256
