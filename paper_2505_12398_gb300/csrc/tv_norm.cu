@@ -91,15 +91,17 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
-// One CTA per row.  Every element of the row is read before any is written, so
-// out_residual may be x or residual.  kSteps * blockDim.x * 8 >= K.
+// One CTA per row, or one warp (blockDim.x = 32) for each of blockDim.y.  Every element of the
+// row is read before any is written, so out_residual may be x or residual.  kSteps *
+// blockDim.x * 8 >= K.
 template <typename X, typename W, bool kQuant, int kSteps>
 __global__ void __launch_bounds__(kSteps < kMaxSteps ? 512 : 1024)
-    rms_norm_kernel(const X* x, const X* residual, const W* __restrict__ weight, int K, float eps,
-                    X* out_residual, __nv_bfloat16* __restrict__ out_bf16,
+    rms_norm_kernel(const X* x, const X* residual, const W* __restrict__ weight, int M, int K,
+                    float eps, X* out_residual, __nv_bfloat16* __restrict__ out_bf16,
                     uint8_t* __restrict__ out_e4m3, float* __restrict__ out_scales) {
   __shared__ float red[32];
-  const size_t row = blockIdx.x;
+  const size_t row = (size_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (row >= (size_t)M) return;                  // (a whole warp, with no barrier ahead)
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, nw = blockDim.x >> 5;
   float h[kSteps][kVec];
   float sq = 0.f;
@@ -132,9 +134,11 @@ __global__ void __launch_bounds__(kSteps < kMaxSteps ? 512 : 1024)
     }
   }
   sq = warp_sum(sq);
-  if (lane == 0) red[wid] = sq;
-  __syncthreads();
-  sq = warp_sum(lane < nw ? red[lane] : 0.f);      // (the same order in every warp)
+  if (nw > 1) {
+    if (lane == 0) red[wid] = sq;
+    __syncthreads();
+    sq = warp_sum(lane < nw ? red[lane] : 0.f);    // (the same order in every warp)
+  }
   const float inv = 1.f / sqrtf(sq / (float)K + eps);
   const int groups = (K + kGroup - 1) / kGroup;
 #pragma unroll
@@ -234,10 +238,13 @@ int launch_norm(int M, int K, const void* x, const void* residual, const void* w
                                (vecs + steps - 1) / steps > 512))
     steps *= 2;
   const int threads = std::min(1024, ((vecs + steps - 1) / steps + 31) / 32 * 32);
+  // Rows of up to 256 columns, a warp each: eight to a CTA where there are many (65536 x 128:
+  // 35 us with a CTA a row, bound by their launches; 18 with eight).
+  const int together = threads == 32 && M > 2 * sm_count ? 8 : 1;
   auto run = [&](auto kernel) {
-    kernel<<<M, threads, 0, stream>>>(
+    kernel<<<(M + together - 1) / together, dim3(threads, together), 0, stream>>>(
         static_cast<const X*>(x), static_cast<const X*>(residual), static_cast<const W*>(weight),
-        K, eps, static_cast<X*>(out_residual), kQuant ? nullptr : static_cast<__nv_bfloat16*>(out),
+        M, K, eps, static_cast<X*>(out_residual), kQuant ? nullptr : static_cast<__nv_bfloat16*>(out),
         kQuant ? static_cast<uint8_t*>(out) : nullptr, out_scales);
   };
   switch (steps) {

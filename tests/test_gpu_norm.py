@@ -161,3 +161,15 @@ def test_refusals(v):
         v.quantize_weight(torch.zeros(4, 24, dtype=torch.bfloat16, device="cuda"))
     empty = v.rms_norm(torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda"), w)
     assert empty[0].shape == (0, 64)
+
+
+@pytest.mark.parametrize("quantize", [True, False])
+@pytest.mark.parametrize("M,K,dtype,wdtype,residual", [
+    (305, 8, "bf16", "bf16", True), (1000, 128, "fp32", "bf16", True),
+    (999, 256, "bf16", "fp32", False), (1001, 200, "fp32", "fp32", True),
+    (4097, 248, "bf16", "bf16", True), (70001, 16, "bf16", "bf16", False),
+])
+def test_many_narrow_rows(v, M, K, dtype, wdtype, residual, quantize):
+    x, r, w = _inputs(M, K, dtype, wdtype, residual, M + K)
+    got = v.rms_norm(x, w, r, eps=1e-5, quantize=quantize)
+    _check(got, x, r, w, 1e-5, quantize)
