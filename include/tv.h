@@ -426,7 +426,8 @@ int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
  *     l = l - frequency * n - presence                where n > 0
  *     l = l + bias
  *     l = -inf                                        where the row's mask bit is 0
- * in fp32, rounded once to the handle's logit type.  N = 0 is the form for single tokens.
+ * in fp32 (a positive l times 1 / repetition rounded), rounded once to the handle's logit
+ * type.  N = 0 is the form for single tokens.
  *   context        or NULL: only the path's tokens are penalised, no biases.
  *   slots          as above (checked against B when NULL).
  *   parents, draft_tokens  [B][N+1] as tv_verify_batch (a row whose path leaves the tree,

@@ -7,6 +7,10 @@ CPU path, and using the binding without the compiled library raises.
 
     v = Verifier(vocab=32000, max_nodes=60, max_batch=64, logit_dtype="bf16")
     path, tau, bonus = v.verify(parents, tokens, logits, draft_probs, 1.0, uniforms)
+
+A ``Verifier`` also has the steps on either side: drafting, the target's final norm and LM
+head (bf16, or e4m3 with block scales), and penalties, biases and grammar masks on the
+tree's logits, for which a ``TokenContext`` holds what the requests' texts add up to.
 """
 
 from ._binding import (PATH_FLAGS, TV_BF16, TV_FP32, TV_STATUS, LibraryError, TokenContext,

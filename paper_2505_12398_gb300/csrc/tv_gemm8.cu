@@ -21,23 +21,24 @@
 //   warps 1, 3   the products, one warp for each half of the tile's columns
 //   warp 2       the scales, by 4-byte asynchronous copies into a ring of their own
 //   warps 4-11   the sums: two warps for each quarter of the rows, one per half of the
-//                columns; 128 fp32 sums and one row a thread, in registers that the other
+//                columns; 128 fp32 sums of one row in a thread, in registers that the other
 //                warps give up (232 of them for 40)
 // Tensor memory holds four products of 128 columns, two for each half, so that one is
 // made while the one before is summed.  Each is read in pieces of 32 and 16 columns, one
 // on its way while the last is summed, two columns per multiply-add.  At the end of a
-// tile the sums are rounded once to bf16; pairs store them through shared memory and TMA,
-// in the shadow of the next tile's first products.
+// tile the sums are rounded once to bf16 and stored: by pairs through shared memory and
+// TMA, by single SMs from registers (the weight's bytes bound them), and rows that are not
+// whole 16-byte pieces through shared memory, 128 bytes of a row at a time.
 //
 // Every wait is bounded; one that gives up raises the timeout status, and the loops go on
 // to their end.
 //
 // Measured, without row statistics (GB300, inputs from memory):
-//   7808 x 4096 x 128256   2937 us, 2790 TFLOP/s, under the power cap (2541 us, 3230
-//                          TFLOP/s, in bursts; the products alone 1732 us; twice the bf16
-//                          rate of a plain library product would be 2135 us)
-//   3904 x 4096 x  32000    386 us, 2650 TFLOP/s (348 us in bursts)
-//     61 x 4096 x 128256     87 us, 6.2 TB/s: the weight's bytes
+//   7808 x 4096 x 128256   2.94 to 3.0 ms, 2740 to 2790 TFLOP/s, under the power cap (2541
+//                          us, 3230 TFLOP/s, in bursts; the products alone 1732 us; twice
+//                          the bf16 rate of a plain library product would be 2135 us)
+//   3904 x 4096 x  32000    391 us, 2620 TFLOP/s (348 us in bursts)
+//     61 x 4096 x 128256     88 us, 6.1 TB/s: the weight's bytes
 //      1 x 4096 x  32000     27 us, 4.9 TB/s: the same, with the launch and its ends
 // A group takes the sums' warps 630 clocks of which 370 are their loads and multiply-adds
 // in isolation; the tensor cores idle for the rest of 630 less 513.
@@ -352,10 +353,9 @@ __device__ __forceinline__ void store_row(const uint32_t (&packed)[16], __nv_bfl
 // Rows of any length: 64 columns of the warp's 32 rows through 4 KB of shared memory, so that
 // a warp stores 128 bytes of one row at a time (2-byte stores of a column by 32 rows: 1162 us
 // at 3904 x 512 x 31997 for 173, 314 at 976 x 1024 x 31997 for 62, 52 at 61 x 4096 x 31997 for
-// 40).  Word j of a row holds
-// its columns 2 j - s and 2 j + 1 - s, s = 1 where the row starts at an odd element, so that
-// whole words are 4-byte aligned; of such a row the first column, and the last of a whole
-// chunk, are stored by the lane that has the row.
+// 40).  Word j of a row holds its columns 2 j - s and 2 j + 1 - s, s = 1 where the row starts
+// at an odd element, so that whole words are 4-byte aligned; of such a row the first column,
+// and the last of a whole chunk, are stored by the lane that has the row.
 //
 // Puts a chunk's words there; before: the last word of the chunk before it.
 __device__ __forceinline__ void stage_words(const uint32_t (&packed)[16], uint32_t before,

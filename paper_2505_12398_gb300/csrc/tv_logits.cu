@@ -244,7 +244,7 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
 // with the loads of the next step on their way while this one is worked on, and the marked
 // tokens, whose counts and biases are gathered in 32-byte sectors and put through shared
 // memory.  At 128 x 61 x 128256 in bf16, 1 in 100 tokens marked, 725 us, 5.6 TB/s (642 us with
-// none marked; 600 at the copy's rate); at 32 x 26 x 32003 in fp32, rows that start at any
+// none marked; 600 at the copy's rate); at 32 x 27 x 32003 in fp32, rows that start at any
 // element and 1 in 7 tokens marked, 68 us, 3.3 TB/s (48 with none, 33); one row of 128256
 // takes about 8 us on a cluster of 8 CTAs, most of it the launch, the look-ups and the join.
 //
@@ -706,7 +706,7 @@ int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
   // CTAs per row: those whose rounds (four CTAs an SM) take the least time, counted in steps
   // of a CTA with two and a half more for its start and end.  At V = 128256: 8 for one row
   // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves: 194 us
-  // for 196), 1 for 7808 (where 2 took 889 us for 846); at 832 rows of 32003 in bf16 1 (53 us,
+  // for 196), 1 for 7808 (where 2 took 889 us for 846); at 864 rows of 32003 in bf16 1 (53 us,
   // 56 with 2), in fp32 2 (68, 69 with 1, 79 with 4).
   const long long rows = (long long)a.B * (a.N + 1), ctas = 4ll * sm_count;
   const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2);
@@ -720,12 +720,18 @@ int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
       C = c;
     }
   }
-  const bool few = rows * C <= sm_count;
-  const cudaError_t e =
-      logit_is_bf16 ? (few ? launch_process<tvk::Bf16Logits, 512>(a, C, stream)
-                           : launch_process<tvk::Bf16Logits, 256>(a, C, stream))
-                    : (few ? launch_process<tvk::F32Logits, 512>(a, C, stream)
-                           : launch_process<tvk::F32Logits, 256>(a, C, stream));
+  // Threads: 512 where there is an SM for every CTA, 128 (eight CTAs an SM in place of four)
+  // for many rows of one step, whose time is their start and end (30500 rows of 1003 in bf16:
+  // 220 us, 344 with 256 threads; 18300 of 4000 in fp32 214, 238; but 739 for 7808 of 128256
+  // would be 896).
+  const int threads = rows * C <= sm_count ? 512 : C == 1 && steps == 1 ? 128 : 256;
+  auto run = logit_is_bf16 ? (threads == 512   ? launch_process<tvk::Bf16Logits, 512>
+                              : threads == 256 ? launch_process<tvk::Bf16Logits, 256>
+                                               : launch_process<tvk::Bf16Logits, 128>)
+                           : (threads == 512   ? launch_process<tvk::F32Logits, 512>
+                              : threads == 256 ? launch_process<tvk::F32Logits, 256>
+                                               : launch_process<tvk::F32Logits, 128>);
+  const cudaError_t e = run(a, C, stream);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return -5;
