@@ -286,12 +286,10 @@ struct Shape {
 // ends of odd rows).
 enum { kStore4 = 0, kStore16 = 1, kStore32 = 2, kStoreTma = 3 };
 
-// Stores 32 columns of the warp's 32 rows from `buf`, this lane's row into it first, in
-// the order that the 64-byte swizzle has (16-byte pieces exchanged by the row's bits 1
-// and 2, which also spreads the lanes over the banks).  Rows and columns past the end of
-// the logits are not written.
-__device__ __forceinline__ void store_tile(const uint32_t (&packed)[16], uint32_t buf, int lane,
-                                           const CUtensorMap* map, int x, int y) {
+// Puts 32 columns of the warp's 32 rows into `buf`, this lane's row, in the order that the
+// 64-byte swizzle has (16-byte pieces exchanged by the row's bits 1 and 2, which also spreads
+// the lanes over the banks).
+__device__ __forceinline__ void fill_tile(const uint32_t (&packed)[16], uint32_t buf, int lane) {
   const uint32_t at = buf + (uint32_t)lane * 64u, turn = ((uint32_t)lane >> 1) & 3u;
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i)
@@ -299,21 +297,28 @@ __device__ __forceinline__ void store_tile(const uint32_t (&packed)[16], uint32_
                  "r"(packed[4 * i]), "r"(packed[4 * i + 1]), "r"(packed[4 * i + 2]),
                  "r"(packed[4 * i + 3])
                  : "memory");
+}
+// Stores `count` of them, from column x on, from the buffers at `buf`.  Rows and columns past
+// the end of the logits are not written.  (One fence and one wait for two: 80 us at 3904 x
+// 512 x 32000, 90 with one for each; four buffers cost the ring a stage: 79 there, but 209 for
+// 200 at 976 x 2048 x 128256.)
+__device__ __forceinline__ void store_tiles(uint32_t buf, int count, int lane,
+                                            const CUtensorMap* map, int x, int y) {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
   if (lane == 0) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
-            reinterpret_cast<uint64_t>(map)),
-        "r"(x), "r"(y), "r"(buf)
-        : "memory");
+    for (int k = 0; k < count; ++k)
+      asm volatile(
+          "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+              reinterpret_cast<uint64_t>(map)),
+          "r"(x + 32 * k), "r"(y), "r"(buf + kOutBytes * (uint32_t)k)
+          : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
-// Until at most kLeft of the stores this thread queued still read their buffers.
-template <int kLeft>
+// Until the stores this thread queued no longer read their buffers.
 __device__ __forceinline__ void stores_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 // 32 columns of a row, rounded to bf16.
@@ -598,9 +603,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         pack_row(sum[k], packed);
         if (kPair && store == kStoreTma) {
           if (row0 < M) {                         // (the same in the whole warp)
-            if (lane == 0) stores_read<kOutBufs - 1>();
-            __syncwarp();
-            store_tile(packed, out0 + kOutBytes * (k % kOutBufs), lane, &map_out, col0, row0);
+            const int slot = k % kOutBufs;
+            if (slot == 0) {
+              if (lane == 0) stores_read();
+              __syncwarp();
+            }
+            fill_tile(packed, out0 + kOutBytes * slot, lane);
+            if (slot == kOutBufs - 1 || c + 32 >= bn || V - col0 <= 32)   // no chunk to wait for
+              store_tiles(out0, slot + 1, lane, &map_out, col0 - 32 * slot, row0);
           }
         } else if (store == kStore4) {
           if (row0 < M) {
@@ -651,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (kPair && lane == 0) stores_read<0>();     // (the buffers go with the CTA)
+    if (kPair && lane == 0) stores_read();     // (the buffers go with the CTA)
     if (bad) failed = 1;
   } else {
     regs_fewer<kRegsFew>();
