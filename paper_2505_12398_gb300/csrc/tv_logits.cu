@@ -392,6 +392,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     return n;
   };
 
+  // whether a token's count and bias are the context's: those of others may hold anything
+  auto marked = [&](int x) { return marks && (marks[x >> 5] >> (x & 31) & 1u); };
+
   const float2 ch = make_float2(a.c_hi, a.c_hi), cl = make_float2(a.c_lo, a.c_lo);
   const float far = 1048576.f / a.c_hi;
   float m_run = TV_NEG_INF, s_run = 0.f;
@@ -497,7 +500,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
           asked = false;
           mk &= mk - 1;
           E* const e = element(code);
-          put(e, penalised(get(e), count, bias, times(token(b0, code)), r));
+          const int x = token(b0, code);
+          const uint32_t on_path = times(x);
+          if (on_path && !marked(x)) {       // (here for the path alone)
+            count = 0;
+            bias = 0.f;
+          }
+          put(e, penalised(get(e), count, bias, on_path, r));
         }
         __syncwarp();
 #pragma unroll
@@ -536,14 +545,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     if (x >= 0 && x < a.V) {
       uint32_t n = 0;
       float bias = 0.f;
-      const bool marked = marks && (marks[x >> 5] >> (x & 31) & 1u);
-      if (marked) {
+      const bool known = marked(x);
+      if (known) {
         n = r.counts[x];
         bias = r.bias[x];
       }
       const uint32_t on_path = times(x);
       float v = get(in + p);
-      if (marked || on_path) v = penalised(v, n, bias, on_path, r);
+      if (known || on_path) v = penalised(v, n, bias, on_path, r);
       if (grammar && !(grammar[x >> 5] >> (x & 31) & 1u)) v = TV_NEG_INF;
       E e;
       put(&e, v);
