@@ -302,8 +302,9 @@ int tv_draft_children(tv_handle* h, int B, int N, const int32_t* parents,
  * out_stats are optional (NULL) and have the layouts of tv_verify_batch_debug
  * (out_stats[b][4], rows normalised by this call, is then 0).  Runs on the
  * persistent kernel, or the cluster kernel where a handle that picks its path
- * itself takes it: handles created for the other paths, and calls on a
- * capturing stream, return TV_ERR_INVALID_ARG.
+ * itself takes it and for vocabularies that are not a multiple of 8: handles
+ * created with TV_FLAG_CLUSTER or TV_FLAG_UNFUSED, and calls on a capturing
+ * stream, return TV_ERR_INVALID_ARG.
  * Errors: those of tv_verify_batch.
  */
 int tv_verify_batch_stats(tv_handle* h, int B, int N, const int32_t* parents,

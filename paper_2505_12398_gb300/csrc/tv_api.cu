@@ -321,10 +321,12 @@ int verify_impl(tv_handle* h, int B, int N, const int32_t* parents, const int32_
   }
   // the two-kernel path implements Traversal Verification only
   if (path == kPathTwo && a.token_level) return TV_ERR_INVALID_ARG;
-  // given row normalisers: the persistent kernel, or the cluster kernel where
-  // the handle chose it itself (and neither under capture)
-  if (row_stats && (path == kPathTwo || (h->flags & TV_FLAG_CLUSTER) ||
-                    (path == kPathCluster && capturing(st))))
+  // given row normalisers: the persistent kernel, or where the handle chose its path
+  // itself the cluster kernel, which is also the second of the two kernels that other
+  // vocabularies take (and none of them under capture)
+  if (row_stats && ((path == kPathTwo && (h->vocab % 8) == 0) ||
+                    (h->flags & (TV_FLAG_CLUSTER | TV_FLAG_UNFUSED)) ||
+                    (path != kPathPersistent && capturing(st))))
     return TV_ERR_INVALID_ARG;
   const int bf16 = h->dtype == TV_BF16 ? 1 : 0;
   cudaEvent_t* ev = h->timing ? h->ev : nullptr;

@@ -170,6 +170,17 @@ int launch_typed(const TravArgs& a, int logit_is_bf16, const FusedPlan& plan, in
                  cudaStream_t stream, cudaEvent_t* ev) {
   if (ev && cudaEventRecord(ev[0], stream) != cudaSuccess) return -5;
   if (ev && cudaEventRecord(ev[1], stream) != cudaSuccess) return -5;
+  if (a.stats_given) {
+    // The caller's normalisers: the traversal alone, with the exponential that such
+    // normalisers are made with (exp_pass, as for vocabularies that are a multiple of 8),
+    // and in stream order behind whatever wrote them.  Measured (us a call with and without
+    // them; trees of 60 nodes, bf16): V = 32003, 1 tree 50 / 58, 32 trees 91 / 117, 128 trees
+    // 142 / 228; V = 128251, 32 trees 185 / 273.
+    if (ev && cudaEventRecord(ev[2], stream) != cudaSuccess) return -5;
+    if (tv_launch_tree(a, logit_is_bf16, plan, stream, false) != 0) return -5;
+    if (ev && cudaEventRecord(ev[3], stream) != cudaSuccess) return -5;
+    return 0;
+  }
   // Few rows: more threads on each, as long as every thread has a block or more.
   // Measured (us; the call with 256 / 512 / 1024 threads; 60-node trees, half of
   // their rows internal): V = 128251 bf16, 61 rows 48 / 41 / 38; V = 151933 fp32, 244

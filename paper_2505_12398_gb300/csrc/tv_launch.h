@@ -75,7 +75,8 @@ int tv_launch_tree(const TravArgs& a, int logit_is_bf16, const FusedPlan& plan,
 bool tv_tree_fits(int R, int V, size_t smem_per_block);
 
 // Queues the two kernels on `stream` (the traversal with the cluster kernel's
-// `plan`); 0 on success, TV_ERR_CUDA otherwise.  With `events` non-null,
+// `plan`), the second alone where the caller gives the normalisers (a.row_stats, a.stats_given);
+// 0 on success, TV_ERR_CUDA otherwise.  With `events` non-null,
 // events[0..3] are recorded before the first kernel, between the kernels and
 // after the last one.
 int tv_launch_all(const TravArgs& a, int logit_is_bf16, const FusedPlan& plan, int sm_count,
