@@ -365,7 +365,8 @@ int tv_quantize_weight(tv_handle* h, int rows, int K, tv_dtype dtype, const void
  *                   [ceil(V / 128)][ceil(K / 128)] fp32 (tv_quantize_weight).
  *   out_logits      [M][V] bf16, 16-byte aligned.
  *   out_row_stats   [M][2] fp32 (max, sum), 8-byte aligned, of the stored logits at
- *                   `temperature`; NULL for the logits alone (temperature is then unused).
+ *                   `temperature` (from 4.24e-39 on, as tv_process_logits); NULL for the
+ *                   logits alone (temperature is then unused).
  * The handle must have been created for bf16 logits; any V.  The first call with row
  * statistics allocates the handle's scratch for max_batch * (max_nodes + 1) rows.
  * Errors: as tv_lm_head.
@@ -438,7 +439,8 @@ int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
  *   masks          [n_masks][ceil(V / 32)] words, bit x % 32 of word x / 32 set where token
  *                  x is allowed; mask_index [B][N+1] int32 gives a row's mask, -1 for
  *                  none.  Both NULL (n_masks = 0): no masks.
- *   temperature    > 0, the temperature the normalisers are for.
+ *   temperature    > 0, the temperature the normalisers are for; one below 4.24e-39, whose
+ *                  log2(e) / T is no float32, is refused (TV_ERR_TEMPERATURE).
  *   logits         [B][N+1][V] of the handle's type, 16-byte aligned.
  *   out_logits     same shape, 16-byte aligned; may be logits (in place), and must not
  *                  overlap it in any other way.

@@ -217,7 +217,12 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-bool temperature_ok(float t) { return std::isfinite(t) && t > 0.f; }
+// A temperature whose log2(e) / T, the factor of every weight's exponent, is a float32: from
+// 4.24e-39 on.  (An infinite factor times a difference of 0 is no weight of 1.)
+bool temperature_ok(float t) {
+  return std::isfinite(t) && t > 0.f &&
+         std::isfinite(static_cast<float>(1.4426950408889634 / static_cast<double>(t)));
+}
 
 // log2(e) / T as c_hi + c_lo.
 void split_scale(float temperature, float* c_hi, float* c_lo) {
@@ -948,7 +953,7 @@ const char* tv_strerror(int code) {
   switch (code) {
     case TV_OK: return "success";
     case TV_ERR_INVALID_ARG: return "invalid argument (null pointer, bad size or flag, misaligned array)";
-    case TV_ERR_TEMPERATURE: return "temperature must be finite and > 0";
+    case TV_ERR_TEMPERATURE: return "temperature must be finite and > 0 (for normalisers: at least 4.24e-39)";
     case TV_ERR_VOCAB: return "vocabulary size out of range for this device";
     case TV_ERR_CAPACITY: return "batch or node count above the handle's limits";
     case TV_ERR_CUDA: return "CUDA runtime error";
