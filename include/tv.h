@@ -428,14 +428,14 @@ int tv_context_accept(tv_handle* h, const tv_context* context, int B, int N,
  *     l = l - frequency * n - presence                where n > 0
  *     l = l + bias
  *     l = -inf                                        where the row's mask bit is 0
- * in fp32 (a positive l times 1 / repetition rounded), rounded once to the handle's logit
- * type.  N = 0 is the form for single tokens.
+ * in fp32, rounded once to the handle's logit type.  N = 0 is the form for single tokens.
  *   context        or NULL: only the path's tokens are penalised, no biases.
  *   slots          as above (checked against B when NULL).
  *   parents, draft_tokens  [B][N+1] as tv_verify_batch (a row whose path leaves the tree,
  *                  or a token outside the vocabulary, is reported in the status word and
  *                  the path taken without it); siblings may share a token here.
- *   penalties      [B][3] fp32 (repetition > 0, frequency, presence); NULL means 1, 0, 0.
+ *   penalties      [B][3] fp32 (repetition >= 2^-128, frequency, presence); NULL means
+ *                  1, 0, 0.
  *   masks          [n_masks][ceil(V / 32)] words, bit x % 32 of word x / 32 set where token
  *                  x is allowed; mask_index [B][N+1] int32 gives a row's mask, -1 for
  *                  none.  Both NULL (n_masks = 0): no masks.
