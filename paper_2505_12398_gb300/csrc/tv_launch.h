@@ -13,7 +13,7 @@ struct TravArgs {
   const float* uniforms;       // [B][N+2]
   float2* stats;               // [B][N+1] row (max, sum of exp2) of internal rows
   int B, N, V;
-  float c_hi, c_lo;            // log2(e) / temperature, c_lo > 0 = c_hi + c_lo
+  float c_hi, c_lo;            // log2(e) / temperature = c_hi + c_lo
   double c;                    // the same constant in float64
   int32_t* out_path;           // [B][N]
   int32_t* out_accept_len;     // [B]
@@ -221,7 +221,7 @@ struct ProcessArgs {
   const void* logits;          // [B][N+1][V]
   void* out;
   float2* row_stats;           // [B][N+1]
-  float c_hi, c_lo;            // log2(e) / temperature, c_lo > 0
+  float c_hi, c_lo;            // log2(e) / temperature = c_hi + c_lo, c_lo > 0
   uint32_t* status;
 };
 
