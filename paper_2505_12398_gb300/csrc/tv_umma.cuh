@@ -1,6 +1,7 @@
 // tv_umma.cuh -- what the tensor-core kernels share: shared-memory and TMA
-// descriptors, tcgen05 issue, commit and tensor-memory reads, the order of
-// tiles, and the epilogue's rounding and running normaliser.
+// descriptors, tcgen05 commit, allocation and tensor-memory reads, and the
+// order of tiles; and the bf16 head's rounding, store and running normaliser
+// (the 8-bit head, whose rows may have any length, has its own).
 #pragma once
 
 #include <cuda.h>
