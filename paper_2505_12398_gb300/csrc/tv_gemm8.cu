@@ -33,14 +33,21 @@
 // Every wait is bounded; one that gives up raises the timeout status, and the loops go on
 // to their end.
 //
-// Measured, without row statistics (GB300, inputs from memory):
-//   7808 x 4096 x 128256   2.94 to 3.0 ms, 2740 to 2790 TFLOP/s, under the power cap (2541
-//                          us, 3230 TFLOP/s, in bursts; the products alone 1732 us; twice
-//                          the bf16 rate of a plain library product would be 2135 us)
-//   3904 x 4096 x  32000    391 us, 2620 TFLOP/s (348 us in bursts)
-//     61 x 4096 x 128256     88 us, 6.1 TB/s: the weight's bytes
-//      1 x 4096 x  32000     27 us, 4.9 TB/s: the same, with the launch and its ends
-// A group takes the sums' warps 630 clocks of which 370 are their loads and multiply-adds
+// Measured, one call after the other, in brackets a call alone (GB300, inputs from memory;
+// the first is under the power cap; its products alone take 1732 us, and twice the bf16 rate
+// of a plain library product would be 2135 us):
+//                          logits alone                            with row statistics
+//   7808 x 4096 x 128256   2.97 to 3.03 ms, 2710 to 2760 TFLOP/s   3.29 ms (3.06 to 3.15)
+//                          (2.60 ms, 3150 TFLOP/s)
+//   3904 x 4096 x  32000   392 to 396 us, 2590 TFLOP/s (345 us)    428 us (390)
+//   3904 x 2048 x  32000   213 us (190)                            246 us (235)
+//   3904 x 1024 x  32000   124 us (119)                            171 us (173)
+//   3904 x  512 x  32000    80 us (89)                             145 us (161)
+//     61 x 4096 x 128256    88 us, 6.1 TB/s: the weight's bytes     97 us
+//      1 x 4096 x  32000    27 us, 4.9 TB/s: the same, with the     31 us
+//                          launch and its ends
+// The statistics, 35 to 70 us at 3904 rows, are worked out by the summing warps at a tile's
+// end, while the tensor cores wait for them.  A group takes the sums' warps 630 clocks of which 370 are their loads and multiply-adds
 // in isolation; the tensor cores idle for the rest of 630 less 513.
 #include <limits.h>
 
@@ -194,8 +201,11 @@ __device__ __forceinline__ uint32_t test_end() {
 }
 
 // Arrives on the barrier at `bar` (kPair: an address in the leader) for a part of tensor
-// memory that tcgen05.wait::ld has read.  Nothing in memory is published with it, so the
-// arrive needs no release at cluster scope, whose fence took over 1500 clocks a group.
+// memory that has been read.  That the product which overwrites it comes after the reads
+// rests on tcgen05.wait::ld, behind which this thread's reads are complete and their values in
+// registers before the arrive is issued, and not on the arrive: a relaxed one orders
+// nothing by itself.  Nothing in memory is published with it, so it has no release at cluster
+// scope, whose fence took over 1500 clocks a group.
 template <bool kPair>
 __device__ __forceinline__ void arrive_read(uint32_t bar) {
   if constexpr (kPair)
