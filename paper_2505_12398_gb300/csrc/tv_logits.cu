@@ -178,7 +178,7 @@ __device__ __forceinline__ float settled(float s, float m, float ch, float cl, f
 // the product with cl all weights would be off to the same side.)  Blocks with a NaN (which
 // weighs nothing) or with a maximum too far out for the product (|max| >= far = 2^20 / ch)
 // are summed from exact differences instead; those, and a maximum with 0 for every logit,
-// took 742 us for 734 at 128 x 61 x 128256 in bf16.
+// took 8 us more at 128 x 61 x 128256 in bf16.
 template <typename L, int N, int W>
 __device__ __forceinline__ void add_blocks(const uint32_t (&w)[N][W], float2 ch, float2 cl,
                                            float far, float& m_run, float& s_run) {
@@ -256,10 +256,12 @@ __device__ __forceinline__ uint32_t shifted(const uint32_t* row, int words, long
 // One cluster of CTAs per row.  What bounds it: the logits' bytes, read and written once,
 // with the loads of the next step on their way while this one is worked on, and the marked
 // tokens, whose counts and biases are gathered in 32-byte sectors and put through shared
-// memory.  At 128 x 61 x 128256 in bf16, 1 in 100 tokens marked, 725 us, 5.6 TB/s (642 us with
-// none marked; 600 at the copy's rate); at 32 x 27 x 32003 in fp32, rows that start at any
-// element and 1 in 7 tokens marked, 68 us, 3.3 TB/s (48 with none, 33); one row of 128256
-// takes about 8 us on a cluster of 8 CTAs, most of it the launch, the look-ups and the join.
+// memory.  At 128 x 61 x 128256 in bf16, 1 in 100 tokens marked, 737 us, 5.5 TB/s (some 95 us
+// less with none marked; 600 at the copy's rate); at 32 x 27 x 32003 in fp32, rows that start at
+// any element and 1 in 7 tokens marked, 69.5 us, 3.2 TB/s (49 with none, 33); one row of 128256
+// takes 5.8 us in bf16 and 7.6 in fp32, one after the other, on a cluster of 8 CTAs, most of it
+// the launch, the look-ups and the join.  The 64 registers a thread that four CTAs of 256 leave
+// are all used: the fp32 forms and the bf16 form of 128 threads spill 20 to 56 bytes.
 //
 // A row is taken in blocks of 8 logits at 8-element
 // boundaries of the whole array (16-byte loads wherever the row starts; the first and last
@@ -726,10 +728,10 @@ cudaError_t launch_process(const ProcessArgs& a, int C, cudaStream_t stream) {
 int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
                       cudaStream_t stream) {
   // CTAs per row: those whose rounds (four CTAs an SM) take the least time, counted in steps
-  // of a CTA with two and a half more for its start and end.  At V = 128256: 8 for one row
-  // and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves: 194 us
-  // for 196), 1 for 7808 (where 2 took 889 us for 846); at 864 rows of 32003 in bf16 1 (53 us,
-  // 56 with 2), in fp32 2 (68, 69 with 1, 79 with 4).
+  // of a CTA with two and a half more for its start and end.  At V = 128256 in bf16: 8 for one
+  // row and for 61 rows, 2 for 1952 (4 rounds of whole rows, 7 of halves: 194.5 us, 196 with 1,
+  // 214 with 4), 1 for 7808 (744 us, 773 with 2, 851 with 4); at 864 rows of 32003 in bf16 1 (55
+  // us, 58 with 2), in fp32 2 (70, 69 with 1, 82 with 4).
   const long long rows = (long long)a.B * (a.N + 1), ctas = 4ll * sm_count;
   const long long step = 8 * 256 * (logit_is_bf16 ? 4 : 2);
   const long long steps = ((long long)a.V + step - 1) / step;
@@ -744,8 +746,10 @@ int tv_launch_process(const ProcessArgs& a, int logit_is_bf16, int sm_count,
   }
   // Threads: 512 where there is an SM for every CTA, 128 (eight CTAs an SM in place of four)
   // for many rows of one step, whose time is their start and end (30500 rows of 1003 in bf16:
-  // 220 us, 344 with 256 threads; 18300 of 4000 in fp32 214, 238; but 739 for 7808 of 128256
-  // would be 896).
+  // 233 us, 364 with 256 threads; 18300 of 4000 in fp32 219, 241; but 904 for the 744 of 7808 of
+  // 128256, and 795 with 512).  The steps above are those of 256 threads.  One of 512 is twice as
+  // long, so that some CTAs of a row may have none: at one row of 32000 in bf16 two of four, which
+  // costs a wider cluster's launch and join (5.7 us; 4.8 with four CTAs of 256 threads).
   const int threads = rows * C <= sm_count ? 512 : C == 1 && steps == 1 ? 128 : 256;
   auto run = logit_is_bf16 ? (threads == 512   ? launch_process<tvk::Bf16Logits, 512>
                               : threads == 256 ? launch_process<tvk::Bf16Logits, 256>
