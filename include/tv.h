@@ -331,7 +331,7 @@ int tv_verify_batch_stats(tv_handle* h, int B, int N, const int32_t* parents,
  *   eps            finite and > 0.
  *   out_residual   [M][K] h; may be x or residual (in place), or NULL.
  *   out            [M][K], 16-byte aligned: bf16 where out_scales is NULL, else e4m3
- *                  (y / scale to the nearest, ties to even).
+ *                  (y times 1 / scale, in fp32, to the nearest, ties to even).
  *   out_scales     [M][ceil(K / 128)] fp32: max(max |y| of the group, 2^-100) / 448; NULL
  *                  for bf16 output.  A group with an infinity or NaN has such a scale.
  * The handle gives the device only (its sizes do not bound M).  M = 0 is a no-op.

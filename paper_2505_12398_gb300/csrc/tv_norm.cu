@@ -3,10 +3,11 @@
 //
 // Norm of a row:  h = x + r;  y = h w / sqrt(mean(h^2) + eps), with h and the sums in
 // fp32 and the new residual stream h rounded once to the type of x.  y is rounded once
-// to bf16, or, in groups of 128 columns, to e4m3 after a division by the group's scale
-// s = max(max|y|, 2^-100) / 448 (448 is the largest e4m3 value; the floor keeps 1 / s
-// finite for rows of zeros).  Weights take the same rounding with one scale for each
-// 128 x 128 block.
+// to bf16, or, in groups of 128 columns, to e4m3 after a product with 1 / s, where s =
+// max(max|y|, 2^-100) / 448 is the group's scale (448 is the largest e4m3 value; the floor
+// keeps 1 / s finite for rows of zeros).  The inverse is rounded once for the group, so that
+// a quotient next to the middle of two values may become either.  Weights take the same
+// rounding with one scale for each 128 x 128 block.
 //
 // Both are bound by their bytes.  The norm keeps a row in the registers of one CTA (8
 // consecutive columns, 16 bytes of bf16, per thread and step), so x and r are read once;
@@ -15,7 +16,10 @@
 // out): norm of 7808 x 4096, 38.6 us, 5.8 TB/s (floor 33.2); of 61 x 4096, 2.3 us of the
 // GPU; quantiser of 32000 x 2048, 34.9 us, 5.6 TB/s (29.0); of 128256 x 4096, 242 us, 6.5
 // TB/s (232.5).  A ring of TMA copies with persistent CTAs in the norm's place took 40.8 us
-// at 7808 x 4096 and 72 us for 36 at 30000 x 1024.
+// at 7808 x 4096 and 72 us for 36 at 30000 x 1024.  Rows of more than 16384 columns take eight
+// steps of 1024 threads, whose 64 registers do not hold a thread's 64 values (92 to 732 bytes
+// spilled): 4000 x 16384 76.6 us, 4000 x 16392 99.1, 2000 x 32768 92.8, 1000 x 65536 107 (floors
+// 67.7).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
