@@ -47,8 +47,9 @@
 //      1 x 4096 x  32000    27 us, 4.9 TB/s: the same, with the     31 us
 //                          launch and its ends
 // The statistics, 35 to 70 us at 3904 rows, are worked out by the summing warps at a tile's
-// end, while the tensor cores wait for them.  A group takes the sums' warps 630 clocks of which 370 are their loads and multiply-adds
-// in isolation; the tensor cores idle for the rest of 630 less 513.
+// end, while the tensor cores wait for them.  A group takes the sums' warps 630 clocks of which
+// 370 are their loads and multiply-adds in isolation; the tensor cores idle for the rest of 630
+// less 513.
 #include <limits.h>
 
 #include <algorithm>
