@@ -221,10 +221,10 @@ def prepare(case, seed):
     s = _inputs(case, seed)
     if own:      # the library's handle, and the cache around the same arrays
         import paper_2505_12398_gb300 as tv
-        s["v"] = tv.Verifier(1024, s["R"] - 1 if not case["rows"] else 0, case["batch"], "bf16",
-                             path="three")
-        s["cache"] = tv.KVCache(s["v"], 1, s["data"].shape[1], case["kv_heads"], case["dim"],
-                                page_size=case["page"], data=s["data"],
+        s["verifier"] = tv.Verifier(1024, s["R"] - 1 if not case["rows"] else 0, case["batch"],
+                                    "bf16", path="three")
+        s["cache"] = tv.KVCache(s["verifier"], 1, s["data"].shape[1], case["kv_heads"],
+                                case["dim"], page_size=case["page"], data=s["data"],
                                 exponents=s["exponents"])
     return s
 
