@@ -72,7 +72,14 @@ enum {
                                        row without positive finite mass) */
   TV_STATUS_BAD_SLOT = 256u,   /* a context slot outside [0, slots): the row is processed
                                   without a context, the update is dropped */
-  TV_STATUS_BAD_MASK = 512u    /* a mask index outside [-1, n_masks): the row is not masked */
+  TV_STATUS_BAD_MASK = 512u,   /* a mask index outside [-1, n_masks): the row is not masked */
+  TV_STATUS_BAD_PAGE = 1024u,  /* a position outside the request's row of the page table, or a
+                                  page outside the cache: nothing is read or written there */
+  TV_STATUS_BAD_LENGTH = 2048u, /* a negative length or first position (the request is taken
+                                   as empty), or a row count outside [0, R] (clamped) */
+  TV_STATUS_BAD_PATH = 4096u,  /* an accepted path that does not rise inside the tree: the
+                                  request's cache and length stay as they were */
+  TV_STATUS_NAN = 8192u        /* a NaN was given to a 4-bit cache, which holds 0 for it */
 };
 
 /* Flags for tv_create.  At most one path flag may be given; with none the
@@ -456,6 +463,66 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
                       const uint32_t* masks, const int32_t* mask_index, int n_masks,
                       float temperature, const void* logits, void* out_logits,
                       float* out_row_stats, void* cuda_stream);
+
+/*
+ * The target's attention over drafted trees, and the key/value cache that it reads (no
+ * counterpart in the paper, whose method takes the target's logits as given).  The cache
+ * is paged and holds its values in 4 bits: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign)
+ * with one e4m3 scale for each 16 columns of a row, and a power of two for each layer,
+ * head and side (keys or values):
+ *     value = code * scale * 2^exponent
+ * The arrays are the caller's (the struct itself is read on the host during a call).
+ *   layers, pages, kv_heads   each >= 1.
+ *   head_dim    64 or 128.
+ *   page_size   tokens of a page: 16, 32, 64 or 128.
+ *   data        [layers][pages][kv_heads][2][page_size * head_dim * 9 / 16] bytes, 16-byte
+ *               aligned; side 0 holds keys, 1 values.  A block has the codes
+ *               [head_dim / 32][page_size][16], element 2 j of 32 in the low half of byte j,
+ *               and then the scales [head_dim / 32][page_size][2] (never NaN, and 0x7f is
+ *               not to be put there).
+ *   exponents   [layers][2][kv_heads] int32 (device) in [-64, 64] (others are taken as the
+ *               nearest of these), or NULL: all 0.
+ * A request's tokens are found by lengths [B] int32 (tokens that are cached) and table
+ * [B][max_pages] int32 (its pages, in order; entries behind the last are not read).
+ * Requests may share pages that are not written.
+ */
+typedef struct {
+  int32_t layers, pages, kv_heads, head_dim, page_size;
+  void* data;
+  const int32_t* exponents;
+} tv_cache;
+
+/*
+ * tv_cache_write -- quantises R rows of keys and values of a layer into the positions
+ * behind what is cached: row i of request b at position lengths[b] + i (the rows of a tree
+ * in the order of its nodes, the root's first).  Lengths do not change.  For the 16
+ * columns x of a scale, with G = 2^exponent:
+ *     scale = e4m3(min(max |x| / (6 G), 448)),   code = e2m1(x / (scale G))
+ * both to the nearest of the exact quotient, ties to even; magnitudes past 6 scale G (and
+ * infinities) become that, and a NaN becomes 0 (TV_STATUS_NAN).
+ *   k, v       [B][R][kv_heads][head_dim] of type dtype, 16-byte aligned.
+ *   rows       [B] int32 rows of each request (the rest is not read), NULL: R of all.
+ * tv_cache_read -- positions first[b] + i < lengths[b], i < n, of a layer as out_k, out_v
+ * [B][n][kv_heads][head_dim] of type dtype (rounded once; zeros behind the last position).
+ *   first      [B] int32, NULL: from 0.
+ * tv_cache_accept -- after a verification: for every layer the rows of the accepted path
+ * move behind the root's, from position lengths[b] + path[b][j] to lengths[b] + 1 + j, and
+ * out_lengths[b] = lengths[b] + 1 + tau[b].  path [B][N] and tau [B] are
+ * tv_verify_batch's out_accepted_path and out_accept_len; a tree marked invalid (tau -1)
+ * moves nothing and keeps its length.  out_lengths must not overlap lengths.
+ * Only B (tv_cache_accept: and N) is bounded by the handle's sizes.  B = 0 (R = 0, n = 0) is a
+ * no-op.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CAPACITY, TV_ERR_CUDA.
+ */
+int tv_cache_write(tv_handle* h, const tv_cache* cache, int layer, int B, int R, tv_dtype dtype,
+                   const void* k, const void* v, const int32_t* lengths, const int32_t* table,
+                   int max_pages, const int32_t* rows, void* cuda_stream);
+int tv_cache_read(tv_handle* h, const tv_cache* cache, int layer, int B, int n, tv_dtype dtype,
+                  const int32_t* lengths, const int32_t* table, int max_pages,
+                  const int32_t* first, void* out_k, void* out_v, void* cuda_stream);
+int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int32_t* lengths,
+                    const int32_t* table, int max_pages, const int32_t* path,
+                    const int32_t* tau, int32_t* out_lengths, void* cuda_stream);
 
 /*
  * tv_debug_withhold_job -- test hook for the failure path; no counterpart in

@@ -10,11 +10,13 @@ CPU path, and using the binding without the compiled library raises.
 
 A ``Verifier`` also has the steps on either side: drafting, the target's final norm and LM
 head (bf16, or e4m3 with block scales), and penalties, biases and grammar masks on the
-tree's logits, for which a ``TokenContext`` holds what the requests' texts add up to.
+tree's logits, for which a ``TokenContext`` holds what the requests' texts add up to.  A
+``KVCache`` is the target's key/value cache in 4 bits: its rows are quantised as they are
+written, read back, and moved after a verification.
 """
 
-from ._binding import (PATH_FLAGS, TV_BF16, TV_FP32, TV_STATUS, LibraryError, TokenContext,
-                       Verifier, library, library_path, status_names)
+from ._binding import (PATH_FLAGS, TV_BF16, TV_FP32, TV_STATUS, KVCache, LibraryError,
+                       TokenContext, Verifier, library, library_path, status_names)
 
-__all__ = ["Verifier", "TokenContext", "library", "library_path", "LibraryError", "PATH_FLAGS",
+__all__ = ["Verifier", "TokenContext", "KVCache", "library", "library_path", "LibraryError", "PATH_FLAGS",
            "TV_BF16", "TV_FP32", "TV_STATUS", "status_names"]

@@ -23,6 +23,10 @@ TV_STATUS = {
     "DRAFT_EXHAUSTED": 128,
     "BAD_SLOT": 256,
     "BAD_MASK": 512,
+    "BAD_PAGE": 1024,
+    "BAD_LENGTH": 2048,
+    "BAD_PATH": 4096,
+    "NAN": 8192,
 }
 # columns (of a weight: and rows) of an 8-bit operand that share a scale
 GROUP = 128
@@ -53,6 +57,13 @@ class _Context(ctypes.Structure):
     _fields_ = [("slots", ctypes.c_int32), ("counts", _P), ("bias", _P), ("marks", _P)]
 
 
+class _Cache(ctypes.Structure):
+    """tv_cache of include/tv.h."""
+    _fields_ = [("layers", ctypes.c_int32), ("pages", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("data", _P), ("exponents", _P)]
+
+
 _SIGS = {
     "tv_create": (_I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, ctypes.c_uint]),
     "tv_verify_batch": (_I, [_P, _I, _I, _P, _P, _P, _P, _F, _P, _P, _P, _P, _P]),
@@ -70,6 +81,9 @@ _SIGS = {
     "tv_context_add": (_I, [_P, _P, _I, _I, _I, _P, _P, _P, _P]),
     "tv_context_accept": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P]),
     "tv_process_logits": (_I, [_P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _I, _F, _P, _P, _P, _P]),
+    "tv_cache_write": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P]),
+    "tv_cache_read": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _I, _P, _P, _P, _P]),
+    "tv_cache_accept": (_I, [_P, _P, _I, _I, _P, _P, _I, _P, _P, _P, _P]),
     "tv_last_host_copy_bytes": (_I, [_P, _P, _P]),
     "tv_get_status": (_I, [_P, ctypes.POINTER(ctypes.c_uint32)]),
     "tv_debug_withhold_job": (_I, [_P, _I]),
@@ -611,3 +625,112 @@ class TokenContext:
         _check_in(bonus, torch.int32, (B,), self.device, "bonus")
         self._call("tv_context_accept", B, R - 1, self._slots(slots, B), _at(tokens),
                    _at(path), _at(bonus), self.verifier._stream(stream))
+
+
+class KVCache:
+    """A paged key/value cache in 4 bits (tv_cache) and the attention over it: ``data``
+    [layers, pages, kv_heads, 2, page_size * head_dim * 9 / 16] uint8 (keys, then values) and
+    ``exponents`` [layers, 2, kv_heads] int32, zeros where none are given.  A request's
+    tokens are found by ``lengths`` [B] int32 (tokens cached) and ``table`` [B, max_pages]
+    int32 (its pages, in order).  Calls run on the given (default: current) stream."""
+
+    def __init__(self, verifier, layers, pages, kv_heads, head_dim, page_size=64, data=None,
+                 exponents=None):
+        import torch
+        if head_dim not in (64, 128):
+            raise ValueError(f"head_dim: expected 64 or 128, got {head_dim}")
+        if page_size not in (16, 32, 64, 128):
+            raise ValueError(f"page_size: expected 16, 32, 64 or 128, got {page_size}")
+        if min(layers, pages, kv_heads) < 1:
+            raise ValueError("layers, pages and kv_heads: expected at least one of each")
+        self.verifier, self.device = verifier, verifier.device
+        self.layers, self.pages, self.kv_heads = layers, pages, kv_heads
+        self.head_dim, self.page_size = head_dim, page_size
+        shape = (layers, pages, kv_heads, 2, page_size * head_dim * 9 // 16)
+        dev = self.device
+        self.data = torch.zeros(shape, dtype=torch.uint8, device=dev) if data is None else data
+        self.exponents = torch.zeros(layers, 2, kv_heads, dtype=torch.int32, device=dev) \
+            if exponents is None else exponents
+        _check_in(self.data, torch.uint8, shape, dev, "data")
+        _check_in(self.exponents, torch.int32, (layers, 2, kv_heads), dev, "exponents")
+        self.struct = _Cache(layers, pages, kv_heads, head_dim, page_size, self.data.data_ptr(),
+                             self.exponents.data_ptr())
+        self.ref = ctypes.cast(ctypes.pointer(self.struct), _P)
+
+    def _call(self, name, *args):
+        rc = getattr(self.verifier.lib, name)(self.verifier.handle, self.ref, *args)
+        if rc != 0:
+            raise LibraryError(name, rc, self.verifier.lib)
+
+    def _table(self, lengths, table, B):
+        """The number of pages in a row of a page table that is one."""
+        import torch
+        n = table.shape[1] if table.dim() == 2 else -1
+        _check_in(lengths, torch.int32, (B,), self.device, "lengths")
+        _check_in(table, torch.int32, (B, n), self.device, "table")
+        return n
+
+    def _kind(self, dtype):
+        import torch
+        if dtype in ("bf16", torch.bfloat16):
+            return TV_BF16, torch.bfloat16
+        if dtype in ("fp32", torch.float32):
+            return TV_FP32, torch.float32
+        raise ValueError(f"dtype: expected bf16 or fp32, got {dtype}")
+
+    def write(self, layer, k, v, lengths, table, rows=None, stream=None):
+        """Quantises keys and values [B, R, kv_heads, head_dim] (bf16 or fp32) into the
+        positions behind what is cached, row i of request b at lengths[b] + i; ``rows`` [B]
+        int32 gives the rows of each request (default: all R).  Lengths do not change
+        (tv_cache_write)."""
+        import torch
+        B, R = k.shape[:2]
+        code = self.verifier._float_code(k, "k")
+        shape = (B, R, self.kv_heads, self.head_dim)
+        _check_in(k, k.dtype, shape, self.device, "k")
+        _check_in(v, k.dtype, shape, self.device, "v")
+        n = self._table(lengths, table, B)
+        if rows is not None:
+            _check_in(rows, torch.int32, (B,), self.device, "rows")
+        self._call("tv_cache_write", layer, B, R, code, k.data_ptr(), v.data_ptr(),
+                   lengths.data_ptr(), table.data_ptr(), n, _at(rows),
+                   self.verifier._stream(stream))
+
+    def read(self, layer, lengths, table, n, first=None, dtype="bf16", out=None, stream=None):
+        """Keys and values [B, n, kv_heads, head_dim] of positions first[b] + i < lengths[b]
+        (``first`` [B] int32, default 0), zeros behind the last (tv_cache_read).  ``out`` =
+        (k, v) to write into."""
+        import torch
+        B = lengths.shape[0]
+        pages = self._table(lengths, table, B)
+        code, kind = self._kind(dtype)
+        if first is not None:
+            _check_in(first, torch.int32, (B,), self.device, "first")
+        shape = (B, n, self.kv_heads, self.head_dim)
+        k, v = self.verifier._empty(stream, (shape, kind), (shape, kind)) if out is None else out
+        if out is not None:
+            _check_out(k, kind, shape, self.device)
+            _check_out(v, kind, shape, self.device)
+        self._call("tv_cache_read", layer, B, n, code, lengths.data_ptr(), table.data_ptr(),
+                   pages, _at(first), k.data_ptr(), v.data_ptr(),
+                   self.verifier._stream(stream))
+        return k, v
+
+    def accept(self, path, tau, lengths, table, out=None, stream=None):
+        """After a verification with the paths [B, N] and tau [B] that it returned: moves, in
+        every layer, the accepted nodes' rows behind the root's and returns the new lengths
+        lengths + 1 + tau (tv_cache_accept); a tree marked invalid keeps its length.
+        ``out`` [B] int32 to write them into, not ``lengths`` itself."""
+        import torch
+        B, N = path.shape
+        _check_in(path, torch.int32, (B, N), self.device, "path")
+        _check_in(tau, torch.int32, (B,), self.device, "tau")
+        n = self._table(lengths, table, B)
+        if out is None:
+            out, = self.verifier._empty(stream, ((B,), torch.int32))
+        else:
+            _check_out(out, torch.int32, (B,), self.device)
+        self._call("tv_cache_accept", B, N, lengths.data_ptr(), table.data_ptr(), n,
+                   path.data_ptr(), tau.data_ptr(), out.data_ptr(),
+                   self.verifier._stream(stream))
+        return out

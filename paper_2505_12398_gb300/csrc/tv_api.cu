@@ -263,6 +263,35 @@ bool context_args(const tv_context* c, ContextArgs* out) {
   return true;
 }
 
+// A cache's arrays and sizes; false where the struct cannot be one.
+bool cache_args(const tv_cache* c, CacheArgs* out) {
+  if (!c || c->layers < 1 || c->pages < 1 || c->kv_heads < 1 || !c->data ||
+      !aligned16(c->data) || !aligned4(c->exponents))
+    return false;
+  if (c->head_dim != 64 && c->head_dim != 128) return false;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
+    return false;
+  if (c->kv_heads > (1 << 16)) return false;       // (indexes of a row's pieces are an int)
+  out->layers = c->layers;
+  out->pages = c->pages;
+  out->kv_heads = c->kv_heads;
+  out->head_dim = c->head_dim;
+  out->page_size = c->page_size;
+  out->page_shift = __builtin_ctz((unsigned)c->page_size);
+  out->data = static_cast<uint8_t*>(c->data);
+  out->exponents = c->exponents;
+  return true;
+}
+
+// Where the requests' tokens are; false where the arrays cannot say so.
+bool page_table(const int32_t* lengths, const int32_t* table, int max_pages, PageTable* out) {
+  if (!lengths || !table || max_pages < 1) return false;
+  out->lengths = lengths;
+  out->table = table;
+  out->max_pages = max_pages;
+  return true;
+}
+
 int check_call(const tv_handle* h, int B, int N, const void* parents, const void* tokens,
                const void* logits, const void* drafts, float temperature,
                const void* uniforms, const void* out_path, const void* out_len,
@@ -856,6 +885,70 @@ int tv_process_logits(tv_handle* h, const tv_context* context, int B, int N,
   a.status = h->status;
   const int rc = tv_launch_process(a, h->dtype == TV_BF16, h->dev.sm_count,
                                    static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_cache_write(tv_handle* h, const tv_cache* cache, int layer, int B, int R, tv_dtype dtype,
+                   const void* k, const void* v, const int32_t* lengths, const int32_t* table,
+                   int max_pages, const int32_t* rows, void* cuda_stream) {
+  NvtxRange range("tv_cache_write");
+  CacheArgs c;
+  PageTable t;
+  if (!h || !cache_args(cache, &c) || layer < 0 || layer >= c.layers || B < 0 || R < 0)
+    return TV_ERR_INVALID_ARG;
+  if (dtype != TV_BF16 && dtype != TV_FP32) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch) return TV_ERR_CAPACITY;
+  if (B == 0 || R == 0) return TV_OK;
+  if (!page_table(lengths, table, max_pages, &t) || !k || !v || !aligned16(k) || !aligned16(v))
+    return TV_ERR_INVALID_ARG;
+  if (!tv_cache_rows_fit(c, B, R)) return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_cache_write(c, t, layer, B, R, dtype == TV_BF16, k, v, rows,
+                                       h->status, static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_cache_read(tv_handle* h, const tv_cache* cache, int layer, int B, int n, tv_dtype dtype,
+                  const int32_t* lengths, const int32_t* table, int max_pages,
+                  const int32_t* first, void* out_k, void* out_v, void* cuda_stream) {
+  NvtxRange range("tv_cache_read");
+  CacheArgs c;
+  PageTable t;
+  if (!h || !cache_args(cache, &c) || layer < 0 || layer >= c.layers || B < 0 || n < 0)
+    return TV_ERR_INVALID_ARG;
+  if (dtype != TV_BF16 && dtype != TV_FP32) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch) return TV_ERR_CAPACITY;
+  if (B == 0 || n == 0) return TV_OK;
+  if (!page_table(lengths, table, max_pages, &t) || !out_k || !out_v || !aligned16(out_k) ||
+      !aligned16(out_v))
+    return TV_ERR_INVALID_ARG;
+  if (!tv_cache_rows_fit(c, B, n)) return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_cache_read(c, t, layer, B, n, dtype == TV_BF16, first, out_k, out_v,
+                                      h->status, static_cast<cudaStream_t>(cuda_stream));
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
+int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int32_t* lengths,
+                    const int32_t* table, int max_pages, const int32_t* path,
+                    const int32_t* tau, int32_t* out_lengths, void* cuda_stream) {
+  NvtxRange range("tv_cache_accept");
+  CacheArgs c;
+  PageTable t;
+  if (!h || !cache_args(cache, &c) || B < 0 || N < 0) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch || N > h->max_nodes) return TV_ERR_CAPACITY;
+  if (B == 0) return TV_OK;
+  if (!page_table(lengths, table, max_pages, &t) || (N > 0 && !path) || !tau || !out_lengths)
+    return TV_ERR_INVALID_ARG;
+  // (every part of a request's rows reads its length while one writes the new one)
+  if (out_lengths < lengths + B && lengths < out_lengths + B) return TV_ERR_INVALID_ARG;
+  if (!tv_cache_moves_fit(c, B)) return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const int rc = tv_launch_cache_accept(c, t, B, N, path, tau, out_lengths, h->status,
+                                        static_cast<cudaStream_t>(cuda_stream));
   return rc == 0 ? TV_OK : TV_ERR_CUDA;
 }
 

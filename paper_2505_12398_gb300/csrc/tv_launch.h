@@ -1,6 +1,7 @@
 // tv_launch.h -- internal interface between the host API and the kernels.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -236,3 +237,59 @@ int tv_launch_context_add(const ContextArgs& c, int kind, int B, int n, const in
 int tv_launch_context_accept(const ContextArgs& c, int B, int N, const int32_t* slots,
                              const int32_t* tokens, const int32_t* path, const int32_t* bonus,
                              int V, uint32_t* status, cudaStream_t stream);
+
+// ---- a 4-bit key/value cache and the attention over it (tv_cache.cu, tv_attend.cu) ----
+
+// The cache's arrays and sizes (layout in tv_cache.cuh).
+struct CacheArgs {
+  int layers, pages, kv_heads, head_dim, page_size, page_shift;   // page_size = 1 << page_shift
+  uint8_t* data;
+  const int32_t* exponents;    // [layers][2][kv_heads] or nullptr: 0
+};
+
+// Where the requests' tokens are.
+struct PageTable {
+  const int32_t* lengths;      // [B] tokens that are cached
+  const int32_t* table;        // [B][max_pages] pages of a request, in order
+  int max_pages;
+};
+
+// Whether a call on R rows of B requests, or on the paths of B, is one grid.
+bool tv_cache_rows_fit(const CacheArgs& c, int B, int R);
+bool tv_cache_moves_fit(const CacheArgs& c, int B);
+// Quantises R rows of k and v [B][R][kv_heads][head_dim] (of request b the first rows[b],
+// nullptr: all) into positions lengths[b] + i.  0 or -5, as for the ones after it.
+int tv_launch_cache_write(const CacheArgs& c, const PageTable& t, int layer, int B, int R,
+                          int is_bf16, const void* k, const void* v, const int32_t* rows,
+                          uint32_t* status, cudaStream_t stream);
+// Positions first[b] + i < lengths[b] (first nullptr: from 0), i < n, as k and v
+// [B][n][kv_heads][head_dim]; zeros behind the last.
+int tv_launch_cache_read(const CacheArgs& c, const PageTable& t, int layer, int B, int n,
+                         int is_bf16, const int32_t* first, void* k, void* v, uint32_t* status,
+                         cudaStream_t stream);
+// Of every layer, moves the rows of the accepted paths [B][N] behind the root's, and the
+// lengths after it.
+int tv_launch_cache_accept(const CacheArgs& c, const PageTable& t, int B, int N,
+                           const int32_t* path, const int32_t* tau, int32_t* out_lengths,
+                           uint32_t* status, cudaStream_t stream);
+
+struct AttendArgs {
+  CacheArgs c;
+  PageTable t;
+  int layer, B, R, group;      // query heads of a key/value head
+  const __nv_bfloat16* q;      // [B][R][kv_heads * group][head_dim]
+  const int32_t* parents;      // [B][R] or nullptr: row i sees rows 0 .. i
+  const int32_t* rows;         // [B] or nullptr: R
+  float scale_log2e;
+  __nv_bfloat16* out;
+  float* part;                 // scratch of pieces of split items
+  int* counters;               // arrivals at them, zeros between calls
+  uint32_t* status;
+};
+
+// Bytes and counters of the scratch, for any call.
+size_t tv_attend_scratch(int sm_count);
+int tv_attend_counters(int sm_count);
+int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream);
+
+
