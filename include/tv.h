@@ -525,6 +525,32 @@ int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int
                     const int32_t* tau, int32_t* out_lengths, void* cuda_stream);
 
 /*
+ * tv_tree_attention -- the attention of every row of B trees over the cache:
+ *     out_i = sum over j of p_ij v_j,   p_i = softmax over j of scale * (q_i . k_j)
+ * where row i of request b sees what is cached (positions below lengths[b]), its ancestors in
+ * the tree and itself, row n of the tree being at position lengths[b] + n (tv_cache_write puts
+ * it there).  Query head x reads key/value head x / (heads / kv_heads).  Sums and weights'
+ * sums are float32, weights and queries fp16 relative to the row's largest.
+ *   R          rows: max_nodes + 1 at most with parents, else any.  R = 1 is the form for
+ *              single tokens.
+ *   heads      query heads, a multiple of the cache's kv_heads.
+ *   q          [B][R][heads][head_dim] bf16, 16-byte aligned.
+ *   parents    [B][R] int32, as tv_verify_batch's (a row whose path leaves the tree is
+ *              reported in the status word and the path taken as far as it goes), or NULL: row i
+ *              sees rows 0 to i (a piece of a prompt behind what is cached of it).
+ *   rows       [B] int32 rows of each request, NULL: R of all; the rows behind are 0 in out.
+ *   scale      finite.
+ *   out        [B][R][heads][head_dim] bf16, 16-byte aligned; must not overlap q.
+ * Tokens without a page (TV_STATUS_BAD_PAGE) are left out; a row that sees nothing is 0.
+ * The first call allocates the handle's scratch and may not be captured; later ones may.
+ * Errors: TV_ERR_INVALID_ARG, TV_ERR_CAPACITY, TV_ERR_CUDA.
+ */
+int tv_tree_attention(tv_handle* h, const tv_cache* cache, int layer, int B, int R, int heads,
+                      const void* q, const int32_t* lengths, const int32_t* table,
+                      int max_pages, const int32_t* parents, const int32_t* rows, float scale,
+                      void* out, void* cuda_stream);
+
+/*
  * tv_debug_withhold_job -- test hook for the failure path; no counterpart in
  * the paper.  The next call on this handle that runs the persistent kernel
  * writes tree `tree`'s first job into the work queue but never publishes it.

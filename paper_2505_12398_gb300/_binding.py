@@ -84,6 +84,7 @@ _SIGS = {
     "tv_cache_write": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _P, _P, _I, _P, _P]),
     "tv_cache_read": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _I, _P, _P, _P, _P]),
     "tv_cache_accept": (_I, [_P, _P, _I, _I, _P, _P, _I, _P, _P, _P, _P]),
+    "tv_tree_attention": (_I, [_P, _P, _I, _I, _I, _I, _P, _P, _P, _I, _P, _P, _F, _P, _P]),
     "tv_last_host_copy_bytes": (_I, [_P, _P, _P]),
     "tv_get_status": (_I, [_P, ctypes.POINTER(ctypes.c_uint32)]),
     "tv_debug_withhold_job": (_I, [_P, _I]),
@@ -715,6 +716,33 @@ class KVCache:
                    pages, _at(first), k.data_ptr(), v.data_ptr(),
                    self.verifier._stream(stream))
         return k, v
+
+    def attend(self, layer, q, lengths, table, parents=None, rows=None, scale=None, out=None,
+               stream=None):
+        """Attention [B, R, heads, head_dim] bf16 of queries q of that shape over the cache:
+        row i of request b, at position lengths[b] + i, sees what is cached, its ancestors in
+        the tree ``parents`` [B, R] int32 (None: rows 0 to i) and itself; ``rows`` [B] int32
+        gives the rows of each request (the output's others are 0), ``scale`` the factor of the
+        scores (default head_dim ** -0.5).  heads is a multiple of kv_heads, whose query heads
+        lie together (tv_tree_attention)."""
+        import torch
+        B, R, heads = q.shape[:3]
+        shape = (B, R, heads, self.head_dim)
+        _check_in(q, torch.bfloat16, shape, self.device, "q")
+        n = self._table(lengths, table, B)
+        if parents is not None:
+            _check_in(parents, torch.int32, (B, R), self.device, "parents")
+        if rows is not None:
+            _check_in(rows, torch.int32, (B,), self.device, "rows")
+        if out is None:
+            out, = self.verifier._empty(stream, (shape, torch.bfloat16))
+        else:
+            _check_out(out, torch.bfloat16, shape, self.device)
+        self._call("tv_tree_attention", layer, B, R, heads, q.data_ptr(), lengths.data_ptr(),
+                   table.data_ptr(), n, _at(parents), _at(rows),
+                   float(scale) if scale is not None else self.head_dim ** -0.5,
+                   out.data_ptr(), self.verifier._stream(stream))
+        return out
 
     def accept(self, path, tau, lengths, table, out=None, stream=None):
         """After a verification with the paths [B, N] and tau [B] that it returned: moves, in

@@ -38,6 +38,9 @@ struct tv_handle {
   // per-(row, tile) scratch of tv_lm_head (allocated on first use)
   float2* lmh_part = nullptr;
   float2* lmh8_part = nullptr;   // the same of tv_lm_head_scaled
+  // pieces of tv_tree_attention's split items, and the arrivals at them (first use)
+  float* attend_part = nullptr;
+  int* attend_counters = nullptr;
   // staging for tv_verify_batch_host (allocated on first use), and the bytes
   // its last call copied each way
   char* stage = nullptr;
@@ -952,6 +955,62 @@ int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int
   return rc == 0 ? TV_OK : TV_ERR_CUDA;
 }
 
+int tv_tree_attention(tv_handle* h, const tv_cache* cache, int layer, int B, int R, int heads,
+                      const void* q, const int32_t* lengths, const int32_t* table,
+                      int max_pages, const int32_t* parents, const int32_t* rows, float scale,
+                      void* out, void* cuda_stream) {
+  NvtxRange range("tv_tree_attention");
+  AttendArgs a;
+  if (!h || !cache_args(cache, &a.c) || layer < 0 || layer >= a.c.layers || B < 0 || R < 0)
+    return TV_ERR_INVALID_ARG;
+  if (heads < a.c.kv_heads || (heads % a.c.kv_heads) != 0) return TV_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return TV_ERR_INVALID_ARG;
+  if (B > h->max_batch || (parents && R > h->max_nodes + 1)) return TV_ERR_CAPACITY;
+  if (B == 0 || R == 0) return TV_OK;
+  if (!page_table(lengths, table, max_pages, &a.t) || !q || !out || !aligned16(q) ||
+      !aligned16(out))
+    return TV_ERR_INVALID_ARG;
+  a.group = heads / a.c.kv_heads;
+  if ((long long)R * heads > 0x3fffffffll) return TV_ERR_INVALID_ARG;   // (rows are an int)
+  const size_t bytes = (size_t)B * R * heads * a.c.head_dim * 2;
+  if (static_cast<const char*>(q) < static_cast<char*>(out) + bytes &&
+      static_cast<char*>(out) < static_cast<const char*>(q) + bytes)
+    return TV_ERR_INVALID_ARG;
+  DeviceGuard guard(h->device);
+  if (!guard.ok()) return TV_ERR_CUDA;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (!h->attend_counters) {
+    if (capturing(st)) return TV_ERR_INVALID_ARG;
+    const size_t n = (size_t)tv_attend_counters(h->dev.sm_count) * sizeof(int);
+    int* counters = nullptr;
+    if ((!h->attend_part &&
+         cudaMalloc(&h->attend_part, tv_attend_scratch(h->dev.sm_count)) != cudaSuccess) ||
+        cudaMalloc(&counters, n) != cudaSuccess) {
+      cudaGetLastError();
+      return TV_ERR_CUDA;
+    }
+    if (cudaMemsetAsync(counters, 0, n, st) != cudaSuccess) {
+      cudaGetLastError();
+      cudaFree(counters);
+      return TV_ERR_CUDA;
+    }
+    h->attend_counters = counters;
+  }
+  a.layer = layer;
+  a.B = B;
+  a.R = R;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.parents = parents;
+  a.rows = rows;
+  a.scale_log2e = static_cast<float>(1.4426950408889634 * static_cast<double>(scale));
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.part = h->attend_part;
+  a.counters = h->attend_counters;
+  a.status = h->status;
+  const int rc = tv_launch_attend(a, h->dev.sm_count, st);
+  return rc == 0 ? TV_OK : TV_ERR_CUDA;
+}
+
 int tv_debug_withhold_job(tv_handle* h, int tree) {
   if (!h || tree < 0 || tree >= h->max_batch) return TV_ERR_INVALID_ARG;
   h->withhold_tree = tree;
@@ -1036,6 +1095,8 @@ int tv_destroy(tv_handle* h) {
     if (h->stage) cudaFree(h->stage);
     if (h->lmh_part) cudaFree(h->lmh_part);
     if (h->lmh8_part) cudaFree(h->lmh8_part);
+    if (h->attend_part) cudaFree(h->attend_part);
+    if (h->attend_counters) cudaFree(h->attend_counters);
     cudaGetLastError();
   }
   delete h;

@@ -1,0 +1,524 @@
+// tv_attend.cu -- attention over the 4-bit key/value cache for few query rows per key/value
+// head (sm_103a): decoding steps and small trees.
+//
+//   o_i = sum_j p_ij v_j,  p_i = softmax_j(scale q_i . k_j)  over the tokens j that row i sees.
+//
+// Bound by the cache's bytes, and next to that by the instructions that widen the codes, so
+// neither goes through shared memory: a warp takes 16 tokens at a time from global memory
+// into the registers of mma.sync fragments, each lane widening the codes it loaded.
+// (tcgen05 wants its operands in shared memory, 4 bytes of traffic there per value, written and
+// read, for the 9/16 that come from memory.)  With lane = 4 g + t:
+//   S^T [16 tokens x 8 rows]  = K Q^T      A: the lane's 2 tokens, g and g + 8, in the D / 4
+//                                          columns of index t; the order of columns inside
+//                                          a product is free, so these are D / 4 adjacent ones
+//   O^T [16 columns x 8 rows] += V^T P^T   A: the lane's D / 8 columns of index g in its 4
+//                                          tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9; codes of two
+//                                          tokens are paired before they are widened
+// and S^T's accumulators become P^T's operand by two 8 x 8 transposes.  Keys and values are
+// exact in fp16, without the power of two of their head; queries are scaled by a power of
+// two per row, so that their largest magnitude is in [2^14, 2^15), and rounded to fp16, which
+// changes only columns 2^-21 below the row's largest and smaller.  Weights are 2^(t - m + 6) in
+// fp16, rounded by at most 2^-12 of themselves: m is the largest t (log2(e) times the score) so
+// far, or up to 8 below it, which saves most rescaling; they stay below 2^14 and keep all bits
+// down to 2^-20 of the largest.  Sums are float32.
+//
+// Work is cut evenly: a step is 128 tokens (16 for each of 8 warps) of one item, an item is
+// one (request, key/value head, tile of rows), and every CTA takes the same number of
+// consecutive steps, found from the lengths on the device.  An item that spans CTAs is joined by
+// the last of them to finish, in the order of its pieces.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/tv.h"
+#include "tv_attend.cuh"
+#include "tv_cache.cuh"
+#include "tv_device.cuh"
+#include "tv_launch.h"
+
+namespace tvk {
+namespace attend {
+
+
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kUnit = 16;                        // tokens of a warp's step
+constexpr int kStep = kUnit * kWarps;
+constexpr int kMaxNodes = 1024;                  // rows of a tree
+constexpr int kPerSm = 2;
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+      "{%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// A unit's codes and scales as a lane loads them.
+template <int D>
+struct Raw {
+  static constexpr int kK = D / 32;              // words of a token's codes, D / 4 columns
+  static constexpr int kV = D / 64;              // D / 8 columns
+  uint32_t k[2][kK], v[4][kV];
+  uint32_t ks, vs;                               // scales of two tokens of a chunk
+};
+
+template <int D>
+__device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, int page_size, int slot,
+                                          int lane) {
+  const int g = lane >> 2, t = lane & 3;
+  const uint8_t* const values = keys + (size_t)page_size * D * 9 / 16;
+  constexpr int kChunks = D / 32;
+  const int kc = t * kChunks / 4, vc = g * kChunks / 8;      // chunks of the lane's columns
+  const uint8_t* const kp = keys + ((size_t)kc * page_size + slot) * 16 + (t * (D / 8)) % 16;
+  const uint8_t* const vp = values + ((size_t)vc * page_size + slot) * 16 + (g * (D / 16)) % 16;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (D == 128) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(kp + (g + 8 * i) * 16));
+      r.k[i][0] = u.x;
+      r.k[i][1] = u.y;
+      r.k[i][2] = u.z;
+      r.k[i][3] = u.w;
+    } else {
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(kp + (g + 8 * i) * 16));
+      r.k[i][0] = u.x;
+      r.k[i][1] = u.y;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint8_t* const p = vp + (2 * t + (i & 1) + 8 * (i >> 1)) * 16;
+    if constexpr (D == 128) {
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
+      r.v[i][0] = u.x;
+      r.v[i][1] = u.y;
+    } else {
+      r.v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    }
+  }
+  // lane 8 c + j: tokens 2 j and 2 j + 1 of chunk c
+  const size_t at = (size_t)page_size * D / 2 +
+                    ((size_t)((lane >> 3) % kChunks) * page_size + slot) * 2 + (lane & 7) * 4;
+  r.ks = __ldg(reinterpret_cast<const uint32_t*>(keys + at));
+  r.vs = __ldg(reinterpret_cast<const uint32_t*>(values + at));
+}
+
+// Shared memory of a CTA; what follows it: the warps' sums [kWarps][rows][D + 4].
+struct Shared {
+  long long scan[kThreads];
+  long long total;
+  int request;                                   // where the CTA's range begins
+  long long offset;
+  int last;
+  float m[kWarps][32], l[kWarps][32];
+  float fac[kWarps][32], sum[32], top[32];
+  int32_t parents[kMaxNodes];
+  uint32_t seen[32][kMaxNodes / 32];             // tree rows that a tile's rows see
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) {
+  constexpr int kRows = 8 * NT;
+  constexpr int kDT = D / 16;                    // column tiles of O^T
+  constexpr int kKS = D / 16;                    // products of S^T
+  constexpr int kPitch = D + 4;
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
+  float* const sums = reinterpret_cast<float*>(smem + sizeof(Shared));
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int G = a.group, H = a.c.kv_heads;
+
+  // rows behind a request's last are 0
+  zero_rows(a, D);
+
+  // all steps, and the request in which this CTA's begin
+  const int per = (a.B + kThreads - 1) / kThreads;
+  long long mine = 0;
+  for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
+    const Request q = request_of(a, b);
+    mine += q.steps(kStep) * q.tiles(G, kRows) * H;
+  }
+  const long long before = block_scan(sh.scan, mine, &sh.total);
+  const long long total = sh.total;
+  const long long ctas = min((long long)gridDim.x, total);
+  const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
+  const long long end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
+  if (begin >= before && begin < before + mine) {
+    long long left = begin - before;
+    for (int b = tid * per;; ++b) {
+      const Request q = request_of(a, b);
+      const long long n = q.steps(kStep) * q.tiles(G, kRows) * H;
+      if (left < n) {
+        sh.request = b;
+        sh.offset = left;
+        break;
+      }
+      left -= n;
+    }
+  }
+  __syncthreads();
+  if (begin >= end) return;
+
+  int b = sh.request;
+  long long in_request = sh.offset;
+  for (long long cur = begin; cur < end;) {
+    const Request rq = request_of(a, b);
+    const long long steps = rq.steps(kStep);
+    const int tiles = rq.tiles(G, kRows);
+    if (in_request >= steps * tiles * H) {
+      in_request -= steps * tiles * H;
+      ++b;
+      continue;
+    }
+    const int item = (int)(in_request / steps), s0 = (int)(in_request % steps);
+    const int s1 = s0 + (int)min(steps - s0, end - cur);
+    const int head = item / tiles, m0 = item % tiles * kRows;
+    if (rq.overrun && item == 0 && s0 == 0 && tid == 0) atomicOr(a.status, rq.overrun);
+    const bool masked = (long long)s1 * kStep > rq.len;       // some tokens are the tree's
+    if (masked && a.parents) {
+      const int words = (rq.rows + 31) / 32;
+      for (int i = tid; i < rq.rows; i += kThreads) sh.parents[i] = a.parents[(size_t)b * a.R + i];
+      for (int i = tid; i < kRows * words; i += kThreads) sh.seen[i / words][i % words] = 0u;
+      __syncthreads();
+      if (tid < kRows && m0 + tid < rq.rows * G) {
+        if (!walk(sh.parents, (m0 + tid) / G,
+                  [&](int j) { sh.seen[tid][j >> 5] |= 1u << (j & 31); }))
+          atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
+      }
+      __syncthreads();
+    }
+
+    // queries: row 8 n + g, the columns of index t, in the order of a product's pairs
+    uint32_t q[NT][kKS][2];
+    float fac[NT][2];                            // of rows 8 n + 2 t and the next
+    const int ek = exponent_of(a.c, a.layer, 0, head), ev = exponent_of(a.c, a.layer, 1, head);
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int m = m0 + 8 * n + g;
+      const bool in = m < rq.rows * G;
+      const uint4* const src = reinterpret_cast<const uint4*>(
+          a.q + (((size_t)b * a.R + (in ? m / G : 0)) * H * G + (size_t)head * G + m % G) * D +
+          t * (D / 4));
+      uint32_t w[D / 8];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint4 u = in ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+        w[4 * i] = u.x;
+        w[4 * i + 1] = u.y;
+        w[4 * i + 2] = u.z;
+        w[4 * i + 3] = u.w;
+      }
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        top = max_nan(top, max_nan(fabsf(bf16_lo(w[i])), fabsf(bf16_hi(w[i]))));
+      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const QueryScale s(top);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i)
+        q[n][i >> 1][i & 1] = pack_half2(s.apply(bf16_lo(w[i])), s.apply(bf16_hi(w[i])));
+      const float f = s.factor(a.scale_log2e, ek);
+      fac[n][0] = __shfl_sync(0xffffffffu, f, 8 * t);
+      fac[n][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
+    }
+
+    float o[NT][kDT][4], mref[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < kDT; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[n][i][k] = 0.f;
+      mref[n][0] = mref[n][1] = TV_NEG_INF;
+      l[n][0] = l[n][1] = 0.f;
+    }
+
+    auto page_at = [&](int s) -> int {
+      const int pos = s * kStep + warp * kUnit;
+      return s < s1 && pos < rq.tokens ? page_of(a.c, a.t, b, pos) : -1;
+    };
+    auto fetch = [&](Raw<D>& r, int page, int s) {
+      if (page >= 0)
+        load_unit<D>(r, block_of(a.c, a.layer, page, head, 0), a.c.page_size,
+                     (s * kStep + warp * kUnit) & (a.c.page_size - 1), lane);
+    };
+    Raw<D> raw;
+    int page = page_at(s0), page_next = page_at(s0 + 1);
+    fetch(raw, page, s0);
+    for (int s = s0; s < s1; ++s) {
+      const int pos = s * kStep + warp * kUnit;
+      Raw<D> now = raw;
+      const bool there = page >= 0;
+      if (!there && pos < rq.tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+      page = page_next;
+      fetch(raw, page, s + 1);
+      page_next = page_at(s + 2);
+      if (!there) continue;
+
+      // S^T
+      float st[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) st[n][k] = 0.f;
+      {
+        constexpr int kChunks = D / 32;
+        const int from = (t * kChunks / 4) * 8 + (g >> 1);
+        uint32_t sc[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w = __shfl_sync(0xffffffffu, now.ks, from + 4 * i);
+          sc[i] = decode_scales(g & 1 ? w >> 16 : w & 0xffffu);
+        }
+#pragma unroll
+        for (int w = 0; w < Raw<D>::kK; ++w) {             // 8 columns: two products
+          uint32_t h[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            decode8(now.k[i][w], h[i]);
+            const bool upper = D == 128 ? w >= 2 : (t & 1);
+            const uint32_t s2 = upper ? hi_hi(sc[i]) : lo_lo(sc[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) h[i][k] = mul2(h[i][k], s2);
+          }
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const uint32_t af[4] = {h[0][2 * p], h[1][2 * p], h[0][2 * p + 1], h[1][2 * p + 1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              mma16816(st[n], af, q[n][2 * w + p][0], q[n][2 * w + p][1]);
+          }
+        }
+      }
+
+      // weights: st[n][k] is token g (k < 2) or g + 8, row 8 n + 2 t + (k & 1)
+      bool grow = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float x = st[n][k] * fac[n][k & 1];
+          if (pos + kUnit > rq.len) {
+            const int at = pos + g + (k & 2) * 4 - rq.len, row = 8 * n + 2 * t + (k & 1);
+            bool on = at < 0;
+            if (!on && at < rq.rows && at + rq.len < rq.tokens)
+              on = a.parents ? (sh.seen[row][at >> 5] >> (at & 31) & 1u) != 0u
+                             : at <= (m0 + row) / G;
+            x = on ? x : TV_NEG_INF;
+          }
+          st[n][k] = x;
+          grow = grow || x > mref[n][k & 1] + kSlack;
+        }
+      if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float top = fmaxf(st[n][k], st[n][k + 2]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            if (top > mref[n][k]) {
+              const float down = ex2(mref[n][k] - top);    // (0 from -inf)
+              mref[n][k] = top;
+              l[n][k] *= down;
+#pragma unroll
+              for (int i = 0; i < kDT; ++i) {
+                o[n][i][k] *= down;
+                o[n][i][k + 2] *= down;
+              }
+            }
+          }
+      }
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float p[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float m = mref[n][k & 1];
+          p[k] = ex2(st[n][k] - (m == TV_NEG_INF ? 0.f : m) + kLift);
+          l[n][k & 1] += p[k];
+        }
+        pb[n][0] = transpose8(pack_half2(p[0], p[1]));
+        pb[n][1] = transpose8(pack_half2(p[2], p[3]));
+      }
+
+      // O^T
+      {
+        constexpr int kChunks = D / 32;
+        const int from = (g * kChunks / 8) * 8 + t;
+        uint32_t sc[2];                                    // of tokens 2 t, 2 t + 1; 8 further
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t w = __shfl_sync(0xffffffffu, now.vs, from + 4 * i);
+          const bool upper = D == 128 ? (g & 1) : (g & 2);
+          uint32_t two = __byte_perm(w, 0u, upper ? 0x4431u : 0x4420u);
+          // (bytes behind the last token may be anything, a NaN among it)
+          const int left = rq.tokens - (pos + 2 * t + 8 * i);
+          if (left < 2) two = left < 1 ? 0u : two & 0xffu;
+          sc[i] = decode_scales(two);
+        }
+#pragma unroll
+        for (int w = 0; w < Raw<D>::kV; ++w) {             // 8 columns: four tiles
+          uint32_t e[2][4], f[2][4];                       // even and odd columns, token pairs
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t x = now.v[2 * i][w], y = now.v[2 * i + 1][w];
+            decode8((x & 0x0f0f0f0fu) | (y << 4 & 0xf0f0f0f0u), e[i]);
+            decode8((x >> 4 & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u), f[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              e[i][k] = mul2(e[i][k], sc[i]);
+              f[i][k] = mul2(f[i][k], sc[i]);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t af[4] = {e[0][k], f[0][k], e[1][k], f[1][k]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma16816(o[n][4 * w + k], af, pb[n][0], pb[n][1]);
+          }
+        }
+      }
+    }
+
+    // the warps' sums joined.  o[n][i][k]: column (D / 8) g + 2 i + (k >> 1), row
+    // 8 n + 2 t + (k & 1)
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[n][k] += __shfl_xor_sync(0xffffffffu, l[n][k], x);
+        const int row = 8 * n + 2 * t + k;
+        if (g == 0) {
+          sh.m[warp][row] = mref[n][k];
+          sh.l[warp][row] = l[n][k];
+        }
+        float* const dst = sums + ((size_t)warp * kRows + row) * kPitch + g * (D / 8);
+#pragma unroll
+        for (int i = 0; i < kDT; ++i)
+          *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[n][i][k], o[n][i][k + 2]);
+      }
+    __syncthreads();
+    if (tid < kRows) {
+      float top = TV_NEG_INF, sum = 0.f;
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.m[w][tid]);
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = sh.m[w][tid] == TV_NEG_INF ? 0.f : ex2(sh.m[w][tid] - top);
+        // (a row that is not a number has no maximum, and its sums are NaN)
+        sh.fac[w][tid] = sh.l[w][tid] != sh.l[w][tid] ? sh.l[w][tid] : f;
+        sum += sh.l[w][tid] * sh.fac[w][tid];
+      }
+      sh.top[tid] = top;
+      sh.sum[tid] = sum;
+    }
+    __syncthreads();
+    const bool whole = s0 == 0 && s1 == steps;
+    const float up = pow2i(ev);
+    const int slot = 2 * (int)blockIdx.x + (s0 == 0);
+    for (int x = tid; x < kRows * D / 4; x += kThreads) {
+      const int row = x / (D / 4), col = x % (D / 4) * 4;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < kWarps; ++w) {
+        const float4 v =
+            *reinterpret_cast<const float4*>(sums + ((size_t)w * kRows + row) * kPitch + col);
+        const float f = sh.fac[w][row];
+        y.x += f * v.x;
+        y.y += f * v.y;
+        y.z += f * v.z;
+        y.w += f * v.w;
+      }
+      if (whole)
+        store_out(a, b, head, m0 + row, rq.rows * G, col, D, y, sh.sum[row], up);
+      else
+        reinterpret_cast<float4*>(a.part)[(size_t)slot * (kRows * D / 4) + x] = y;
+    }
+    if (!whole) {
+      float2* const stats = reinterpret_cast<float2*>(a.part + (size_t)2 * gridDim.x * kRows * D);
+      if (tid < kRows) stats[(size_t)slot * kRows + tid] = make_float2(sh.top[tid], sh.sum[tid]);
+      // pieces lie in the CTAs from the one with the item's first step to that with its last
+      const long long g0 = cur - s0, g1 = g0 + steps - 1;
+      const int c0 = (int)(((g0 + 1) * ctas - 1) / total), c1 = (int)(((g1 + 1) * ctas - 1) / total);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int seen = atomicAdd(&a.counters[c0], 1);
+        sh.last = seen == c1 - c0;
+        if (sh.last) a.counters[c0] = 0;
+      }
+      __syncthreads();
+      if (sh.last) {
+        __threadfence();
+        for (int x = tid; x < kRows * D / 4; x += kThreads) {
+          const int row = x / (D / 4), col = x % (D / 4) * 4;
+          float top = TV_NEG_INF, sum = 0.f;
+          for (int c = c0; c <= c1; ++c)
+            top = fmaxf(top, __ldcg(&stats[(size_t)(2 * c + (c == c0)) * kRows + row]).x);
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int c = c0; c <= c1; ++c) {
+            const size_t at = 2 * c + (c == c0);
+            const float2 ms = __ldcg(&stats[at * kRows + row]);
+            const float f = ms.y != ms.y ? ms.y : ms.x == TV_NEG_INF ? 0.f : ex2(ms.x - top);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part) +
+                                    at * (kRows * D / 4) + x);
+            sum += f * ms.y;
+            y.x += f * v.x;
+            y.y += f * v.y;
+            y.z += f * v.z;
+            y.w += f * v.w;
+          }
+          store_out(a, b, head, m0 + row, rq.rows * G, col, D, y, sum, up);
+        }
+      }
+    }
+    __syncthreads();
+    cur += s1 - s0;
+    in_request += s1 - s0;
+  }
+}
+
+template <int D, int NT>
+int launch(const AttendArgs& a, int sm_count, cudaStream_t stream) {
+  const size_t smem = sizeof(Shared) + (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
+  if (cudaFuncSetAttribute(attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           (int)smem) != cudaSuccess) {
+    cudaGetLastError();
+    return -5;
+  }
+  attend_kernel<D, NT><<<kPerSm * sm_count, kThreads, smem, stream>>>(a);
+  return cudaGetLastError() == cudaSuccess ? 0 : -5;
+}
+
+}  // namespace attend
+}  // namespace tvk
+
+using namespace tvk::attend;
+
+size_t tv_attend_scratch(int sm_count) {
+  // two pieces of each CTA, of 32 rows of 64 columns or 16 of 128 (and their statistics)
+  return (size_t)kPerSm * sm_count * 2 * (16 * 128 + 2 * 32) * sizeof(float);
+}
+int tv_attend_counters(int sm_count) { return kPerSm * sm_count; }
+
+int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream) {
+  const long long rows = (long long)a.R * a.group;
+  if (a.c.head_dim == 128)
+    return rows <= 8 ? launch<128, 1>(a, sm_count, stream) : launch<128, 2>(a, sm_count, stream);
+  if (rows <= 8) return launch<64, 1>(a, sm_count, stream);
+  return rows <= 16 ? launch<64, 2>(a, sm_count, stream) : launch<64, 4>(a, sm_count, stream);
+}
