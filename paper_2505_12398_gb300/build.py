@@ -23,7 +23,7 @@ LIB = os.path.join(HERE, "libtv.so")
 SOURCES = ["tv_api.cu", "tv_kernels.cu", "tv_tree.cu", "tv_flow.cu", "tv_noalloc.cu", "tv_gemm.cu",
            "tv_bonus.cu",
            "tv_draft.cu", "tv_gemm8.cu", "tv_norm.cu", "tv_logits.cu", "tv_cache.cu",
-           "tv_attend.cu"]
+           "tv_attend.cu", "tv_attend_tile.cu"]
 HEADERS = ["tv_device.cuh", "tv_launch.h", "tv_ptx.cuh", "tv_control.cuh", "tv_umma.cuh",
            "tv_cache.cuh", "tv_attend.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

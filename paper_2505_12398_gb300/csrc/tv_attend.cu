@@ -30,6 +30,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/tv.h"
 #include "tv_attend.cuh"
 #include "tv_cache.cuh"
@@ -44,7 +46,7 @@ namespace attend {
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kUnit = 16;                        // tokens of a warp's step
-constexpr int kStep = kUnit * kWarps;
+static_assert(kStep == kUnit * kWarps, "a step is 16 tokens of each warp");
 constexpr int kMaxNodes = 1024;                  // rows of a tree
 constexpr int kPerSm = 2;
 
@@ -117,17 +119,19 @@ __device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, int pa
 }
 
 // Shared memory of a CTA; what follows it: the warps' sums [kWarps][rows][D + 4].
-struct Shared {
-  long long scan[kThreads];
-  long long total;
-  int request;                                   // where the CTA's range begins
-  long long offset;
-  int last;
+struct alignas(16) Shared {
+  Schedule plan;
+  Shares shares;
+  Walker walker;                                 // (thread 0's)
+  Piece piece;
+  int more, last;
   float m[kWarps][32], l[kWarps][32];
   float fac[kWarps][32], sum[32], top[32];
   int32_t parents[kMaxNodes];
   uint32_t seen[32][kMaxNodes / 32];             // tree rows that a tile's rows see
 };
+
+static_assert(sizeof(Shared) % 16 == 0, "the sums behind it are read 16 bytes at a time");
 
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) {
@@ -144,56 +148,28 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
   // rows behind a request's last are 0
   zero_rows(a, D);
 
-  // all steps, and the request in which this CTA's begin
-  const int per = (a.B + kThreads - 1) / kThreads;
-  long long mine = 0;
-  for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b) {
-    const Request q = request_of(a, b);
-    mine += q.steps(kStep) * q.tiles(G, kRows) * H;
-  }
-  const long long before = block_scan(sh.scan, mine, &sh.total);
-  const long long total = sh.total;
-  const long long ctas = min((long long)gridDim.x, total);
-  const long long begin = blockIdx.x < ctas ? total * blockIdx.x / ctas : 0;
-  const long long end = blockIdx.x < ctas ? total * (blockIdx.x + 1) / ctas : 0;
-  if (begin >= before && begin < before + mine) {
-    long long left = begin - before;
-    for (int b = tid * per;; ++b) {
-      const Request q = request_of(a, b);
-      const long long n = q.steps(kStep) * q.tiles(G, kRows) * H;
-      if (left < n) {
-        sh.request = b;
-        sh.offset = left;
-        break;
-      }
-      left -= n;
+  {
+    Walker w;
+    const Shares shares = plan(a, sh.plan, kRows, blockIdx.x, gridDim.x, w);
+    if (tid == 0) {
+      sh.shares = shares;
+      sh.walker = w;
     }
   }
-  __syncthreads();
-  if (begin >= end) return;
-
-  int b = sh.request;
-  long long in_request = sh.offset;
-  for (long long cur = begin; cur < end;) {
-    const Request rq = request_of(a, b);
-    const long long steps = rq.steps(kStep);
-    const int tiles = rq.tiles(G, kRows);
-    if (in_request >= steps * tiles * H) {
-      in_request -= steps * tiles * H;
-      ++b;
-      continue;
-    }
-    const int item = (int)(in_request / steps), s0 = (int)(in_request % steps);
-    const int s1 = s0 + (int)min(steps - s0, end - cur);
-    const int head = item / tiles, m0 = item % tiles * kRows;
-    if (rq.overrun && item == 0 && s0 == 0 && tid == 0) atomicOr(a.status, rq.overrun);
-    const bool masked = (long long)s1 * kStep > rq.len;       // some tokens are the tree's
+  const Piece& p = sh.piece;
+  for (;;) {
+    if (tid == 0) sh.more = sh.walker.next(a, kRows, sh.piece);
+    __syncthreads();
+    if (!sh.more) break;
+    const int b = p.b, head = p.head, m0 = p.m0, s0 = p.s0, s1 = p.s1;
+    const int len = p.rq.len, nrows = p.rq.rows, tokens = p.tokens;
+    const bool masked = (long long)s1 * kStep > len;       // some tokens are the tree's
     if (masked && a.parents) {
-      const int words = (rq.rows + 31) / 32;
-      for (int i = tid; i < rq.rows; i += kThreads) sh.parents[i] = a.parents[(size_t)b * a.R + i];
+      const int words = (nrows + 31) / 32;
+      for (int i = tid; i < nrows; i += kThreads) sh.parents[i] = a.parents[(size_t)b * a.R + i];
       for (int i = tid; i < kRows * words; i += kThreads) sh.seen[i / words][i % words] = 0u;
       __syncthreads();
-      if (tid < kRows && m0 + tid < rq.rows * G) {
+      if (tid < kRows && m0 + tid < nrows * G) {
         if (!walk(sh.parents, (m0 + tid) / G,
                   [&](int j) { sh.seen[tid][j >> 5] |= 1u << (j & 31); }))
           atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
@@ -208,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int m = m0 + 8 * n + g;
-      const bool in = m < rq.rows * G;
+      const bool in = m < nrows * G;
       const uint4* const src = reinterpret_cast<const uint4*>(
           a.q + (((size_t)b * a.R + (in ? m / G : 0)) * H * G + (size_t)head * G + m % G) * D +
           t * (D / 4));
@@ -249,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
 
     auto page_at = [&](int s) -> int {
       const int pos = s * kStep + warp * kUnit;
-      return s < s1 && pos < rq.tokens ? page_of(a.c, a.t, b, pos) : -1;
+      return s < s1 && pos < tokens ? page_of(a.c, a.t, b, pos) : -1;
     };
     auto fetch = [&](Raw<D>& r, int page, int s) {
       if (page >= 0)
@@ -263,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       const int pos = s * kStep + warp * kUnit;
       Raw<D> now = raw;
       const bool there = page >= 0;
-      if (!there && pos < rq.tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+      if (!there && pos < tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
       page = page_next;
       fetch(raw, page, s + 1);
       page_next = page_at(s + 2);
@@ -296,11 +272,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
             for (int k = 0; k < 4; ++k) h[i][k] = mul2(h[i][k], s2);
           }
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const uint32_t af[4] = {h[0][2 * p], h[1][2 * p], h[0][2 * p + 1], h[1][2 * p + 1]};
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t af[4] = {h[0][2 * k], h[1][2 * k], h[0][2 * k + 1], h[1][2 * k + 1]};
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-              mma16816(st[n], af, q[n][2 * w + p][0], q[n][2 * w + p][1]);
+              mma16816(st[n], af, q[n][2 * w + k][0], q[n][2 * w + k][1]);
           }
         }
       }
@@ -312,10 +288,10 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           float x = st[n][k] * fac[n][k & 1];
-          if (pos + kUnit > rq.len) {
-            const int at = pos + g + (k & 2) * 4 - rq.len, row = 8 * n + 2 * t + (k & 1);
+          if (pos + kUnit > len) {
+            const int at = pos + g + (k & 2) * 4 - len, row = 8 * n + 2 * t + (k & 1);
             bool on = at < 0;
-            if (!on && at < rq.rows && at + rq.len < rq.tokens)
+            if (!on && at < nrows && at + len < tokens)
               on = a.parents ? (sh.seen[row][at >> 5] >> (at & 31) & 1u) != 0u
                              : at <= (m0 + row) / G;
             x = on ? x : TV_NEG_INF;
@@ -346,15 +322,15 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       uint32_t pb[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float p[4];
+        float x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float m = mref[n][k & 1];
-          p[k] = ex2(st[n][k] - (m == TV_NEG_INF ? 0.f : m) + kLift);
-          l[n][k & 1] += p[k];
+          x[k] = ex2(st[n][k] - (m == TV_NEG_INF ? 0.f : m) + kLift);
+          l[n][k & 1] += x[k];
         }
-        pb[n][0] = transpose8(pack_half2(p[0], p[1]));
-        pb[n][1] = transpose8(pack_half2(p[2], p[3]));
+        pb[n][0] = transpose8(pack_half2(x[0], x[1]));
+        pb[n][1] = transpose8(pack_half2(x[2], x[3]));
       }
 
       // O^T
@@ -368,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
           const bool upper = D == 128 ? (g & 1) : (g & 2);
           uint32_t two = __byte_perm(w, 0u, upper ? 0x4431u : 0x4420u);
           // (bytes behind the last token may be anything, a NaN among it)
-          const int left = rq.tokens - (pos + 2 * t + 8 * i);
+          const int left = tokens - (pos + 2 * t + 8 * i);
           if (left < 2) two = left < 1 ? 0u : two & 0xffu;
           sc[i] = decode_scales(two);
         }
@@ -428,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       sh.sum[tid] = sum;
     }
     __syncthreads();
-    const bool whole = s0 == 0 && s1 == steps;
+    const bool whole = p.whole();
     const float up = pow2i(ev);
     const int slot = 2 * (int)blockIdx.x + (s0 == 0);
     for (int x = tid; x < kRows * D / 4; x += kThreads) {
@@ -444,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
         y.w += f * v.w;
       }
       if (whole)
-        store_out(a, b, head, m0 + row, rq.rows * G, col, D, y, sh.sum[row], up);
+        store_out(a, b, head, m0 + row, nrows * G, col, D, y, sh.sum[row], up);
       else
         reinterpret_cast<float4*>(a.part)[(size_t)slot * (kRows * D / 4) + x] = y;
     }
@@ -452,8 +428,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       float2* const stats = reinterpret_cast<float2*>(a.part + (size_t)2 * gridDim.x * kRows * D);
       if (tid < kRows) stats[(size_t)slot * kRows + tid] = make_float2(sh.top[tid], sh.sum[tid]);
       // pieces lie in the CTAs from the one with the item's first step to that with its last
-      const long long g0 = cur - s0, g1 = g0 + steps - 1;
-      const int c0 = (int)(((g0 + 1) * ctas - 1) / total), c1 = (int)(((g1 + 1) * ctas - 1) / total);
+      const int c0 = sh.shares.owner(p.first), c1 = sh.shares.owner(p.first + p.steps - 1);
       __threadfence();
       __syncthreads();
       if (tid == 0) {
@@ -482,13 +457,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
             y.z += f * v.z;
             y.w += f * v.w;
           }
-          store_out(a, b, head, m0 + row, rq.rows * G, col, D, y, sum, up);
+          store_out(a, b, head, m0 + row, nrows * G, col, D, y, sum, up);
         }
       }
     }
     __syncthreads();
-    cur += s1 - s0;
-    in_request += s1 - s0;
   }
 }
 
@@ -511,12 +484,14 @@ using namespace tvk::attend;
 
 size_t tv_attend_scratch(int sm_count) {
   // two pieces of each CTA, of 32 rows of 64 columns or 16 of 128 (and their statistics)
-  return (size_t)kPerSm * sm_count * 2 * (16 * 128 + 2 * 32) * sizeof(float);
+  const size_t few = (size_t)kPerSm * sm_count * 2 * (16 * 128 + 2 * 32) * sizeof(float);
+  return std::max(few, tv_attend_tile_scratch(sm_count));
 }
 int tv_attend_counters(int sm_count) { return kPerSm * sm_count; }
 
 int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const long long rows = (long long)a.R * a.group;
+  if (rows > (a.c.head_dim == 128 ? 16 : 32)) return tv_launch_attend_tile(a, sm_count, stream);
   if (a.c.head_dim == 128)
     return rows <= 8 ? launch<128, 1>(a, sm_count, stream) : launch<128, 2>(a, sm_count, stream);
   if (rows <= 8) return launch<64, 1>(a, sm_count, stream);

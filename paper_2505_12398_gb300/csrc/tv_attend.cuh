@@ -25,31 +25,158 @@ constexpr int kMaxTokens = 1 << 30;    // tokens of a request that are looked at
 constexpr float kSlack = 8.f;
 constexpr float kLift = 6.f;
 
+constexpr int kStep = 128;             // tokens of a step
+
 struct Request {
   int len, rows, tokens;       // cached tokens, query rows, and tokens that the last row may see
-  uint32_t overrun;            // status bits
-  __device__ __forceinline__ long long steps(int step) const {
-    return rows > 0 ? (tokens + step - 1) / step : 0;
-  }
-  __device__ __forceinline__ int tiles(int group, int rows_of_tile) const {
-    return (int)(((long long)rows * group + rows_of_tile - 1) / rows_of_tile);
-  }
+  bool overrun;                // some of them are outside the page table
 };
 
 // A request with a negative length has no rows; tokens that the page table has no room for
 // are left out.
 __device__ __forceinline__ Request request_of(const AttendArgs& a, int b) {
   Request q;
-  q.overrun = 0;
   const int want = a.rows ? a.rows[b] : a.R;
   q.len = a.t.lengths[b];
   q.rows = q.len < 0 ? 0 : min(max(want, 0), a.R);
   q.len = max(q.len, 0);
   const long long room = min((long long)a.t.max_pages << a.c.page_shift, (long long)kMaxTokens);
   const long long all = (long long)q.len + q.rows;
-  if (all > room) q.overrun = TV_STATUS_BAD_PAGE;
+  q.overrun = all > room;
   q.tokens = (int)min(all, room);
   return q;
+}
+
+// Work is cut into items, one (request, key/value head, tile of `tile` rows) each, in that
+// order, and those into steps of 128 tokens.
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, const Request& q, int tile) {
+  return (int)(((long long)q.rows * a.group + tile - 1) / tile);
+}
+// Tokens that a tile's rows may see.
+__device__ __forceinline__ int tokens_of(const AttendArgs& a, const Request& q, int i, int tile) {
+  if (a.parents) return q.tokens;
+  const long long last = ((long long)(i + 1) * tile - 1) / a.group;
+  return (int)min((long long)q.tokens, q.len + min(last, (long long)q.rows - 1) + 1);
+}
+__device__ __forceinline__ int steps_of(int tokens) { return (tokens + kStep - 1) / kStep; }
+// Steps of a request's items of one head.
+__device__ __forceinline__ long long head_steps(const AttendArgs& a, const Request& q, int tile) {
+  const int tiles = tiles_of(a, q, tile);
+  if (a.parents || tiles <= 1) return (long long)tiles * steps_of(q.tokens);
+  long long n = 0;
+  for (int i = 0; i < tiles; ++i) n += steps_of(tokens_of(a, q, i, tile));
+  return n;
+}
+
+// A run of an item's steps [s0, s1).
+struct Piece {
+  Request rq;
+  int b, head, m0, s0, s1;
+  int tokens, steps;           // of the whole item
+  long long first;             // the item's first step among all
+  __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == steps; }
+};
+
+// The share of the steps that a CTA takes: [total c / ctas, total (c + 1) / ctas).
+struct Shares {
+  long long total, ctas;
+  __device__ __forceinline__ long long begin(long long c) const { return total * c / ctas; }
+  __device__ __forceinline__ int owner(long long step) const {
+    return (int)(((step + 1) * ctas - 1) / total);
+  }
+};
+
+// Goes through the pieces of the steps [cur, end).
+struct Walker {
+  int b;
+  long long in_request, cur, end;
+  __device__ __forceinline__ bool next(const AttendArgs& a, int tile, Piece& p) {
+    while (cur < end) {
+      p.rq = request_of(a, b);
+      const long long per_head = head_steps(a, p.rq, tile), n = per_head * a.c.kv_heads;
+      if (in_request >= n) {
+        in_request -= n;
+        ++b;
+        continue;
+      }
+      p.b = b;
+      p.head = (int)(in_request / per_head);
+      long long at = in_request % per_head;
+      int i = 0;
+      if (a.parents) {
+        const int each = steps_of(p.rq.tokens);
+        i = (int)(at / each);
+        at %= each;
+        p.tokens = p.rq.tokens;
+      } else {
+        for (;; ++i) {
+          p.tokens = tokens_of(a, p.rq, i, tile);
+          if (at < steps_of(p.tokens)) break;
+          at -= steps_of(p.tokens);
+        }
+      }
+      p.steps = steps_of(p.tokens);
+      p.m0 = i * tile;
+      p.s0 = (int)at;
+      p.first = cur - at;
+      const int count = (int)min((long long)p.steps - at, end - cur);
+      p.s1 = p.s0 + count;
+      cur += count;
+      in_request += count;
+      return true;
+    }
+    return false;
+  }
+};
+
+struct Schedule {
+  long long warp_sum[32], total, offset;
+  int request;
+};
+
+// The steps of all requests, and a walker over those of CTA `cta` of at most `ctas`.  By all
+// threads of the block; has a barrier of it.
+__device__ __forceinline__ Shares plan(const AttendArgs& a, Schedule& sh, int tile, int cta,
+                                       int ctas, Walker& w) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = blockDim.x;
+  const int per = (a.B + n - 1) / n;
+  long long mine = 0;
+  for (int b = tid * per; b < min(a.B, (tid + 1) * per); ++b)
+    mine += head_steps(a, request_of(a, b), tile) * a.c.kv_heads;
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long x = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 31) sh.warp_sum[warp] = upto;
+  __syncthreads();
+  long long before = upto - mine, total = 0;
+  for (int i = 0; i < (n >> 5); ++i) {
+    if (i < warp) before += sh.warp_sum[i];
+    total += sh.warp_sum[i];
+  }
+  Shares s;
+  s.total = total;
+  s.ctas = min((long long)ctas, total);
+  w.cur = cta < s.ctas ? s.begin(cta) : 0;
+  w.end = cta < s.ctas ? s.begin(cta + 1) : 0;
+  if (w.cur < w.end && w.cur >= before && w.cur < before + mine) {
+    long long left = w.cur - before;
+    for (int b = tid * per;; ++b) {
+      const long long k = head_steps(a, request_of(a, b), tile) * a.c.kv_heads;
+      if (left < k) {
+        sh.request = b;
+        sh.offset = left;
+        break;
+      }
+      left -= k;
+    }
+  }
+  __syncthreads();
+  w.b = sh.request;
+  w.in_request = sh.offset;
+  return s;
 }
 
 // Calls see(j) for row i of a tree, its parent and so on to the root; false where that leaves
@@ -65,32 +192,19 @@ __device__ __forceinline__ bool walk(const int32_t* parents, int i, F see) {
   }
 }
 
-// Inclusive sums over the block's threads (256 of them); returns the sum before this thread's.
-__device__ __forceinline__ long long block_scan(long long* scan, long long mine,
-                                                long long* total) {
-  const int tid = threadIdx.x;
-  scan[tid] = mine;
-  __syncthreads();
-  for (int d = 1; d < (int)blockDim.x; d <<= 1) {
-    const long long x = tid >= d ? scan[tid - d] : 0;
-    __syncthreads();
-    scan[tid] += x;
-    __syncthreads();
-  }
-  if (tid == (int)blockDim.x - 1) *total = scan[tid];
-  const long long before = scan[tid] - mine;
-  __syncthreads();
-  return before;
-}
-
-// Writes 0 to the rows behind each request's last, and reports lengths and row counts that
-// cannot be.
+// Writes 0 to the rows behind each request's last, and reports lengths, row counts and
+// page tables that cannot be.
 __device__ __forceinline__ void zero_rows(const AttendArgs& a, int D) {
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const int rows = request_of(a, b).rows;
+    const Request q = request_of(a, b);
+    const int rows = q.rows;
     const int want = a.rows ? a.rows[b] : a.R;
-    if (threadIdx.x == 0 && (a.t.lengths[b] < 0 || want < 0 || want > a.R))
-      atomicOr(a.status, (uint32_t)TV_STATUS_BAD_LENGTH);
+    if (threadIdx.x == 0) {
+      uint32_t bits = 0;
+      if (a.t.lengths[b] < 0 || want < 0 || want > a.R) bits |= TV_STATUS_BAD_LENGTH;
+      if (rows > 0 && q.overrun) bits |= TV_STATUS_BAD_PAGE;
+      if (bits) atomicOr(a.status, bits);
+    }
     const size_t row = (size_t)a.c.kv_heads * a.group * D / 8;     // 16-byte pieces
     uint4* const out = reinterpret_cast<uint4*>(a.out) + (size_t)b * a.R * row;
     for (size_t x = rows * row + threadIdx.x; x < a.R * row; x += blockDim.x)
