@@ -145,9 +145,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int G = a.group, H = a.c.kv_heads;
 
-  // rows behind a request's last are 0
-  zero_rows(a, D);
-
   {
     Walker w;
     const Shares shares = plan(a, sh.plan, kRows, blockIdx.x, gridDim.x, w);
@@ -463,6 +460,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
     }
     __syncthreads();
   }
+  zero_rows(a, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps);
 }
 
 template <int D, int NT>

@@ -193,22 +193,24 @@ __device__ __forceinline__ bool walk(const int32_t* parents, int i, F see) {
 }
 
 // Writes 0 to the rows behind each request's last, and reports lengths, row counts and
-// page tables that cannot be.
-__device__ __forceinline__ void zero_rows(const AttendArgs& a, int D) {
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+// page tables that cannot be.  By a warp, `me` of `all`.
+__device__ __forceinline__ void zero_rows(const AttendArgs& a, int D, int me, int all) {
+  const int lane = threadIdx.x & 31;
+  const size_t row = (size_t)a.c.kv_heads * a.group * D / 8;     // 16-byte pieces
+  for (int b = all < a.B ? me : me % a.B; b < a.B; b += all) {
+    // (some warps for a request, or some requests for a warp)
+    const int sub = all < a.B ? 0 : me / a.B, subs = all < a.B ? 1 : (all - 1 - b) / a.B + 1;
     const Request q = request_of(a, b);
-    const int rows = q.rows;
-    const int want = a.rows ? a.rows[b] : a.R;
-    if (threadIdx.x == 0) {
+    if (sub == 0 && lane == 0) {
+      const int want = a.rows ? a.rows[b] : a.R;
       uint32_t bits = 0;
       if (a.t.lengths[b] < 0 || want < 0 || want > a.R) bits |= TV_STATUS_BAD_LENGTH;
-      if (rows > 0 && q.overrun) bits |= TV_STATUS_BAD_PAGE;
+      if (q.rows > 0 && q.overrun) bits |= TV_STATUS_BAD_PAGE;
       if (bits) atomicOr(a.status, bits);
     }
-    const size_t row = (size_t)a.c.kv_heads * a.group * D / 8;     // 16-byte pieces
     uint4* const out = reinterpret_cast<uint4*>(a.out) + (size_t)b * a.R * row;
-    for (size_t x = rows * row + threadIdx.x; x < a.R * row; x += blockDim.x)
-      out[x] = make_uint4(0, 0, 0, 0);
+    for (int i = q.rows + sub; i < a.R; i += subs)
+      for (size_t x = lane; x < row; x += 32) out[i * row + x] = make_uint4(0, 0, 0, 0);
   }
 }
 

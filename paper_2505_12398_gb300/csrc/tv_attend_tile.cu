@@ -11,7 +11,8 @@
 //   warp 16           the products: S = Q K^T (both from shared memory) and O += P V (P
 //                     from tensor memory), S and O of both tiles in tensor memory
 //   warp 17           the CTA's pieces, in a ring that the others read
-// (the registers that these and two idle warps beside them leave go to the softmax).
+//   warps 18, 19      zeros in the rows behind the requests' last
+// (the registers that these four leave go to the softmax).
 // The two tiles take turns: while one's scores become weights, the tensor cores work on the
 // other.  Where an item has 128 rows or fewer both tiles are the same rows and take
 // alternate steps, and their sums are joined at the end.
@@ -51,6 +52,11 @@ constexpr int kStages = 2;
 constexpr int kOkSlots = 4;
 constexpr uint32_t kHalfBytes = kTile * 128;     // 64 columns (128 bytes) of a tile's rows
 constexpr int kJoinParts = 8;                    // blocks that join one item's rows
+
+// An item that begins in a CTA and goes on in later ones, up to `last`; b < 0: there is none.
+struct Split {
+  int b, head, m0, last;
+};
 
 // A piece as the warps take it; more = 0: there is none.
 struct Work {
@@ -129,6 +135,24 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
       : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]),
+                 "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -216,10 +240,23 @@ struct Token {
   }
 };
 
+__device__ __forceinline__ void hide(uint32_t (&c)[32], uint32_t see) {
+#pragma unroll
+  for (int y = 0; y < 32; ++y)
+    if (!(see >> y & 1)) c[y] = 0xff800000u;
+}
 // The lowest n bits of a word that holds bits [at, at + 32).
 __device__ __forceinline__ uint32_t low_bits(int n, int at) {
   const int k = n - at;
   return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+}
+
+// The scratch: two pieces of every CTA, their rows' (maximum, sum), the CTAs' split items.
+__device__ __forceinline__ float2* stats_of(const AttendArgs& a, int D, int ctas) {
+  return reinterpret_cast<float2*>(a.part + (size_t)2 * ctas * 2 * kTile * D);
+}
+__device__ __forceinline__ Split* splits_of(const AttendArgs& a, int D, int ctas) {
+  return reinterpret_cast<Split*>(stats_of(a, D, ctas) + (size_t)2 * ctas * 2 * kTile);
 }
 
 template <int D>
@@ -254,9 +291,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     fence_mbar_init();
   }
   if (warp == kMmaWarp) tmem_alloc<false>(&sh.tmem);
-  zero_rows(a, D);
   Walker walker;
-  plan(a, sh.plan, rows_of_item, blockIdx.x, gridDim.x, walker);
+  const Shares shares = plan(a, sh.plan, rows_of_item, blockIdx.x, gridDim.x, walker);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -325,15 +361,22 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     } else if (warp == kMmaWarp + 1 && lane == 0) {
       // ---- pieces ----
       Piece p;
+      Split split_item = {-1, 0, 0, 0};
       for (uint32_t n = 0;; ++n) {
         wait_on(&sh.taken[n % kWorkSlots], ((n / kWorkSlots) & 1) ^ 1, bad);
         Work w = {};
-        if (!bad && walker.next(a, rows_of_item, p))
+        if (!bad && walker.next(a, rows_of_item, p)) {
           w = Work{1, p.b, p.head, p.m0, p.s0, p.s1, p.steps, p.tokens, p.rq.len, p.rq.rows};
+          if (p.s0 == 0 && p.s1 < p.steps)
+            split_item = Split{p.b, p.head, p.m0, shares.owner(p.first + p.steps - 1)};
+        }
         sh.work[n % kWorkSlots] = w;
         mbar_arrive(&sh.given[n % kWorkSlots]);
         if (!w.more) break;
       }
+      splits_of(a, D, gridDim.x)[blockIdx.x] = split_item;
+    } else if (warp > kMmaWarp + 1) {
+      zero_rows(a, D, blockIdx.x * 2 + (warp & 1), gridDim.x * 2);
     }
   } else if (warp >= kSoftmaxWarps) {
     // ---- keys and values to fp16 ----
@@ -380,7 +423,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       }
       softmax_barrier();
       if (!sh.softmax_more) break;
-      const Work& p = sh.work[taken % kWorkSlots];
+      const Work p = sh.work[taken % kWorkSlots];
       const int len = p.len, M = p.rows * a.group;
       const int m = p.m0 + (split ? 0 : x * kTile) + r;
       const bool in = m < M;
@@ -464,21 +507,21 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             for (int k = 0; k < 4; ++k) see[k] &= mine[k];
           }
           // the largest score
-          float top = TV_NEG_INF;
+          float top = TV_NEG_INF, top1 = TV_NEG_INF;
           uint32_t c[32];
-#pragma unroll
+#pragma unroll 1
           for (int k = 0; k < 4; ++k) {
             tmem_ld32(ts + 32 * k, c);
+            const uint32_t now = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
             tmem_wait(c);
-            if (part) {
+            if (part) hide(c, now);
 #pragma unroll
-              for (int y = 0; y < 32; ++y)
-                if (!(see[k] >> y & 1)) c[y] = 0xff800000u;
+            for (int y = 0; y < 32; y += 4) {
+              top = fmaxf(fmaxf(top, __uint_as_float(c[y])), __uint_as_float(c[y + 1]));
+              top1 = fmaxf(fmaxf(top1, __uint_as_float(c[y + 2])), __uint_as_float(c[y + 3]));
             }
-#pragma unroll
-            for (int y = 0; y < 32; ++y) top = fmaxf(top, __uint_as_float(c[y]));
           }
-          top *= f;
+          top = f * fmaxf(top, top1);
           if (__any_sync(0xffffffffu, top > mref + kSlack)) {
             float down = 1.f;
             if (top > mref) {
@@ -489,7 +532,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             if (i >= 2) {                                  // there is a sum to scale
               wait_on(&sh.ofull[x], (count - 1) & 1, bad);
               tc_fence_after();
-#pragma unroll
+#pragma unroll 1
               for (int k = 0; k < D / 32; ++k) {
                 tmem_ld32(to + 32 * k, c);
                 tmem_wait(c);
@@ -499,31 +542,29 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
               }
             }
           }
-          // the weights
           const float off = kLift - (mref == TV_NEG_INF ? 0.f : mref);
-          float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
+          const float2 ff = make_float2(f, f), oo = make_float2(off, off);
+          float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
           for (int k = 0; k < 4; ++k) {
             tmem_ld32(ts + 32 * k, c);
+            const uint32_t now = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
             tmem_wait(c);
-            if (part) {
-#pragma unroll
-              for (int y = 0; y < 32; ++y)
-                if (!(see[k] >> y & 1)) c[y] = 0xff800000u;
-            }
+            if (part) hide(c, now);
             uint32_t w[16];
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const float e0 = ex2(fmaf(__uint_as_float(c[2 * y]), f, off));
-              const float e1 = ex2(fmaf(__uint_as_float(c[2 * y + 1]), f, off));
-              sum0 += e0;
-              sum1 += e1;
-              const __half2 h = __floats2half2_rn(e0, e1);
-              w[y] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int y = 0; y < 32; y += 2) {
+              float2 e = __ffma2_rn(make_float2(__uint_as_float(c[y]), __uint_as_float(c[y + 1])), ff, oo);
+              e.x = ex2(e.x);
+              e.y = ex2(e.y);
+              acc[(y >> 1) & 1] = __fadd2_rn(acc[(y >> 1) & 1], e);
+              const __half2 h = __floats2half2_rn(e.x, e.y);
+              w[y >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
             tmem_st16(ts + 16 * k, w);
           }
-          l += sum0 + sum1;
+          acc[0] = __fadd2_rn(acc[0], acc[1]);
+          l += acc[0].x + acc[0].y;
           tmem_stored();
         }
         tc_fence_before();
@@ -601,9 +642,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
           }
         }
         if (!whole && !(split && x == 1)) {
-          float2* const stats = reinterpret_cast<float2*>(
-              a.part + (size_t)2 * gridDim.x * 2 * kTile * D);
-          stats[slot * 2 * kTile + at_row] = make_float2(mref, l);
+          stats_of(a, D, gridDim.x)[slot * 2 * kTile + at_row] = make_float2(mref, l);
         }
       }
       tc_fence_before();
@@ -621,35 +660,25 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
 }
 
 // Joins the pieces of an item that spans CTAs: block c * kJoinParts + part takes a part of
-// the rows of the item that begins in CTA c and goes on in the next.
+// the rows of the item that begins in CTA c and goes on in later ones.
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int split, int ctas) {
-  __shared__ Schedule sh;
-  const int rows_of_item = split ? kTile : 2 * kTile;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // (launched before the pieces are there)
   const int c0 = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts;
-  Walker w;
-  const Shares shares = plan(a, sh, rows_of_item, c0, ctas, w);
-  Piece p, last;
-  bool any = false;
-  while (w.next(a, rows_of_item, p)) {
-    last = p;
-    any = true;
-  }
-  if (!any || last.s0 != 0 || last.s1 == last.steps) return;
-  const int c1 = shares.owner(last.first + last.steps - 1);
-  const int M = last.rq.rows * a.group;
-  const float up = pow2i(exponent_of(a.c, a.layer, 1, last.head));
-  const int rows = rows_of_item / kJoinParts;
-  const float2* const stats =
-      reinterpret_cast<const float2*>(a.part + (size_t)2 * ctas * 2 * kTile * D);
+  const Split item = splits_of(a, D, ctas)[c0];
+  if (item.b < 0) return;
+  const int M = request_of(a, item.b).rows * a.group;
+  const float up = pow2i(exponent_of(a.c, a.layer, 1, item.head));
+  const int rows = (split ? kTile : 2 * kTile) / kJoinParts;
+  const float2* const stats = stats_of(a, D, ctas);
   for (int x = threadIdx.x; x < rows * D / 4; x += blockDim.x) {
     const int row = part * rows + x / (D / 4), col = x % (D / 4) * 4;
-    if (last.m0 + row >= M) break;
+    if (item.m0 + row >= M) break;
     float top = TV_NEG_INF, sum = 0.f;
-    for (int c = c0; c <= c1; ++c)
+    for (int c = c0; c <= item.last; ++c)
       top = fmaxf(top, stats[((size_t)2 * c + (c == c0)) * 2 * kTile + row].x);
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= c1; ++c) {
+    for (int c = c0; c <= item.last; ++c) {
       const size_t at = ((size_t)2 * c + (c == c0)) * 2 * kTile + row;
       const float2 ms = stats[at];
       const float f = ms.y != ms.y ? ms.y : ms.x == TV_NEG_INF ? 0.f : ex2(ms.x - top);
@@ -660,7 +689,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int split, int 
       y.z += f * v.z;
       y.w += f * v.w;
     }
-    store_out(a, last.b, last.head, last.m0 + row, M, col, D, y, sum, up);
+    store_out(a, item.b, item.head, item.m0 + row, M, col, D, y, sum, up);
   }
 }
 
@@ -675,8 +704,21 @@ int launch_tiles(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const int split = (long long)a.R * a.group <= kTile;
   const int wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   tile_kernel<D><<<sm_count, kTileThreads, smem, stream>>>(a, split, wide);
-  join_kernel<D><<<sm_count * kJoinParts, 256, 0, stream>>>(a, split, sm_count);
-  return cudaGetLastError() == cudaSuccess ? 0 : -5;
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t join = {};
+  join.gridDim = dim3((unsigned)(sm_count * kJoinParts));
+  join.blockDim = dim3(256);
+  join.stream = stream;
+  join.attrs = &early;
+  join.numAttrs = 1;
+  if (cudaGetLastError() != cudaSuccess ||
+      cudaLaunchKernelEx(&join, join_kernel<D>, a, split, sm_count) != cudaSuccess) {
+    cudaGetLastError();
+    return -5;
+  }
+  return 0;
 }
 
 }  // namespace attend
@@ -685,7 +727,7 @@ int launch_tiles(const AttendArgs& a, int sm_count, cudaStream_t stream) {
 using namespace tvk::attend;
 
 size_t tv_attend_tile_scratch(int sm_count) {
-  return (size_t)sm_count * 2 * 2 * kTile * (128 + 2) * sizeof(float);
+  return (size_t)sm_count * (2 * 2 * kTile * (128 + 2) * sizeof(float) + sizeof(Split));
 }
 
 int tv_launch_attend_tile(const AttendArgs& a, int sm_count, cudaStream_t stream) {
