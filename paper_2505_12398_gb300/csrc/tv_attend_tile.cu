@@ -3,16 +3,18 @@
 // cores.  Mathematics, rounding and the cut into pieces are those of tv_attend.cu.
 //
 // One persistent CTA per SM, two tiles of 128 rows at a time:
-//   warps 0-3, 4-7    softmax of tile 0 and 1, one row per thread: scores from tensor
-//                     memory, weights back into it as fp16, over the scores' first half
-//   warps 8-11        widen 128 tokens' keys to fp16 in shared memory (a token per thread,
+//   warps 0-7, 8-15   softmax of tile 0 and 1, half a row (64 of a step's tokens) per thread:
+//                     scores from tensor memory, weights back into it as fp16, over the
+//                     first half of the thread's own scores
+//   warps 16-19       widen 128 tokens' keys to fp16 in shared memory (a token per thread,
 //                     its codes loaded a step ahead), two stages
-//   warps 12-15       the same for values
-//   warp 16           the products: S = Q K^T (both from shared memory) and O += P V (P
+//   warps 20-23       the same for values
+//   warp 24           the products: S = Q K^T (both from shared memory) and O += P V (P
 //                     from tensor memory), S and O of both tiles in tensor memory
-//   warp 17           the CTA's pieces, in a ring that the others read
-//   warps 18, 19      zeros in the rows behind the requests' last
-// (the registers that these four leave go to the softmax).
+//   warp 25           the CTA's pieces, in a ring that the others read
+//   warps 26, 27      the next piece's queries to fp16 in shared memory as soon as the last
+//                     product that reads the present ones is done; at the end, zeros in the
+//                     rows behind the requests' last
 // The two tiles take turns: while one's scores become weights, the tensor cores work on the
 // other.  Where an item has 128 rows or fewer both tiles are the same rows and take
 // alternate steps, and their sums are joined at the end.
@@ -39,15 +41,12 @@ namespace attend {
 using namespace gemm;
 
 constexpr int kTile = 128;
-constexpr int kSoftmaxWarps = 8;
+constexpr int kHalfTile = 64;                    // tokens of a thread
+constexpr int kSoftmaxWarps = 16;
 constexpr int kWidenWarps = 8;                   // four for keys, four for values
 constexpr int kMmaWarp = kSoftmaxWarps + kWidenWarps;
-constexpr int kTileThreads = 32 * (kMmaWarp + 4);
-// registers per thread after the split
-constexpr int kRegsSoftmax = 136, kRegsWiden = 72, kRegsMma = 64, kRegsLaunch = 96;
-static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kWidenWarps * kRegsWiden + 4 * kRegsMma) <=
-                  kTileThreads * kRegsLaunch,
-              "the warpgroups' registers fit what the block was launched with");
+constexpr int kQueryWarps = 2;
+constexpr int kTileThreads = 32 * (kMmaWarp + 2 + kQueryWarps);
 constexpr int kStages = 2;
 constexpr int kOkSlots = 4;
 constexpr uint32_t kHalfBytes = kTile * 128;     // 64 columns (128 bytes) of a tile's rows
@@ -64,31 +63,23 @@ struct Work {
   __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == steps; }
 };
 constexpr int kWorkSlots = 4;
-constexpr int kTakers = kSoftmaxWarps + kWidenWarps + 1;
+constexpr int kTakers = kSoftmaxWarps + kWidenWarps + 1 + kQueryWarps;
 
 struct TileShared {
   uint64_t given[kWorkSlots], taken[kWorkSlots];
   Work work[kWorkSlots];
-  int softmax_more;
+  int more[2][2];                                // [piece % 2][tile]
   uint64_t kfull[kStages], kempty[kStages], vfull[kStages], vempty[kStages];
-  uint64_t sfull[2], pfull[2], ofull[2], qfull;
+  uint64_t sfull[2], pfull[2], ofull[2], qfull, qempty, merge;
   uint32_t tmem;
   // tokens of a step that exist and have a page; a slot is used again four steps later, when
   // both softmaxes are done with it
-  uint4 ok[kOkSlots];
-  float m[2][kTile], l[2][kTile];
+  alignas(16) uint32_t ok[kOkSlots][4];
+  float factor[2][2 * kTile];                    // [piece % 2], of a row's scores
+  float top[2][2][kTile], l[2][2][kTile], m[2][kTile];
   Schedule plan;
-  int32_t parents[1024];
+  int32_t parents[2][1024];                      // [piece % 2]
 };
-
-template <int kRegs>
-__device__ __forceinline__ void regs_fewer() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
-template <int kRegs>
-__device__ __forceinline__ void regs_more() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
-}
 
 __device__ __forceinline__ void wait_on(uint64_t* bar, uint32_t parity, uint32_t& bad) {
   if (!mbar_try_wait(bar, parity) && !bad) bad = mbar_wait(bar, parity) ? 0u : 1u;
@@ -106,13 +97,16 @@ __device__ __forceinline__ void give_back(TileShared& sh, uint32_t n) {
   if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.taken[n % kWorkSlots]);
 }
 
-// Descriptor of an operand whose rows are 128 bytes (with the 128-byte swizzle) and whose
-// columns are the other dimension than that of the sum: 8 rows of the sum's dimension after
-// 1024 bytes, the next 64 columns after kHalfBytes.
-__device__ __forceinline__ uint64_t column_desc(const void* p) {
-  const uint64_t addr = smem_u32(p);
-  return ((addr >> 4) & 0x3FFFull) | ((uint64_t)(kHalfBytes >> 4) << 16) |
-         ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+// Descriptors of operands whose rows are 128 bytes with the 128-byte swizzle, in two words:
+// the start address >> 4 and the leading offset, and what all have (8 rows after 1024 bytes).
+// Rows along the other dimension than the sum's (as smem_desc), and rows along the sum's, the
+// next 64 columns of the other after kHalfBytes.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t row_desc(const void* p) {
+  return (smem_u32(p) >> 4) | (1u << 16);
+}
+__device__ __forceinline__ uint32_t column_desc(const void* p) {
+  return (smem_u32(p) >> 4) | ((kHalfBytes >> 4) << 16);
 }
 // Instruction descriptor of kind::f16: fp32 accumulator (bits 4-5 = 1), fp16 A and B (0), B by
 // columns (bit 16), N >> 3 in bits 17-22, M >> 4 in bits 24-28.
@@ -120,20 +114,22 @@ __device__ __forceinline__ constexpr uint32_t f16_desc(int m, int n, bool by_col
   return (1u << 4) | ((by_columns ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(m >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       bool accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(kDescHigh), "r"(idesc), "r"((uint32_t)accumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                       bool accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(kDescHigh), "r"(idesc), "r"((uint32_t)accumulate)
       : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
@@ -181,8 +177,19 @@ __device__ __forceinline__ void tmem_stored() {
 __device__ __forceinline__ void async_visible() {      // shared memory written, for the products
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
-__device__ __forceinline__ void softmax_barrier() {    // both softmaxes' threads
-  asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftmaxWarps) : "memory");
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// Whether any of the 64 threads that share 32 rows says so.
+__device__ __forceinline__ bool pair_any(int id, bool say) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+      "bar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)say), "r"(id)
+      : "memory");
+  return any != 0;
 }
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
                                        uint32_t d) {
@@ -240,11 +247,36 @@ struct Token {
   }
 };
 
-__device__ __forceinline__ void hide(uint32_t (&c)[32], uint32_t see) {
+// A thread's 64 scores, 16 at a time with the next on their way.  (Not a loop: registers that a
+// load is still to fill must not be moved, as they may be from one turn to the next.)
+template <typename F>
+__device__ __forceinline__ void for_scores(uint32_t ts, F use) {
+  uint32_t c[2][16];
+  tmem_ld16(ts, c[0]);
 #pragma unroll
-  for (int y = 0; y < 32; ++y)
-    if (!(see >> y & 1)) c[y] = 0xff800000u;
+  for (int k = 0; k < kHalfTile / 16; ++k) {
+    uint32_t(&x)[16] = c[k & 1];
+    tmem_wait16(x);
+    if (k + 1 < kHalfTile / 16) tmem_ld16(ts + 16 * (k + 1), c[(k + 1) & 1]);
+    use(k, x);
+  }
 }
+// Scores that a row does not see become -inf in tensor memory; a set bit in `see` is seen.
+__device__ __noinline__ void hide_scores(uint32_t ts, uint2 see) {
+#pragma unroll 1
+  for (int k = 0; k < kHalfTile; k += 16) {
+    uint32_t c[16];
+    tmem_ld16(ts + k, c);
+    tmem_wait16(c);
+    const uint32_t bits = (k < 32 ? see.x : see.y) >> (k & 16);
+#pragma unroll
+    for (int y = 0; y < 16; ++y)
+      if (!(bits >> y & 1)) c[y] = 0xff800000u;
+    tmem_st16(ts + k, c);
+  }
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // The lowest n bits of a word that holds bits [at, at + 32).
 __device__ __forceinline__ uint32_t low_bits(int n, int at) {
   const int k = n - at;
@@ -280,10 +312,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sh.sfull[x], 1);
-      mbar_init(&sh.pfull[x], 4);
+      mbar_init(&sh.pfull[x], kSoftmaxWarps / 2);
       mbar_init(&sh.ofull[x], 1);
     }
-    mbar_init(&sh.qfull, kSoftmaxWarps);
+    mbar_init(&sh.qfull, kQueryWarps);
+    mbar_init(&sh.qempty, 1 + kSoftmaxWarps);
+    mbar_init(&sh.merge, kSoftmaxWarps);
     for (int i = 0; i < kWorkSlots; ++i) {
       mbar_init(&sh.given[i], 1);
       mbar_init(&sh.taken[i], kTakers);
@@ -299,67 +333,88 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   const uint32_t tmem = sh.tmem;
   uint32_t bad = 0, taken = 0;                   // pieces so far
 
-  if (warp >= kMmaWarp) {
+  if (warp == kMmaWarp) {
     // ---- products ----
-    regs_fewer<kRegsMma>();
-    if (warp == kMmaWarp) {
-      const uint64_t qd[2] = {smem_desc(q_tiles), smem_desc(q_tiles + (split ? 0 : kTileBytes))};
-      const uint64_t kd = smem_desc(k_tiles), vd = column_desc(v_tiles);
-      uint32_t steps_done = 0, pcount[2] = {0, 0};
-      for (; const Work* const w = take(sh, taken, bad); ++taken) {
-        const int n = w->s1 - w->s0, ops = split ? n : 2 * n;
-        give_back(sh, taken);
-        wait_on(&sh.qfull, taken & 1, bad);
+    const uint32_t qd0 = row_desc(q_tiles), qd1 = row_desc(q_tiles + (split ? 0 : kTileBytes));
+    const uint32_t kd = row_desc(k_tiles), vd = column_desc(v_tiles);
+    uint32_t steps_done = 0, pcount[2] = {0, 0};
+    for (; const Work* const w = take(sh, taken, bad); ++taken) {
+      const int n = w->s1 - w->s0, ops = split ? n : 2 * n;
+      give_back(sh, taken);
+      auto step_of = [&](int i) { return steps_done + (uint32_t)(split ? i : i >> 1); };
+      auto wait_keys = [&](int i, int x) {
+        const uint32_t s = step_of(i);
+        if (split || x == 0) wait_on(&sh.kfull[s % kStages], (s / kStages) & 1, bad);
+      };
+      auto wait_weights = [&](int i, int x) {
+        const uint32_t s = step_of(i);
+        if (split || x == 0) wait_on(&sh.vfull[s % kStages], (s / kStages) & 1, bad);
+        wait_on(&sh.pfull[x], pcount[x] & 1, bad);
+        ++pcount[x];
         tc_fence_after();
-        auto scores = [&](int i, int x) {
-          const uint32_t s = steps_done + (split ? i : i >> 1), stage = s % kStages;
-          if (split || x == 0) {
-            wait_on(&sh.kfull[stage], (s / kStages) & 1, bad);
+      };
+      auto scores = [&](int i, int x) {
+        const uint32_t stage = step_of(i) % kStages;
+        if (elect_one()) {
+          const uint32_t q = x ? qd1 : qd0, k0 = kd + stage * (kTileBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (uint32_t)((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+            mma_ss(tmem + x * kTile, q + off, k0 + off, f16_desc(kTile, kTile, false), k > 0);
+          }
+          umma_commit<false>(&sh.sfull[x]);
+          if (split || x == 1) umma_commit<false>(&sh.kempty[stage]);
+          if (i == ops - 1) umma_commit<false>(&sh.qempty);
+        }
+        __syncwarp();
+      };
+      auto values = [&](int i, int x) {
+        const uint32_t stage = step_of(i) % kStages;
+        if (elect_one()) {
+          const uint32_t v0 = vd + stage * (kTileBytes >> 4);
+#pragma unroll
+          for (int k = 0; k < kTile / 16; ++k)
+            mma_ts(tmem + 2 * kTile + x * D,
+                   tmem + x * kTile + (k >> 2) * kHalfTile + (k & 3) * 8, v0 + k * (2048u >> 4),
+                   f16_desc(kTile, D, true), i >= 2 || k > 0);
+          umma_commit<false>(&sh.ofull[x]);
+          if (split || x == 1) umma_commit<false>(&sh.vempty[stage]);
+        }
+        __syncwarp();
+      };
+      // (where the tiles share a step its keys are there long before; where they do not they may
+      // come later than the weights)
+      auto turn = [&](int i, int x) {
+        const bool next = i + 2 < ops;
+        if (next && !split) wait_keys(i + 2, x);
+        wait_weights(i, x);
+        values(i, x);
+        if (next) {
+          if (split) {
+            wait_keys(i + 2, x);
             tc_fence_after();
           }
-          if (elect_one()) {
-  #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (uint32_t)((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-              mma_ss(tmem + x * kTile, qd[x] + off, kd + stage * (kTileBytes >> 4) + off,
-                     f16_desc(kTile, kTile, false), k > 0);
-            }
-            umma_commit<false>(&sh.sfull[x]);
-            if (split || x == 1) umma_commit<false>(&sh.kempty[stage]);
-          }
-          __syncwarp();
-        };
-        auto values = [&](int i, int x) {
-          const uint32_t s = steps_done + (split ? i : i >> 1), stage = s % kStages;
-          if (split || x == 0) wait_on(&sh.vfull[stage], (s / kStages) & 1, bad);
-          wait_on(&sh.pfull[x], pcount[x] & 1, bad);
-          ++pcount[x];
-          tc_fence_after();
-          if (elect_one()) {
-  #pragma unroll
-            for (int k = 0; k < kTile / 16; ++k)
-              mma_ts(tmem + 2 * kTile + x * D, tmem + x * kTile + k * 8,
-                     vd + stage * (kTileBytes >> 4) + k * (2048u >> 4), f16_desc(kTile, D, true),
-                     i >= 2 || k > 0);
-            umma_commit<false>(&sh.ofull[x]);
-            if (split || x == 1) umma_commit<false>(&sh.vempty[stage]);
-          }
-          __syncwarp();
-        };
-        scores(0, 0);
-        if (ops > 1) scores(1, 1);
-        for (int i = 0; i < ops; i += 2) {
-          values(i, 0);
-          if (i + 2 < ops) scores(i + 2, 0);
-          if (i + 1 < ops) {
-            values(i + 1, 1);
-            if (i + 3 < ops) scores(i + 3, 1);
-          }
+          scores(i + 2, x);
         }
-        steps_done += (uint32_t)n;
+      };
+      wait_on(&sh.qfull, taken & 1, bad);
+      wait_keys(0, 0);
+      tc_fence_after();
+      scores(0, 0);
+      if (ops > 1) {
+        wait_keys(1, 1);
+        tc_fence_after();
+        scores(1, 1);
       }
-    } else if (warp == kMmaWarp + 1 && lane == 0) {
-      // ---- pieces ----
+      for (int i = 0; i < ops; i += 2) {
+        turn(i, 0);
+        if (i + 1 < ops) turn(i + 1, 1);
+      }
+      steps_done += (uint32_t)n;
+    }
+  } else if (warp == kMmaWarp + 1) {
+    // ---- pieces ----
+    if (lane == 0) {
       Piece p;
       Split split_item = {-1, 0, 0, 0};
       for (uint32_t n = 0;; ++n) {
@@ -375,12 +430,67 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         if (!w.more) break;
       }
       splits_of(a, D, gridDim.x)[blockIdx.x] = split_item;
-    } else if (warp > kMmaWarp + 1) {
-      zero_rows(a, D, blockIdx.x * 2 + (warp & 1), gridDim.x * 2);
     }
+  } else if (warp > kMmaWarp + 1) {
+    // ---- queries: a row by D / 8 lanes, 8 columns each ----
+    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAhead = 4;
+    const int me = warp - (kMmaWarp + 2), col = lane % kLanes;
+    for (; const Work* const w = take(sh, taken, bad); ++taken) {
+      const Work p = *w;
+      give_back(sh, taken);
+      const int M = p.rows * a.group;
+      const int key_exponent = exponent_of(a.c, a.layer, 0, p.head);
+      wait_on(&sh.qempty, (taken & 1) ^ 1, bad);
+      if (a.parents && p.s1 * kStep > p.len)
+        for (int i = lane + 32 * me; i < p.rows; i += 32 * kQueryWarps)
+          sh.parents[taken & 1][i] = a.parents[(size_t)p.b * a.R + i];
+      // (rows behind the last stay as they are: nothing of theirs is stored)
+      const int rows = min(rows_of_item, M - p.m0);
+      for (int r0 = me * kRows; r0 < rows; r0 += kQueryWarps * kRows * kAhead) {
+        uint4 w4[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int r = min(r0 + k * kQueryWarps * kRows + lane / kLanes, rows - 1), m = p.m0 + r;
+          w4[k] = __ldg(reinterpret_cast<const uint4*>(
+                            a.q + (((size_t)p.b * a.R + m / a.group) * a.c.kv_heads * a.group +
+                                   (size_t)p.head * a.group + m % a.group) * D) + col);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int r = min(r0 + k * kQueryWarps * kRows + lane / kLanes, rows - 1);
+          const uint32_t u[4] = {w4[k].x, w4[k].y, w4[k].z, w4[k].w};
+          float top = 0.f;
+#pragma unroll
+          for (int y = 0; y < 4; ++y)
+            top = max_nan(top, max_nan(fabsf(bf16_lo(u[y])), fabsf(bf16_hi(u[y]))));
+#pragma unroll
+          for (int d = kLanes / 2; d > 0; d >>= 1)
+            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const QueryScale s(top);
+          float f = s.factor(a.scale_log2e, key_exponent);
+          const float sign = f < 0.f ? -1.f : 1.f;         // the factor is made positive,
+          f = fabsf(f);
+          if (f < 1e-37f) f = 1e-37f;                      // and keeps -inf what it is
+          uint32_t h[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const __half2 z = __floats2half2_rn(sign * s.apply(bf16_lo(u[y])),
+                                                sign * s.apply(bf16_hi(u[y])));
+            h[y] = *reinterpret_cast<const uint32_t*>(&z);
+          }
+          sts128(piece_at(smem_u32(q_tiles) + (uint32_t)(r >> 7) * kTileBytes, r & (kTile - 1),
+                          col),
+                 h[0], h[1], h[2], h[3]);
+          if (col == 0) sh.factor[taken & 1][r] = f;
+        }
+      }
+      async_visible();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.qfull);
+    }
+    zero_rows(a, D, (int)blockIdx.x * kQueryWarps + me, (int)gridDim.x * kQueryWarps);
   } else if (warp >= kSoftmaxWarps) {
     // ---- keys and values to fp16 ----
-    regs_fewer<kRegsWiden>();
     const int side = warp >= kSoftmaxWarps + 4, row = tid & (kTile - 1);
     uint64_t* const full = side ? sh.vfull : sh.kfull;
     uint64_t* const empty = side ? sh.vempty : sh.kempty;
@@ -388,6 +498,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     uint32_t s = 0;
     for (; const Work* const w = take(sh, taken, bad); ++taken) {
       const Work p = *w;
+      give_back(sh, taken);
       Token<D> next;
       next.load(a, p, (p.s1 - 1) * kStep + row, side);
       for (int step = p.s1 - 1; step >= p.s0; --step, ++s) {
@@ -398,7 +509,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         now.widen_to(base + stage * kTileBytes, row);
         if (!side) {
           const uint32_t word = __ballot_sync(0xffffffffu, now.there);
-          if (lane == 0) reinterpret_cast<uint32_t*>(&sh.ok[s % kOkSlots])[warp & 3] = word;
+          if (lane == 0) sh.ok[s % kOkSlots][warp & 3] = word;
           if (!now.there && step * kStep + row < p.tokens)
             atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
         }
@@ -406,71 +517,34 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         __syncwarp();
         if (lane == 0) mbar_arrive(&full[stage]);
       }
-      give_back(sh, taken);
     }
   } else {
     // ---- softmax ----
-    regs_more<kRegsSoftmax>();
-    const int x = warp >> 2, r = tid & (kTile - 1);
+    const int x = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
+    const int tile_id = 1 + x, pair_id = 4 + 4 * x + (warp & 3);         // barriers
     const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16;
-    const uint32_t ts = tmem + x * kTile + lanes, to = tmem + 2 * kTile + x * D + lanes;
-    const uint32_t q_at = smem_u32(q_tiles) + (split ? 0u : (uint32_t)x * kTileBytes);
-    uint32_t steps_done = 0, count = 0;          // of this tile: scores taken
+    const uint32_t ts = tmem + x * kTile + half * kHalfTile + lanes;
+    const uint32_t to = tmem + 2 * kTile + x * D + half * (D / 2) + lanes;
+    uint32_t steps_done = 0, count = 0, merged = 0;        // count: scores of this tile taken
     for (;; ++taken) {
-      if (warp == 0) {                           // (the softmaxes meet at barriers)
+      if ((warp & 7) == 0) {                     // (a tile's warps meet at barriers)
         const bool more = take(sh, taken, bad) != nullptr;
-        if (lane == 0) sh.softmax_more = more;
+        if (lane == 0) sh.more[taken & 1][x] = more;
       }
-      softmax_barrier();
-      if (!sh.softmax_more) break;
+      named_barrier(tile_id, 16 * kSoftmaxWarps);
+      if (!sh.more[taken & 1][x]) break;
       const Work p = sh.work[taken % kWorkSlots];
+      give_back(sh, taken);
       const int len = p.len, M = p.rows * a.group;
       const int m = p.m0 + (split ? 0 : x * kTile) + r;
       const bool in = m < M;
       const int node = in ? m / a.group : 0;
       const bool live = __any_sync(0xffffffffu, in);
-      if (a.parents && p.s1 * kStep > len)
-        for (int i = tid; i < p.rows; i += 32 * kSoftmaxWarps)
-          sh.parents[i] = a.parents[(size_t)p.b * a.R + i];
-      // this thread's row of queries
-      float f;
-      {
-        uint4 w[D / 8];
-        const uint4* const src = reinterpret_cast<const uint4*>(
-            a.q + (((size_t)p.b * a.R + node) * a.c.kv_heads * a.group +
-                   (size_t)p.head * a.group + (in ? m % a.group : 0)) * D);
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          w[i] = in ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
-          const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            top = max_nan(top, max_nan(fabsf(bf16_lo(u[k])), fabsf(bf16_hi(u[k]))));
-        }
-        const QueryScale s(top);
-        f = s.factor(a.scale_log2e, exponent_of(a.c, a.layer, 0, p.head));
-        const float sign = f < 0.f ? -1.f : 1.f;           // the factor is made positive,
-        f = fabsf(f);
-        if (f < 1e-37f) f = 1e-37f;                        // and keeps -inf what it is
-        if (!(split && x == 1)) {
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) {
-            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-            uint32_t h[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const __half2 y = __floats2half2_rn(sign * s.apply(bf16_lo(u[k])),
-                                                  sign * s.apply(bf16_hi(u[k])));
-              h[k] = *reinterpret_cast<const uint32_t*>(&y);
-            }
-            sts128(piece_at(q_at, r, i), h[0], h[1], h[2], h[3]);
-          }
-        }
-      }
-      async_visible();
-      softmax_barrier();                                   // (parents are there, too)
-      if (lane == 0) mbar_arrive(&sh.qfull);
+      const int32_t* const parents = sh.parents[taken & 1];
+      wait_on(&sh.qfull, taken & 1, bad);
+      const float f = in ? sh.factor[taken & 1][(split ? 0 : x * kTile) + r] : 1e-37f;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.qempty);
 
       float mref = TV_NEG_INF, l = 0.f;
       int at_node = node;                                  // the path's next node, -1: done
@@ -481,48 +555,44 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         wait_on(&sh.sfull[x], count & 1, bad);
         tc_fence_after();
         if (live) {
-          const uint4 ok = sh.ok[(steps_done + (uint32_t)j) % kOkSlots];
-          const bool part = pos + kStep > len || (ok.x & ok.y & ok.z & ok.w) != 0xffffffffu;
-          uint32_t see[4] = {ok.x, ok.y, ok.z, ok.w};
+          uint2 see = *reinterpret_cast<const uint2*>(
+              &sh.ok[(steps_done + (uint32_t)j) % kOkSlots][2 * half]);
           if (pos + kStep > len) {                         // some tokens are the tree's
-            uint32_t mine[4];
-            const int upto = len - pos + (a.parents ? 0 : node + 1);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) mine[k] = low_bits(upto, 32 * k);
+            const int from = pos + half * kHalfTile;
+            const int upto = len - from + (a.parents ? 0 : node + 1);
+            uint2 mine = make_uint2(low_bits(upto, 0), low_bits(upto, 32));
             if (a.parents) {
               while (at_node >= 0 && len + at_node >= pos) {
-                const int bit = len + at_node - pos;
-                if (bit < kStep) {
-#pragma unroll
-                  for (int k = 0; k < 4; ++k)
-                    if (bit >> 5 == k) mine[k] |= 1u << (bit & 31);
-                }
-                const int up = sh.parents[at_node];
+                const int bit = len + at_node - from;
+                if (bit >= 0 && bit < 32) mine.x |= 1u << bit;
+                if (bit >= 32 && bit < 64) mine.y |= 1u << (bit - 32);
+                const int up = parents[at_node];
                 if (in && (at_node == 0 ? up != -1 : up < 0 || up >= at_node))
                   atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
                 at_node = at_node == 0 || up >= at_node ? -1 : max(up, -1);
               }
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) see[k] &= mine[k];
+            see.x &= mine.x;
+            see.y &= mine.y;
           }
-          // the largest score
-          float top = TV_NEG_INF, top1 = TV_NEG_INF;
-          uint32_t c[32];
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) {
-            tmem_ld32(ts + 32 * k, c);
-            const uint32_t now = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
-            tmem_wait(c);
-            if (part) hide(c, now);
+          if (__any_sync(0xffffffffu, (see.x & see.y) != 0xffffffffu)) hide_scores(ts, see);
+          // the largest score of this half
+          float top2[2] = {TV_NEG_INF, TV_NEG_INF};
+          for_scores(ts, [&](int, const uint32_t (&c)[16]) {
 #pragma unroll
-            for (int y = 0; y < 32; y += 4) {
-              top = fmaxf(fmaxf(top, __uint_as_float(c[y])), __uint_as_float(c[y + 1]));
-              top1 = fmaxf(fmaxf(top1, __uint_as_float(c[y + 2])), __uint_as_float(c[y + 3]));
+            for (int y = 0; y < 16; y += 4) {
+              top2[0] = fmaxf(fmaxf(top2[0], __uint_as_float(c[y])), __uint_as_float(c[y + 1]));
+              top2[1] = fmaxf(fmaxf(top2[1], __uint_as_float(c[y + 2])),
+                              __uint_as_float(c[y + 3]));
             }
-          }
-          top = f * fmaxf(top, top1);
-          if (__any_sync(0xffffffffu, top > mref + kSlack)) {
+          });
+          // (lanes without a row hold scores of whatever was there, and have no say)
+          float top = in ? f * fmaxf(top2[0], top2[1]) : TV_NEG_INF;
+          // weights are relative to what the largest score was, until it has grown too far
+          if (pair_any(pair_id, top > mref + kSlack)) {
+            sh.top[x][half][r] = top;
+            named_barrier(pair_id, 64);
+            top = fmaxf(top, sh.top[x][half ^ 1][r]);
             float down = 1.f;
             if (top > mref) {
               down = ex2(mref - top);
@@ -533,36 +603,33 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
               wait_on(&sh.ofull[x], (count - 1) & 1, bad);
               tc_fence_after();
 #pragma unroll 1
-              for (int k = 0; k < D / 32; ++k) {
-                tmem_ld32(to + 32 * k, c);
+              for (int k = 0; k < D / 2; k += 32) {
+                uint32_t c[32];
+                tmem_ld32(to + k, c);
                 tmem_wait(c);
 #pragma unroll
                 for (int y = 0; y < 32; ++y) c[y] = __float_as_uint(__uint_as_float(c[y]) * down);
-                tmem_st32(to + 32 * k, c);
+                tmem_st32(to + k, c);
               }
             }
           }
           const float off = kLift - (mref == TV_NEG_INF ? 0.f : mref);
           const float2 ff = make_float2(f, f), oo = make_float2(off, off);
           float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll 1
-          for (int k = 0; k < 4; ++k) {
-            tmem_ld32(ts + 32 * k, c);
-            const uint32_t now = k == 0 ? see[0] : k == 1 ? see[1] : k == 2 ? see[2] : see[3];
-            tmem_wait(c);
-            if (part) hide(c, now);
-            uint32_t w[16];
+          uint32_t w[16];
+          for_scores(ts, [&](int k, const uint32_t (&c)[16]) {
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-              float2 e = __ffma2_rn(make_float2(__uint_as_float(c[y]), __uint_as_float(c[y + 1])), ff, oo);
+            for (int y = 0; y < 16; y += 2) {
+              float2 e = __ffma2_rn(
+                  make_float2(__uint_as_float(c[y]), __uint_as_float(c[y + 1])), ff, oo);
               e.x = ex2(e.x);
               e.y = ex2(e.y);
               acc[(y >> 1) & 1] = __fadd2_rn(acc[(y >> 1) & 1], e);
               const __half2 h = __floats2half2_rn(e.x, e.y);
-              w[y >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+              w[8 * (k & 1) + (y >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            tmem_st16(ts + 16 * k, w);
-          }
+            if (k & 1) tmem_st16(ts + 8 * (k - 1), w);
+          });
           acc[0] = __fadd2_rn(acc[0], acc[1]);
           l += acc[0].x + acc[0].y;
           tmem_stored();
@@ -575,79 +642,89 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       steps_done += (uint32_t)n;
 
       // the sums
-      const bool any = x < ops;
-      if (any) wait_on(&sh.ofull[x], (count - 1) & 1, bad);
+      if (x < ops) wait_on(&sh.ofull[x], (count - 1) & 1, bad);
       tc_fence_after();
+      sh.l[x][half][r] = x < ops ? l : 0.f;
       float fac[2] = {1.f, 0.f};
       if (split) {
-        sh.m[x][r] = any ? mref : TV_NEG_INF;
-        sh.l[x][r] = any ? l : 0.f;
-        softmax_barrier();
+        if (half == 0) sh.m[x][r] = x < ops ? mref : TV_NEG_INF;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.merge);
+        wait_on(&sh.merge, merged++ & 1, bad);
         const float m0 = sh.m[0][r], m1 = sh.m[1][r];
         mref = fmaxf(m0, m1);
         fac[0] = m0 == TV_NEG_INF ? 0.f : ex2(m0 - mref);
         fac[1] = m1 == TV_NEG_INF ? 0.f : ex2(m1 - mref);
-        l = sh.l[0][r] * fac[0] + sh.l[1][r] * fac[1];
+        l = (sh.l[0][0][r] + sh.l[0][1][r]) * fac[0] + (sh.l[1][0][r] + sh.l[1][1][r]) * fac[1];
+      } else {
+        named_barrier(pair_id, 64);
+        l = sh.l[x][0][r] + sh.l[x][1][r];
       }
-      const bool whole = p.whole();
-      const float inv = !whole ? 1.f
-                        : l == 0.f ? 0.f : pow2i(exponent_of(a.c, a.layer, 1, p.head)) / l;
-      const size_t slot = 2 * (size_t)blockIdx.x + (p.s0 == 0);
-      const int at_row = m - p.m0;
-      if (live) {
-        // (split: half of the columns each)
-        const int c0 = split ? x * (D / 64) : 0, c1 = split ? c0 + D / 64 : D / 32;
-        const uint32_t t0 = tmem + 2 * kTile + lanes;
-        for (int k = c0; k < c1; ++k) {
+      if (live && !(split && x == 1)) {          // (tile 0's threads read both tiles' sums)
+        const bool whole = p.whole();
+        const float inv = !whole ? 1.f
+                          : l == 0.f ? 0.f
+                                     : pow2i(exponent_of(a.c, a.layer, 1, p.head)) / l;
+        const size_t row = (2 * (size_t)blockIdx.x + (p.s0 == 0)) * 2 * kTile + (m - p.m0);
+        fac[0] *= inv;
+        fac[1] *= inv;
+#pragma unroll 1
+        for (int k = 0; k < D / 2; k += 32) {
+          const int col = half * (D / 2) + k;
           uint32_t c[32];
-          float y[32];
-          tmem_ld32((split ? t0 : to) + 32 * k, c);
+          tmem_ld32(to + k, c);
           tmem_wait(c);
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            y[i] = split && fac[0] == 0.f ? 0.f : __uint_as_float(c[i]) * fac[0];
+          for (int y = 0; y < 32; ++y)
+            c[y] = split && fac[0] == 0.f ? 0u : __float_as_uint(__uint_as_float(c[y]) * fac[0]);
           if (split && ops > 1) {
-            tmem_ld32(t0 + D + 32 * k, c);
-            tmem_wait(c);
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              y[i] += fac[1] == 0.f ? 0.f : __uint_as_float(c[i]) * fac[1];
+            for (int z = 0; z < 2; ++z) {
+              uint32_t d[16];
+              tmem_ld16(to + D + k + 16 * z, d);
+              tmem_wait16(d);
+#pragma unroll
+              for (int y = 0; y < 16; ++y)
+                c[16 * z + y] = __float_as_uint(
+                    __uint_as_float(c[16 * z + y]) +
+                    (fac[1] == 0.f ? 0.f : __uint_as_float(d[y]) * fac[1]));
+            }
           }
           if (whole) {
             uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i] * inv, y[2 * i + 1] * inv);
-              w[i] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int y = 0; y < 16; ++y) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(c[2 * y]),
+                                                             __uint_as_float(c[2 * y + 1]));
+              w[y] = *reinterpret_cast<const uint32_t*>(&h);
             }
             if (in) {
               __nv_bfloat16* const dst =
                   a.out + (((size_t)p.b * a.R + node) * a.c.kv_heads * a.group +
-                           (size_t)p.head * a.group + m % a.group) * D + 32 * k;
+                           (size_t)p.head * a.group + m % a.group) * D + col;
               if (wide) {
                 st_global_32b(dst, w);
                 st_global_32b(dst + 16, w + 8);
               } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  reinterpret_cast<uint4*>(dst)[i] =
-                      make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                for (int y = 0; y < 4; ++y)
+                  reinterpret_cast<uint4*>(dst)[y] =
+                      make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
               }
             }
-          } else {
-            float* const dst = a.part + (slot * 2 * kTile + at_row) * D + 32 * k;
+          } else if (in) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              st_global_32b(dst + i, reinterpret_cast<const uint32_t*>(y) + i);
+            for (int y = 0; y < 32; y += 8) st_global_32b(a.part + row * D + col + y, c + y);
           }
         }
-        if (!whole && !(split && x == 1)) {
-          stats_of(a, D, gridDim.x)[slot * 2 * kTile + at_row] = make_float2(mref, l);
-        }
+        if (!whole && half == 0 && in) stats_of(a, D, gridDim.x)[row] = make_float2(mref, l);
       }
       tc_fence_before();
-      give_back(sh, taken);
-      softmax_barrier();       // the next piece's queries and sums go where these were
+      if (split) {                               // both tiles' sums may be overwritten
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.merge);
+        wait_on(&sh.merge, merged++ & 1, bad);
+      }
     }
   }
   if (bad) atomicOr(a.status, (uint32_t)TV_STATUS_TIMEOUT);
