@@ -220,15 +220,17 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return y;
 }
 
-// Scales a row of queries whose largest magnitude is `top` by a power of two, to [2^14, 2^15).
+// Scales a row of queries whose largest magnitude is `top` by a power of two, to [2^14, 2^15)
+// (or, of subnormal ones, as near as the exponent of the least normal one brings it).
 struct QueryScale {
   float up0, up1;              // two factors (one power of two may be no float32)
   int e;
   bool finite;
   __device__ __forceinline__ explicit QueryScale(float top) {
     finite = top <= 3.4028234e38f;                 // (false for NaN)
-    e = finite && top > 0.f ? ilogbf(top) - 14 : 0;
-    const int half = -e / 2;                       // |e| <= 163
+    const int biased = max(__float_as_int(top) >> 23, 1);
+    e = finite && top > 0.f ? biased - (127 + 14) : 0;
+    const int half = -e / 2;                       // -140 <= e <= 113
     up0 = pow2i(half);
     up1 = pow2i(-e - half);
   }
@@ -236,7 +238,9 @@ struct QueryScale {
   // what makes log2(e) times the score of a product of scaled queries and keys; NaN for a
   // row that is not finite
   __device__ __forceinline__ float factor(float scale_log2e, int key_exponent) const {
-    return finite ? ldexpf(scale_log2e, e + key_exponent) : __int_as_float(0x7fffffff);
+    const int n = e + key_exponent, half = n / 2;
+    const float f = scale_log2e * pow2i(half) * pow2i(n - half);
+    return finite ? f : __int_as_float(0x7fffffff);
   }
 };
 

@@ -3,27 +3,29 @@
 // cores.  Mathematics, rounding and the cut into pieces are those of tv_attend.cu.
 //
 // One persistent CTA per SM, two tiles of 128 rows at a time:
-//   warps 0-7, 8-15   softmax of tile 0 and 1, half a row (64 of a step's tokens) per thread:
-//                     scores from tensor memory, weights back into it as fp16, over the
-//                     first half of the thread's own scores
-//   warps 16-19       widen 128 tokens' keys to fp16 in shared memory (a token per thread,
-//                     its codes loaded a step ahead), two stages
-//   warps 20-23       the same for values
-//   warp 24           the products: S = Q K^T (both from shared memory) and O += P V (P
-//                     from tensor memory), S and O of both tiles in tensor memory
-//   warp 25           the CTA's pieces, in a ring that the others read
-//   warps 26, 27      the next piece's queries to fp16 in shared memory as soon as the last
-//                     product that reads the present ones is done; at the end, zeros in the
-//                     rows behind the requests' last
+//   warps 0-3, 4-7    softmax of tile 0 and 1, one row per thread: a step's 128 scores from
+//                     tensor memory into registers, weights back into it as fp16, those of 64
+//                     tokens over the first half of their scores
+//   warps 8-11        widen 128 tokens' keys and values to fp16 in shared memory (a token per
+//                     thread, its codes loaded a step ahead), two stages
+//   warps 12, 13      the products of tile 0 and 1: S = Q K^T (both from shared memory) and
+//                     O += P V (P from tensor memory), S and O in tensor memory
+//   warp 14           the CTA's pieces, in a ring that the others read
+//   warp 15           zeros in the rows behind the requests' last
+// (registers that the others leave go to the softmax).  The softmax threads also bring their rows
+// of queries to shared memory: two warps beside them took 24 thousand clocks for 256 rows.
 // The two tiles take turns: while one's scores become weights, the tensor cores work on the
-// other.  Where an item has 128 rows or fewer both tiles are the same rows and take
+// other.  (A warp's products are issued little faster than they run, and each barrier that it
+// tests takes 100 clocks: with one warp for both tiles the tensor cores had half of the time
+// nothing to do.)  Where an item has 128 rows or fewer both tiles are the same rows and take
 // alternate steps, and their sums are joined at the end.
 // Steps go from the last tokens to the first, so that a row's path to the root is walked once,
 // and the tree's tokens, which rows see in part, come first.
 //
 // A product that overwrites a tile's scores is issued after the one that reads its weights,
-// by the same thread: the tensor cores take them in that order.  Every wait is bounded; one that
-// gives up raises the timeout status, and the loops go on to their end.
+// by the same thread and of the same shape: the tensor cores take them in that order (where
+// the head dimension is 64 their shapes differ, and the first waits for the second).  Every wait
+// is bounded; one that gives up raises the timeout status, and the loops go on to their end.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -41,16 +43,20 @@ namespace attend {
 using namespace gemm;
 
 constexpr int kTile = 128;
-constexpr int kHalfTile = 64;                    // tokens of a thread
-constexpr int kSoftmaxWarps = 16;
-constexpr int kWidenWarps = 8;                   // four for keys, four for values
+constexpr int kHalfTile = 64;                    // tokens whose weights are handed over at once
+constexpr int kSoftmaxWarps = 8;
+constexpr int kWidenWarps = 4;
 constexpr int kMmaWarp = kSoftmaxWarps + kWidenWarps;
-constexpr int kQueryWarps = 2;
-constexpr int kTileThreads = 32 * (kMmaWarp + 2 + kQueryWarps);
+constexpr int kPieceWarp = kMmaWarp + 2;
+constexpr int kTileThreads = 32 * (kPieceWarp + 2);
+// registers per thread after the split
+constexpr int kRegsSoftmax = 176, kRegsWiden = 88, kRegsOther = 72, kRegsLaunch = 128;
+static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kWidenWarps * kRegsWiden + 4 * kRegsOther) <=
+                  kTileThreads * kRegsLaunch,
+              "the warpgroups' registers fit what the block was launched with");
 constexpr int kStages = 2;
 constexpr int kOkSlots = 4;
 constexpr uint32_t kHalfBytes = kTile * 128;     // 64 columns (128 bytes) of a tile's rows
-constexpr int kJoinParts = 8;                    // blocks that join one item's rows
 
 // An item that begins in a CTA and goes on in later ones, up to `last`; b < 0: there is none.
 struct Split {
@@ -63,23 +69,32 @@ struct Work {
   __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == steps; }
 };
 constexpr int kWorkSlots = 4;
-constexpr int kTakers = kSoftmaxWarps + kWidenWarps + 1 + kQueryWarps;
+constexpr int kTakers = 2 + kWidenWarps + 2;       // (of the softmax one of each tile)
 
 struct TileShared {
   uint64_t given[kWorkSlots], taken[kWorkSlots];
   Work work[kWorkSlots];
-  int more[2][2];                                // [piece % 2][tile]
+  Work now[2][2];                                // [tile][piece % 2], the softmax's
   uint64_t kfull[kStages], kempty[kStages], vfull[kStages], vempty[kStages];
-  uint64_t sfull[2], pfull[2], ofull[2], qfull, qempty, merge;
+  uint64_t sfull[2], pfull[2][2], ofull[2];      // pfull: [tile][half of the tokens]
+  uint64_t qfull[2], merge;
   uint32_t tmem;
   // tokens of a step that exist and have a page; a slot is used again four steps later, when
   // both softmaxes are done with it
   alignas(16) uint32_t ok[kOkSlots][4];
-  float factor[2][2 * kTile];                    // [piece % 2], of a row's scores
-  float top[2][2][kTile], l[2][2][kTile], m[2][kTile];
+  float m[2][kTile], l[2][kTile];
   Schedule plan;
-  int32_t parents[2][1024];                      // [piece % 2]
+  int32_t parents[2][1024];                      // [tile]
 };
+
+template <int kRegs>
+__device__ __forceinline__ void regs_fewer() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
+template <int kRegs>
+__device__ __forceinline__ void regs_more() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
+}
 
 __device__ __forceinline__ void wait_on(uint64_t* bar, uint32_t parity, uint32_t& bad) {
   if (!mbar_try_wait(bar, parity) && !bad) bad = mbar_wait(bar, parity) ? 0u : 1u;
@@ -180,17 +195,6 @@ __device__ __forceinline__ void async_visible() {      // shared memory written,
 __device__ __forceinline__ void named_barrier(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
-// Whether any of the 64 threads that share 32 rows says so.
-__device__ __forceinline__ bool pair_any(int id, bool say) {
-  uint32_t any;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
-      "bar.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"((uint32_t)say), "r"(id)
-      : "memory");
-  return any != 0;
-}
 __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint32_t c,
                                        uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c),
@@ -209,8 +213,8 @@ struct Token {
   uint4 code[D / 32];
   uint32_t scale[D / 32];
   bool there;
-  __device__ __forceinline__ void load(const AttendArgs& a, const Work& p, int pos, int side) {
-    const int page = pos < p.tokens ? page_of(a.c, a.t, p.b, pos) : -1;
+  __device__ __forceinline__ void load(const AttendArgs& a, const Work& p, int page, int pos,
+                                       int side) {
     there = page >= 0;
     if (there) {
       const uint8_t* const block = block_of(a.c, a.layer, page, p.head, side);
@@ -247,40 +251,31 @@ struct Token {
   }
 };
 
-// A thread's 64 scores, 16 at a time with the next on their way.  (Not a loop: registers that a
-// load is still to fill must not be moved, as they may be from one turn to the next.)
-template <typename F>
-__device__ __forceinline__ void for_scores(uint32_t ts, F use) {
-  uint32_t c[2][16];
-  tmem_ld16(ts, c[0]);
-#pragma unroll
-  for (int k = 0; k < kHalfTile / 16; ++k) {
-    uint32_t(&x)[16] = c[k & 1];
-    tmem_wait16(x);
-    if (k + 1 < kHalfTile / 16) tmem_ld16(ts + 16 * (k + 1), c[(k + 1) & 1]);
-    use(k, x);
-  }
+// The lowest n of 64 bits.
+__device__ __forceinline__ unsigned long long low_bits64(int n) {
+  return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull;
 }
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
 // Scores that a row does not see become -inf in tensor memory; a set bit in `see` is seen.
-__device__ __noinline__ void hide_scores(uint32_t ts, uint2 see) {
+__device__ __noinline__ void hide_scores(uint32_t ts, uint4 see) {
 #pragma unroll 1
-  for (int k = 0; k < kHalfTile; k += 16) {
+  for (int k = 0; k < kTile; k += 16) {
     uint32_t c[16];
     tmem_ld16(ts + k, c);
     tmem_wait16(c);
-    const uint32_t bits = (k < 32 ? see.x : see.y) >> (k & 16);
+    const uint32_t word = k < 64 ? (k < 32 ? see.x : see.y) : (k < 96 ? see.z : see.w);
+    const uint32_t bits = word >> (k & 16);
 #pragma unroll
     for (int y = 0; y < 16; ++y)
       if (!(bits >> y & 1)) c[y] = 0xff800000u;
     tmem_st16(ts + k, c);
   }
-  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-
-// The lowest n bits of a word that holds bits [at, at + 32).
-__device__ __forceinline__ uint32_t low_bits(int n, int at) {
-  const int k = n - at;
-  return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+  tmem_stored();
 }
 
 // The scratch: two pieces of every CTA, their rows' (maximum, sum), the CTAs' split items.
@@ -306,17 +301,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) {
       mbar_init(&sh.kfull[i], 4);
-      mbar_init(&sh.kempty[i], 1);
+      mbar_init(&sh.kempty[i], split ? 1 : 2);
       mbar_init(&sh.vfull[i], 4);
-      mbar_init(&sh.vempty[i], 1);
+      mbar_init(&sh.vempty[i], split ? 1 : 2);
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sh.sfull[x], 1);
-      mbar_init(&sh.pfull[x], kSoftmaxWarps / 2);
+      for (int i = 0; i < 2; ++i) mbar_init(&sh.pfull[x][i], kSoftmaxWarps / 2);
       mbar_init(&sh.ofull[x], 1);
+      mbar_init(&sh.qfull[x], split ? kSoftmaxWarps : kSoftmaxWarps / 2);
     }
-    mbar_init(&sh.qfull, kQueryWarps);
-    mbar_init(&sh.qempty, 1 + kSoftmaxWarps);
     mbar_init(&sh.merge, kSoftmaxWarps);
     for (int i = 0; i < kWorkSlots; ++i) {
       mbar_init(&sh.given[i], 1);
@@ -333,86 +327,62 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   const uint32_t tmem = sh.tmem;
   uint32_t bad = 0, taken = 0;                   // pieces so far
 
-  if (warp == kMmaWarp) {
+  if (warp >= kMmaWarp) regs_fewer<kRegsOther>();
+  if (warp >= kMmaWarp && warp < kPieceWarp) {
     // ---- products ----
-    const uint32_t qd0 = row_desc(q_tiles), qd1 = row_desc(q_tiles + (split ? 0 : kTileBytes));
+    const int x = warp - kMmaWarp;
+    const uint32_t qd = row_desc(q_tiles + (split ? 0 : x * kTileBytes));
     const uint32_t kd = row_desc(k_tiles), vd = column_desc(v_tiles);
-    uint32_t steps_done = 0, pcount[2] = {0, 0};
+    const uint32_t ts = tmem + x * kTile, to = tmem + 2 * kTile + x * D;
+    uint32_t steps_done = 0, count = 0;          // count: weights of this tile taken
     for (; const Work* const w = take(sh, taken, bad); ++taken) {
-      const int n = w->s1 - w->s0, ops = split ? n : 2 * n;
+      const int n = w->s1 - w->s0, stride = split ? 2 : 1, first = split ? x : 0;
       give_back(sh, taken);
-      auto step_of = [&](int i) { return steps_done + (uint32_t)(split ? i : i >> 1); };
-      auto wait_keys = [&](int i, int x) {
-        const uint32_t s = step_of(i);
-        if (split || x == 0) wait_on(&sh.kfull[s % kStages], (s / kStages) & 1, bad);
-      };
-      auto wait_weights = [&](int i, int x) {
-        const uint32_t s = step_of(i);
-        if (split || x == 0) wait_on(&sh.vfull[s % kStages], (s / kStages) & 1, bad);
-        wait_on(&sh.pfull[x], pcount[x] & 1, bad);
-        ++pcount[x];
+      auto scores = [&](int j) {
+        const uint32_t s = steps_done + (uint32_t)j, stage = s % kStages;
+        wait_on(&sh.kfull[stage], (s / kStages) & 1, bad);
         tc_fence_after();
-      };
-      auto scores = [&](int i, int x) {
-        const uint32_t stage = step_of(i) % kStages;
         if (elect_one()) {
-          const uint32_t q = x ? qd1 : qd0, k0 = kd + stage * (kTileBytes >> 4);
+          const uint32_t k0 = kd + stage * (kTileBytes >> 4);
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint32_t off = (uint32_t)((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-            mma_ss(tmem + x * kTile, q + off, k0 + off, f16_desc(kTile, kTile, false), k > 0);
+            mma_ss(ts, qd + off, k0 + off, f16_desc(kTile, kTile, false), k > 0);
           }
           umma_commit<false>(&sh.sfull[x]);
-          if (split || x == 1) umma_commit<false>(&sh.kempty[stage]);
-          if (i == ops - 1) umma_commit<false>(&sh.qempty);
+          umma_commit<false>(&sh.kempty[stage]);
         }
         __syncwarp();
       };
-      auto values = [&](int i, int x) {
-        const uint32_t stage = step_of(i) % kStages;
-        if (elect_one()) {
-          const uint32_t v0 = vd + stage * (kTileBytes >> 4);
+      wait_on(&sh.qfull[split ? 0 : x], taken & 1, bad);
+      if (first < n) scores(first);
+      for (int j = first; j < n; j += stride, ++count) {
+        const uint32_t s = steps_done + (uint32_t)j, stage = s % kStages;
+        wait_on(&sh.vfull[stage], (s / kStages) & 1, bad);
 #pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            mma_ts(tmem + 2 * kTile + x * D,
-                   tmem + x * kTile + (k >> 2) * kHalfTile + (k & 3) * 8, v0 + k * (2048u >> 4),
-                   f16_desc(kTile, D, true), i >= 2 || k > 0);
-          umma_commit<false>(&sh.ofull[x]);
-          if (split || x == 1) umma_commit<false>(&sh.vempty[stage]);
-        }
-        __syncwarp();
-      };
-      // (where the tiles share a step its keys are there long before; where they do not they may
-      // come later than the weights)
-      auto turn = [&](int i, int x) {
-        const bool next = i + 2 < ops;
-        if (next && !split) wait_keys(i + 2, x);
-        wait_weights(i, x);
-        values(i, x);
-        if (next) {
-          if (split) {
-            wait_keys(i + 2, x);
-            tc_fence_after();
+        for (int half = 0; half < 2; ++half) {
+          wait_on(&sh.pfull[x][half], count & 1, bad);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t v0 =
+                vd + stage * (kTileBytes >> 4) + half * ((kHalfTile * 128u) >> 4);
+#pragma unroll
+            for (int k = 0; k < kHalfTile / 16; ++k)
+              mma_ts(to, ts + half * kHalfTile + k * 8, v0 + k * (2048u >> 4),
+                     f16_desc(kTile, D, true), j > first || half > 0 || k > 0);
+            if (half) {
+              umma_commit<false>(&sh.ofull[x]);
+              umma_commit<false>(&sh.vempty[stage]);
+            }
           }
-          scores(i + 2, x);
+          __syncwarp();
         }
-      };
-      wait_on(&sh.qfull, taken & 1, bad);
-      wait_keys(0, 0);
-      tc_fence_after();
-      scores(0, 0);
-      if (ops > 1) {
-        wait_keys(1, 1);
-        tc_fence_after();
-        scores(1, 1);
-      }
-      for (int i = 0; i < ops; i += 2) {
-        turn(i, 0);
-        if (i + 1 < ops) turn(i + 1, 1);
+        if (D != kTile) wait_on(&sh.ofull[x], count & 1, bad);
+        if (j + stride < n) scores(j + stride);
       }
       steps_done += (uint32_t)n;
     }
-  } else if (warp == kMmaWarp + 1) {
+  } else if (warp == kPieceWarp) {
     // ---- pieces ----
     if (lane == 0) {
       Piece p;
@@ -431,168 +401,185 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       }
       splits_of(a, D, gridDim.x)[blockIdx.x] = split_item;
     }
-  } else if (warp > kMmaWarp + 1) {
-    // ---- queries: a row by D / 8 lanes, 8 columns each ----
-    constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAhead = 4;
-    const int me = warp - (kMmaWarp + 2), col = lane % kLanes;
-    for (; const Work* const w = take(sh, taken, bad); ++taken) {
-      const Work p = *w;
-      give_back(sh, taken);
-      const int M = p.rows * a.group;
-      const int key_exponent = exponent_of(a.c, a.layer, 0, p.head);
-      wait_on(&sh.qempty, (taken & 1) ^ 1, bad);
-      if (a.parents && p.s1 * kStep > p.len)
-        for (int i = lane + 32 * me; i < p.rows; i += 32 * kQueryWarps)
-          sh.parents[taken & 1][i] = a.parents[(size_t)p.b * a.R + i];
-      // (rows behind the last stay as they are: nothing of theirs is stored)
-      const int rows = min(rows_of_item, M - p.m0);
-      for (int r0 = me * kRows; r0 < rows; r0 += kQueryWarps * kRows * kAhead) {
-        uint4 w4[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int r = min(r0 + k * kQueryWarps * kRows + lane / kLanes, rows - 1), m = p.m0 + r;
-          w4[k] = __ldg(reinterpret_cast<const uint4*>(
-                            a.q + (((size_t)p.b * a.R + m / a.group) * a.c.kv_heads * a.group +
-                                   (size_t)p.head * a.group + m % a.group) * D) + col);
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int r = min(r0 + k * kQueryWarps * kRows + lane / kLanes, rows - 1);
-          const uint32_t u[4] = {w4[k].x, w4[k].y, w4[k].z, w4[k].w};
-          float top = 0.f;
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            top = max_nan(top, max_nan(fabsf(bf16_lo(u[y])), fabsf(bf16_hi(u[y]))));
-#pragma unroll
-          for (int d = kLanes / 2; d > 0; d >>= 1)
-            top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, d));
-          const QueryScale s(top);
-          float f = s.factor(a.scale_log2e, key_exponent);
-          const float sign = f < 0.f ? -1.f : 1.f;         // the factor is made positive,
-          f = fabsf(f);
-          if (f < 1e-37f) f = 1e-37f;                      // and keeps -inf what it is
-          uint32_t h[4];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const __half2 z = __floats2half2_rn(sign * s.apply(bf16_lo(u[y])),
-                                                sign * s.apply(bf16_hi(u[y])));
-            h[y] = *reinterpret_cast<const uint32_t*>(&z);
-          }
-          sts128(piece_at(smem_u32(q_tiles) + (uint32_t)(r >> 7) * kTileBytes, r & (kTile - 1),
-                          col),
-                 h[0], h[1], h[2], h[3]);
-          if (col == 0) sh.factor[taken & 1][r] = f;
-        }
-      }
-      async_visible();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.qfull);
-    }
-    zero_rows(a, D, (int)blockIdx.x * kQueryWarps + me, (int)gridDim.x * kQueryWarps);
+  } else if (warp > kPieceWarp) {
+    zero_rows(a, D, (int)blockIdx.x, (int)gridDim.x);
   } else if (warp >= kSoftmaxWarps) {
     // ---- keys and values to fp16 ----
-    const int side = warp >= kSoftmaxWarps + 4, row = tid & (kTile - 1);
-    uint64_t* const full = side ? sh.vfull : sh.kfull;
-    uint64_t* const empty = side ? sh.vempty : sh.kempty;
-    const uint32_t base = smem_u32(side ? v_tiles : k_tiles);
+    regs_fewer<kRegsWiden>();
+    const int row = tid & (kTile - 1);
+    const uint32_t k0 = smem_u32(k_tiles), v0 = smem_u32(v_tiles);
     uint32_t s = 0;
     for (; const Work* const w = take(sh, taken, bad); ++taken) {
       const Work p = *w;
       give_back(sh, taken);
-      Token<D> next;
-      next.load(a, p, (p.s1 - 1) * kStep + row, side);
+      auto page_at = [&](int step) {
+        const int pos = step * kStep + row;
+        return step >= p.s0 && pos < p.tokens ? page_of(a.c, a.t, p.b, pos) : -1;
+      };
+      int page = page_at(p.s1 - 1), page_next = page_at(p.s1 - 2);
+      Token<D> key, value;
+      key.load(a, p, page, (p.s1 - 1) * kStep + row, 0);
+      value.load(a, p, page, (p.s1 - 1) * kStep + row, 1);
       for (int step = p.s1 - 1; step >= p.s0; --step, ++s) {
-        const Token<D> now = next;
-        if (step > p.s0) next.load(a, p, (step - 1) * kStep + row, side);
-        const uint32_t stage = s % kStages;
-        wait_on(&empty[stage], ((s / kStages) & 1) ^ 1, bad);
-        now.widen_to(base + stage * kTileBytes, row);
-        if (!side) {
-          const uint32_t word = __ballot_sync(0xffffffffu, now.there);
-          if (lane == 0) sh.ok[s % kOkSlots][warp & 3] = word;
-          if (!now.there && step * kStep + row < p.tokens)
-            atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
-        }
+        const uint32_t stage = s % kStages, parity = ((s / kStages) & 1) ^ 1;
+        const bool there = page >= 0;
+        page = page_next;
+        page_next = page_at(step - 2);
+        wait_on(&sh.kempty[stage], parity, bad);
+        key.widen_to(k0 + stage * kTileBytes, row);
+        const uint32_t word = __ballot_sync(0xffffffffu, there);
+        if (lane == 0) sh.ok[s % kOkSlots][warp & 3] = word;
         async_visible();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full[stage]);
+        if (lane == 0) mbar_arrive(&sh.kfull[stage]);
+        key.load(a, p, page, (step - 1) * kStep + row, 0);
+        if (!there && step * kStep + row < p.tokens)
+          atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+        wait_on(&sh.vempty[stage], parity, bad);
+        value.widen_to(v0 + stage * kTileBytes, row);
+        async_visible();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.vfull[stage]);
+        value.load(a, p, page, (step - 1) * kStep + row, 1);
       }
     }
   } else {
     // ---- softmax ----
-    const int x = warp >> 3, half = warp >> 2 & 1, r = (warp & 3) * 32 + lane;
-    const int tile_id = 1 + x, pair_id = 4 + 4 * x + (warp & 3);         // barriers
+    regs_more<kRegsSoftmax>();
+    const int x = warp >> 2, r = tid & (kTile - 1);
     const uint32_t lanes = (uint32_t)(warp & 3) * 32u << 16;
-    const uint32_t ts = tmem + x * kTile + half * kHalfTile + lanes;
-    const uint32_t to = tmem + 2 * kTile + x * D + half * (D / 2) + lanes;
+    const uint32_t ts = tmem + x * kTile + lanes, to = tmem + 2 * kTile + x * D + lanes;
     uint32_t steps_done = 0, count = 0, merged = 0;        // count: scores of this tile taken
-    for (;; ++taken) {
-      if ((warp & 7) == 0) {                     // (a tile's warps meet at barriers)
+    // the next piece; false: there is none.  (A tile's warps meet at barriers, so one of them
+    // says it for all.)
+    auto take_next = [&]() -> bool {
+      Work& w = sh.now[x][taken & 1];
+      if ((warp & 3) == 0) {
         const bool more = take(sh, taken, bad) != nullptr;
-        if (lane == 0) sh.more[taken & 1][x] = more;
+        if (lane == 0) {
+          w = sh.work[taken % kWorkSlots];
+          w.more = more;
+        }
+        give_back(sh, taken);
       }
-      named_barrier(tile_id, 16 * kSoftmaxWarps);
-      if (!sh.more[taken & 1][x]) break;
-      const Work p = sh.work[taken % kWorkSlots];
-      give_back(sh, taken);
-      const int len = p.len, M = p.rows * a.group;
+      named_barrier(1 + x, 16 * kSoftmaxWarps);
+      ++taken;
+      return w.more;
+    };
+    // this thread's row of queries
+    uint4 q[D / 8];
+    auto load_queries = [&]() {
+      const Work& next = sh.now[x][(taken - 1) & 1];
+      const int m = min(next.m0 + (split ? 0 : x * kTile) + r, next.rows * a.group - 1);
+      const int i = m / a.group;
+      const uint4* const src = reinterpret_cast<const uint4*>(
+          a.q + (((size_t)next.b * a.R + i) * a.c.kv_heads * a.group +
+                 (size_t)next.head * a.group + (m - i * a.group)) * D);
+#pragma unroll
+      for (int k = 0; k < D / 8; ++k) q[k] = __ldg(src + k);
+    };
+    bool more = take_next();
+    if (more) load_queries();
+    while (more) {
+      const Work& p = sh.now[x][(taken - 1) & 1];
+      const int len = p.len, M = p.rows * a.group, top_step = p.s1 - 1;
       const int m = p.m0 + (split ? 0 : x * kTile) + r;
       const bool in = m < M;
       const int node = in ? m / a.group : 0;
       const bool live = __any_sync(0xffffffffu, in);
-      const int32_t* const parents = sh.parents[taken & 1];
-      wait_on(&sh.qfull, taken & 1, bad);
-      const float f = in ? sh.factor[taken & 1][(split ? 0 : x * kTile) + r] : 1e-37f;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sh.qempty);
+      const int32_t* const parents = sh.parents[x];
+      if (a.parents && p.s1 * kStep > len)
+        for (int i = r; i < p.rows; i += kTile)
+          sh.parents[x][i] = a.parents[(size_t)p.b * a.R + i];
+      float f;
+      {
+        uint32_t top2 = 0;                       // largest magnitudes of two columns, in bf16
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k)
+          top2 = max_nan_bf16x2(max_nan_bf16x2(top2, q[k].x & 0x7fff7fffu),
+                                max_nan_bf16x2(q[k].y & 0x7fff7fffu,
+                                               max_nan_bf16x2(q[k].z & 0x7fff7fffu,
+                                                              q[k].w & 0x7fff7fffu)));
+        const QueryScale s(max_nan(bf16_lo(top2), bf16_hi(top2)));
+        f = s.factor(a.scale_log2e, exponent_of(a.c, a.layer, 0, p.head));
+        const float up0 = f < 0.f ? -s.up0 : s.up0;        // the factor is made positive,
+        f = fabsf(f);
+        if (f < 1e-37f || !in) f = 1e-37f;                 // and keeps -inf what it is
+        const uint32_t q_at = smem_u32(q_tiles) + (split ? 0u : (uint32_t)x * kTileBytes);
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) {
+          if (split && k / (D / 16) != x) continue;        // (half of a row's columns each)
+          const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+          uint32_t h[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const __half2 z = __floats2half2_rn(bf16_lo(u[y]) * up0 * s.up1,
+                                                bf16_hi(u[y]) * up0 * s.up1);
+            h[y] = *reinterpret_cast<const uint32_t*>(&z);
+          }
+          sts128(piece_at(q_at, r, k), h[0], h[1], h[2], h[3]);
+        }
+      }
+      async_visible();
+      named_barrier(1 + x, 16 * kSoftmaxWarps);            // (the parents are there, too)
+      if (lane == 0) mbar_arrive(&sh.qfull[split ? 0 : x]);
 
       float mref = TV_NEG_INF, l = 0.f;
       int at_node = node;                                  // the path's next node, -1: done
       const int n = p.s1 - p.s0, ops = split ? n : 2 * n;
-      for (int i = x; i < ops; i += 2) {
+      for (int i = x; i < ops; i += 2, ++count) {
         const int j = split ? i : i >> 1;
-        const int pos = (p.s1 - 1 - j) * kStep;
+        const int pos = (top_step - j) * kStep;
         wait_on(&sh.sfull[x], count & 1, bad);
         tc_fence_after();
         if (live) {
-          uint2 see = *reinterpret_cast<const uint2*>(
-              &sh.ok[(steps_done + (uint32_t)j) % kOkSlots][2 * half]);
+          uint4 see = *reinterpret_cast<const uint4*>(
+              sh.ok[(steps_done + (uint32_t)j) % kOkSlots]);
           if (pos + kStep > len) {                         // some tokens are the tree's
-            const int from = pos + half * kHalfTile;
-            const int upto = len - from + (a.parents ? 0 : node + 1);
-            uint2 mine = make_uint2(low_bits(upto, 0), low_bits(upto, 32));
+            const int upto = len - pos + (a.parents ? 0 : node + 1);
+            unsigned long long lower = low_bits64(upto), upper = low_bits64(upto - 64);
             if (a.parents) {
               while (at_node >= 0 && len + at_node >= pos) {
-                const int bit = len + at_node - from;
-                if (bit >= 0 && bit < 32) mine.x |= 1u << bit;
-                if (bit >= 32 && bit < 64) mine.y |= 1u << (bit - 32);
+                const int bit = len + at_node - pos;
+                const unsigned long long on = 1ull << (bit & 63);
+                if (bit < 64)
+                  lower |= on;
+                else if (bit < 128)
+                  upper |= on;
                 const int up = parents[at_node];
                 if (in && (at_node == 0 ? up != -1 : up < 0 || up >= at_node))
                   atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
                 at_node = at_node == 0 || up >= at_node ? -1 : max(up, -1);
               }
             }
-            see.x &= mine.x;
-            see.y &= mine.y;
+            see.x &= (uint32_t)lower;
+            see.y &= (uint32_t)(lower >> 32);
+            see.z &= (uint32_t)upper;
+            see.w &= (uint32_t)(upper >> 32);
           }
-          if (__any_sync(0xffffffffu, (see.x & see.y) != 0xffffffffu)) hide_scores(ts, see);
-          // the largest score of this half
-          float top2[2] = {TV_NEG_INF, TV_NEG_INF};
-          for_scores(ts, [&](int, const uint32_t (&c)[16]) {
+          if (__any_sync(0xffffffffu, (see.x & see.y & see.z & see.w) != 0xffffffffu))
+            hide_scores(ts, see);
+          // the largest score, of the second half first: the first half's stay in registers
+          uint32_t c[2][32];
+          float top4[4] = {TV_NEG_INF, TV_NEG_INF, TV_NEG_INF, TV_NEG_INF};
 #pragma unroll
-            for (int y = 0; y < 16; y += 4) {
-              top2[0] = fmaxf(fmaxf(top2[0], __uint_as_float(c[y])), __uint_as_float(c[y + 1]));
-              top2[1] = fmaxf(fmaxf(top2[1], __uint_as_float(c[y + 2])),
-                              __uint_as_float(c[y + 3]));
+          for (int half = 1; half >= 0; --half) {
+            tmem_ld32(ts + kHalfTile * half, c[0]);
+            tmem_ld32(ts + kHalfTile * half + 32, c[1]);
+            tmem_wait(c[0]);
+            tmem_wait(c[1]);
+#pragma unroll
+            for (int y = 0; y < 64; y += 2) {
+              float& t = top4[(y >> 1) & 3];
+              t = fmaxf(fmaxf(t, __uint_as_float(c[y >> 5][y & 31])),
+                        __uint_as_float(c[y >> 5][(y & 31) + 1]));
             }
-          });
+          }
           // (lanes without a row hold scores of whatever was there, and have no say)
-          float top = in ? f * fmaxf(top2[0], top2[1]) : TV_NEG_INF;
+          const float top = in ? f * fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]))
+                               : TV_NEG_INF;
           // weights are relative to what the largest score was, until it has grown too far
-          if (pair_any(pair_id, top > mref + kSlack)) {
-            sh.top[x][half][r] = top;
-            named_barrier(pair_id, 64);
-            top = fmaxf(top, sh.top[x][half ^ 1][r]);
+          if (__any_sync(0xffffffffu, top > mref + kSlack)) {
             float down = 1.f;
             if (top > mref) {
               down = ex2(mref - top);
@@ -603,51 +590,65 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
               wait_on(&sh.ofull[x], (count - 1) & 1, bad);
               tc_fence_after();
 #pragma unroll 1
-              for (int k = 0; k < D / 2; k += 32) {
-                uint32_t c[32];
-                tmem_ld32(to + k, c);
-                tmem_wait(c);
+              for (int k = 0; k < D; k += 16) {
+                uint32_t d[16];
+                tmem_ld16(to + k, d);
+                tmem_wait16(d);
 #pragma unroll
-                for (int y = 0; y < 32; ++y) c[y] = __float_as_uint(__uint_as_float(c[y]) * down);
-                tmem_st32(to + k, c);
+                for (int y = 0; y < 16; ++y) d[y] = __float_as_uint(__uint_as_float(d[y]) * down);
+                tmem_st16(to + k, d);
               }
             }
           }
           const float off = kLift - (mref == TV_NEG_INF ? 0.f : mref);
           const float2 ff = make_float2(f, f), oo = make_float2(off, off);
           float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          uint32_t w[16];
-          for_scores(ts, [&](int k, const uint32_t (&c)[16]) {
 #pragma unroll
-            for (int y = 0; y < 16; y += 2) {
-              float2 e = __ffma2_rn(
-                  make_float2(__uint_as_float(c[y]), __uint_as_float(c[y + 1])), ff, oo);
+          for (int half = 0; half < 2; ++half) {
+            if (half) {
+              tmem_ld32(ts + kHalfTile, c[0]);
+              tmem_ld32(ts + kHalfTile + 32, c[1]);
+              tmem_wait(c[0]);
+              tmem_wait(c[1]);
+            }
+            uint32_t w[32];
+#pragma unroll
+            for (int y = 0; y < 64; y += 2) {
+              const uint32_t(&z)[32] = c[y >> 5];
+              float2 e = __ffma2_rn(make_float2(__uint_as_float(z[y & 31]),
+                                                __uint_as_float(z[(y & 31) + 1])),
+                                    ff, oo);
               e.x = ex2(e.x);
               e.y = ex2(e.y);
               acc[(y >> 1) & 1] = __fadd2_rn(acc[(y >> 1) & 1], e);
               const __half2 h = __floats2half2_rn(e.x, e.y);
-              w[8 * (k & 1) + (y >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
+              w[y >> 1] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            if (k & 1) tmem_st16(ts + 8 * (k - 1), w);
-          });
+            tmem_st32(ts + kHalfTile * half, w);
+            tmem_stored();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.pfull[x][half]);
+          }
           acc[0] = __fadd2_rn(acc[0], acc[1]);
           l += acc[0].x + acc[0].y;
-          tmem_stored();
+        } else if (lane == 0) {
+          mbar_arrive(&sh.pfull[x][0]);
+          mbar_arrive(&sh.pfull[x][1]);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.pfull[x]);
-        ++count;
       }
       steps_done += (uint32_t)n;
+      // (the next queries on their way while the sums are stored)
+      more = take_next();
+      if (more) load_queries();
 
       // the sums
       if (x < ops) wait_on(&sh.ofull[x], (count - 1) & 1, bad);
       tc_fence_after();
-      sh.l[x][half][r] = x < ops ? l : 0.f;
       float fac[2] = {1.f, 0.f};
       if (split) {
-        if (half == 0) sh.m[x][r] = x < ops ? mref : TV_NEG_INF;
+        sh.m[x][r] = x < ops ? mref : TV_NEG_INF;
+        sh.l[x][r] = x < ops ? l : 0.f;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.merge);
         wait_on(&sh.merge, merged++ & 1, bad);
@@ -655,12 +656,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         mref = fmaxf(m0, m1);
         fac[0] = m0 == TV_NEG_INF ? 0.f : ex2(m0 - mref);
         fac[1] = m1 == TV_NEG_INF ? 0.f : ex2(m1 - mref);
-        l = (sh.l[0][0][r] + sh.l[0][1][r]) * fac[0] + (sh.l[1][0][r] + sh.l[1][1][r]) * fac[1];
-      } else {
-        named_barrier(pair_id, 64);
-        l = sh.l[x][0][r] + sh.l[x][1][r];
+        l = sh.l[0][r] * fac[0] + sh.l[1][r] * fac[1];
       }
-      if (live && !(split && x == 1)) {          // (tile 0's threads read both tiles' sums)
+      if (live) {
         const bool whole = p.whole();
         const float inv = !whole ? 1.f
                           : l == 0.f ? 0.f
@@ -668,26 +666,27 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         const size_t row = (2 * (size_t)blockIdx.x + (p.s0 == 0)) * 2 * kTile + (m - p.m0);
         fac[0] *= inv;
         fac[1] *= inv;
+        // (split: of both tiles' sums half of the columns each)
+        const int c0 = split ? x * (D / 2) : 0, c1 = split ? c0 + D / 2 : D;
+        const uint32_t t0 = split ? tmem + 2 * kTile + lanes : to;
 #pragma unroll 1
-        for (int k = 0; k < D / 2; k += 32) {
-          const int col = half * (D / 2) + k;
+        for (int col = c0; col < c1; col += 32) {
           uint32_t c[32];
-          tmem_ld32(to + k, c);
+          tmem_ld32(t0 + col, c);
           tmem_wait(c);
 #pragma unroll
           for (int y = 0; y < 32; ++y)
             c[y] = split && fac[0] == 0.f ? 0u : __float_as_uint(__uint_as_float(c[y]) * fac[0]);
           if (split && ops > 1) {
 #pragma unroll
-            for (int z = 0; z < 2; ++z) {
+            for (int z = 0; z < 32; z += 16) {
               uint32_t d[16];
-              tmem_ld16(to + D + k + 16 * z, d);
+              tmem_ld16(t0 + D + col + z, d);
               tmem_wait16(d);
 #pragma unroll
               for (int y = 0; y < 16; ++y)
-                c[16 * z + y] = __float_as_uint(
-                    __uint_as_float(c[16 * z + y]) +
-                    (fac[1] == 0.f ? 0.f : __uint_as_float(d[y]) * fac[1]));
+                c[z + y] = __float_as_uint(__uint_as_float(c[z + y]) +
+                                           (fac[1] == 0.f ? 0.f : __uint_as_float(d[y]) * fac[1]));
             }
           }
           if (whole) {
@@ -717,7 +716,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             for (int y = 0; y < 32; y += 8) st_global_32b(a.part + row * D + col + y, c + y);
           }
         }
-        if (!whole && half == 0 && in) stats_of(a, D, gridDim.x)[row] = make_float2(mref, l);
+        if (!whole && !(split && x == 1) && in)
+          stats_of(a, D, gridDim.x)[row] = make_float2(mref, l);
       }
       tc_fence_before();
       if (split) {                               // both tiles' sums may be overwritten
@@ -736,37 +736,64 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   }
 }
 
-// Joins the pieces of an item that spans CTAs: block c * kJoinParts + part takes a part of
-// the rows of the item that begins in CTA c and goes on in later ones.
+// Joins the pieces of an item that spans CTAs: block c * parts + part takes a part of the rows of
+// the item that begins in CTA c and goes on in later ones.  Its factors first, for all rows and
+// pieces at once, and then the sums with several pieces' loads on their way.
+constexpr int kJoinRows = 16;
+
 template <int D>
 __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int split, int ctas) {
+  extern __shared__ float join_fac[];                    // [pieces][kJoinRows]
+  __shared__ float inv[kJoinRows];
   asm volatile("griddepcontrol.wait;" ::: "memory");     // (launched before the pieces are there)
-  const int c0 = blockIdx.x / kJoinParts, part = blockIdx.x % kJoinParts;
+  const int parts = (split ? kTile : 2 * kTile) / kJoinRows;
+  const int c0 = blockIdx.x / parts, r0 = blockIdx.x % parts * kJoinRows, tid = threadIdx.x;
   const Split item = splits_of(a, D, ctas)[c0];
   if (item.b < 0) return;
-  const int M = request_of(a, item.b).rows * a.group;
-  const float up = pow2i(exponent_of(a.c, a.layer, 1, item.head));
-  const int rows = (split ? kTile : 2 * kTile) / kJoinParts;
+  const int M = request_of(a, item.b).rows * a.group - item.m0;      // rows of the item
+  if (r0 >= M) return;
+  const int pieces = item.last - c0 + 1;
+  auto row_of = [&](int k, int r) {
+    return ((size_t)2 * (c0 + k) + (k == 0)) * 2 * kTile + r0 + r;
+  };
   const float2* const stats = stats_of(a, D, ctas);
-  for (int x = threadIdx.x; x < rows * D / 4; x += blockDim.x) {
-    const int row = part * rows + x / (D / 4), col = x % (D / 4) * 4;
-    if (item.m0 + row >= M) break;
-    float top = TV_NEG_INF, sum = 0.f;
-    for (int c = c0; c <= item.last; ++c)
-      top = fmaxf(top, stats[((size_t)2 * c + (c == c0)) * 2 * kTile + row].x);
+  // 16 neighbouring threads for a row
+  const int r = tid / 16, sub = tid % 16;
+  float top = TV_NEG_INF, sum = 0.f;
+  if (r0 + r < M)
+    for (int k = sub; k < pieces; k += 16) {
+      const float2 ms = stats[row_of(k, r)];
+      join_fac[k * kJoinRows + r] = ms.x;
+      top = fmaxf(top, ms.x);
+    }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (r0 + r < M)
+    for (int k = sub; k < pieces; k += 16) {
+      const float m = join_fac[k * kJoinRows + r], part = stats[row_of(k, r)].y;
+      const float f = part != part ? part : m == TV_NEG_INF ? 0.f : ex2(m - top);
+      join_fac[k * kJoinRows + r] = f;
+      sum += f * part;
+    }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if (sub == 0) inv[r] = sum;
+  __syncthreads();
+  const float up = pow2i(exponent_of(a.c, a.layer, 1, item.head));
+  for (int x = tid; x < kJoinRows * D / 4; x += 256) {
+    const int row = x / (D / 4), col = x % (D / 4) * 4;
+    if (r0 + row >= M) break;
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c = c0; c <= item.last; ++c) {
-      const size_t at = ((size_t)2 * c + (c == c0)) * 2 * kTile + row;
-      const float2 ms = stats[at];
-      const float f = ms.y != ms.y ? ms.y : ms.x == TV_NEG_INF ? 0.f : ex2(ms.x - top);
-      const float4 v = *reinterpret_cast<const float4*>(a.part + at * D + col);
-      sum += f * ms.y;
+#pragma unroll 8
+    for (int k = 0; k < pieces; ++k) {
+      const float f = join_fac[k * kJoinRows + row];
+      const float4 v = *reinterpret_cast<const float4*>(a.part + row_of(k, row) * D + col);
       y.x += f * v.x;
       y.y += f * v.y;
       y.z += f * v.z;
       y.w += f * v.w;
     }
-    store_out(a, item.b, item.head, item.m0 + row, M, col, D, y, sum, up);
+    store_out(a, item.b, item.head, item.m0 + r0 + row, item.m0 + M, col, D, y, inv[row], up);
   }
 }
 
@@ -785,8 +812,9 @@ int launch_tiles(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t join = {};
-  join.gridDim = dim3((unsigned)(sm_count * kJoinParts));
+  join.gridDim = dim3((unsigned)(sm_count * ((split ? kTile : 2 * kTile) / kJoinRows)));
   join.blockDim = dim3(256);
+  join.dynamicSmemBytes = (size_t)sm_count * kJoinRows * sizeof(float);
   join.stream = stream;
   join.attrs = &early;
   join.numAttrs = 1;
