@@ -4,14 +4,15 @@
 //
 // One persistent CTA per SM, two tiles of 128 rows at a time:
 //   warps 0-3, 4-7    softmax of tile 0 and 1, one row per thread: a step's 128 scores from
-//                     tensor memory into registers, weights back into it as fp16, those of 64
-//                     tokens over the first half of their scores
-//   warps 8-11        widen 128 tokens' keys and values to fp16 in shared memory (a token per
-//                     thread, its codes loaded a step ahead), two stages
-//   warps 12, 13      the products of tile 0 and 1: S = Q K^T (both from shared memory) and
+//                     tensor memory, 32 at a time with the next on their way, and weights back
+//                     into it as fp16, those of 64 tokens over the first half of their scores
+//   warps 8-11        widen 128 tokens' keys to fp16 in shared memory (a token per thread,
+//                     its codes loaded a step ahead), two stages
+//   warps 12-15       the same for values
+//   warps 16, 17      the products of tile 0 and 1: S = Q K^T (both from shared memory) and
 //                     O += P V (P from tensor memory), S and O in tensor memory
-//   warp 14           the CTA's pieces, in a ring that the others read
-//   warp 15           zeros in the rows behind the requests' last
+//   warp 18           the CTA's pieces, in a ring that the others read
+//   warp 19           zeros in the rows behind the requests' last
 // (registers that the others leave go to the softmax).  The softmax threads also bring their rows
 // of queries to shared memory: two warps beside them took 24 thousand clocks for 256 rows.
 // The two tiles take turns: while one's scores become weights, the tensor cores work on the
@@ -45,12 +46,12 @@ using namespace gemm;
 constexpr int kTile = 128;
 constexpr int kHalfTile = 64;                    // tokens whose weights are handed over at once
 constexpr int kSoftmaxWarps = 8;
-constexpr int kWidenWarps = 4;
+constexpr int kWidenWarps = 8;                   // four for keys, four for values
 constexpr int kMmaWarp = kSoftmaxWarps + kWidenWarps;
 constexpr int kPieceWarp = kMmaWarp + 2;
 constexpr int kTileThreads = 32 * (kPieceWarp + 2);
 // registers per thread after the split
-constexpr int kRegsSoftmax = 176, kRegsWiden = 88, kRegsOther = 72, kRegsLaunch = 128;
+constexpr int kRegsSoftmax = 136, kRegsWiden = 72, kRegsOther = 64, kRegsLaunch = 96;
 static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kWidenWarps * kRegsWiden + 4 * kRegsOther) <=
                   kTileThreads * kRegsLaunch,
               "the warpgroups' registers fit what the block was launched with");
@@ -76,7 +77,7 @@ struct TileShared {
   Work work[kWorkSlots];
   Work now[2][2];                                // [tile][piece % 2], the softmax's
   uint64_t kfull[kStages], kempty[kStages], vfull[kStages], vempty[kStages];
-  uint64_t sfull[2], pfull[2][2], ofull[2];      // pfull: [tile][half of the tokens]
+  uint64_t sfull[2], pfull[2][2], ofull[2][2];   // [tile][half of the tokens]
   uint64_t qfull[2], merge;
   uint32_t tmem;
   // tokens of a step that exist and have a page; a slot is used again four steps later, when
@@ -261,6 +262,20 @@ __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
+// Scales a row's sums.
+template <int D>
+__device__ __noinline__ void scale_sums(uint32_t to, float down) {
+#pragma unroll 1
+  for (int k = 0; k < D; k += 16) {
+    uint32_t d[16];
+    tmem_ld16(to + k, d);
+    tmem_wait16(d);
+#pragma unroll
+    for (int y = 0; y < 16; ++y) d[y] = __float_as_uint(__uint_as_float(d[y]) * down);
+    tmem_st16(to + k, d);
+  }
+  tmem_stored();
+}
 // Scores that a row does not see become -inf in tensor memory; a set bit in `see` is seen.
 __device__ __noinline__ void hide_scores(uint32_t ts, uint4 see) {
 #pragma unroll 1
@@ -308,7 +323,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     for (int x = 0; x < 2; ++x) {
       mbar_init(&sh.sfull[x], 1);
       for (int i = 0; i < 2; ++i) mbar_init(&sh.pfull[x][i], kSoftmaxWarps / 2);
-      mbar_init(&sh.ofull[x], 1);
+      for (int i = 0; i < 2; ++i) mbar_init(&sh.ofull[x][i], 1);
       mbar_init(&sh.qfull[x], split ? kSoftmaxWarps : kSoftmaxWarps / 2);
     }
     mbar_init(&sh.merge, kSoftmaxWarps);
@@ -370,14 +385,12 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             for (int k = 0; k < kHalfTile / 16; ++k)
               mma_ts(to, ts + half * kHalfTile + k * 8, v0 + k * (2048u >> 4),
                      f16_desc(kTile, D, true), j > first || half > 0 || k > 0);
-            if (half) {
-              umma_commit<false>(&sh.ofull[x]);
-              umma_commit<false>(&sh.vempty[stage]);
-            }
+            umma_commit<false>(&sh.ofull[x][half]);
+            if (half) umma_commit<false>(&sh.vempty[stage]);
           }
           __syncwarp();
         }
-        if (D != kTile) wait_on(&sh.ofull[x], count & 1, bad);
+        if (D != kTile) wait_on(&sh.ofull[x][1], count & 1, bad);
         if (j + stride < n) scores(j + stride);
       }
       steps_done += (uint32_t)n;
@@ -406,8 +419,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   } else if (warp >= kSoftmaxWarps) {
     // ---- keys and values to fp16 ----
     regs_fewer<kRegsWiden>();
-    const int row = tid & (kTile - 1);
-    const uint32_t k0 = smem_u32(k_tiles), v0 = smem_u32(v_tiles);
+    const int side = warp >= kSoftmaxWarps + 4, row = tid & (kTile - 1);
+    uint64_t* const full = side ? sh.vfull : sh.kfull;
+    uint64_t* const empty = side ? sh.vempty : sh.kempty;
+    const uint32_t base = smem_u32(side ? v_tiles : k_tiles);
     uint32_t s = 0;
     for (; const Work* const w = take(sh, taken, bad); ++taken) {
       const Work p = *w;
@@ -416,31 +431,24 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         const int pos = step * kStep + row;
         return step >= p.s0 && pos < p.tokens ? page_of(a.c, a.t, p.b, pos) : -1;
       };
-      int page = page_at(p.s1 - 1), page_next = page_at(p.s1 - 2);
-      Token<D> key, value;
-      key.load(a, p, page, (p.s1 - 1) * kStep + row, 0);
-      value.load(a, p, page, (p.s1 - 1) * kStep + row, 1);
+      int page_next = page_at(p.s1 - 2);
+      Token<D> token;
+      token.load(a, p, page_at(p.s1 - 1), (p.s1 - 1) * kStep + row, side);
       for (int step = p.s1 - 1; step >= p.s0; --step, ++s) {
-        const uint32_t stage = s % kStages, parity = ((s / kStages) & 1) ^ 1;
-        const bool there = page >= 0;
-        page = page_next;
+        const uint32_t stage = s % kStages;
+        wait_on(&empty[stage], ((s / kStages) & 1) ^ 1, bad);
+        token.widen_to(base + stage * kTileBytes, row);
+        if (!side) {
+          const uint32_t word = __ballot_sync(0xffffffffu, token.there);
+          if (lane == 0) sh.ok[s % kOkSlots][warp & 3] = word;
+          if (!token.there && step * kStep + row < p.tokens)
+            atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+        }
+        async_visible();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[stage]);
+        token.load(a, p, page_next, (step - 1) * kStep + row, side);
         page_next = page_at(step - 2);
-        wait_on(&sh.kempty[stage], parity, bad);
-        key.widen_to(k0 + stage * kTileBytes, row);
-        const uint32_t word = __ballot_sync(0xffffffffu, there);
-        if (lane == 0) sh.ok[s % kOkSlots][warp & 3] = word;
-        async_visible();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.kfull[stage]);
-        key.load(a, p, page, (step - 1) * kStep + row, 0);
-        if (!there && step * kStep + row < p.tokens)
-          atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
-        wait_on(&sh.vempty[stage], parity, bad);
-        value.widen_to(v0 + stage * kTileBytes, row);
-        async_visible();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.vfull[stage]);
-        value.load(a, p, page, (step - 1) * kStep + row, 1);
       }
     }
   } else {
@@ -467,19 +475,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       return w.more;
     };
     // this thread's row of queries
-    uint4 q[D / 8];
-    auto load_queries = [&]() {
+    auto queries = [&]() {
       const Work& next = sh.now[x][(taken - 1) & 1];
       const int m = min(next.m0 + (split ? 0 : x * kTile) + r, next.rows * a.group - 1);
       const int i = m / a.group;
-      const uint4* const src = reinterpret_cast<const uint4*>(
+      return reinterpret_cast<const uint4*>(
           a.q + (((size_t)next.b * a.R + i) * a.c.kv_heads * a.group +
                  (size_t)next.head * a.group + (m - i * a.group)) * D);
-#pragma unroll
-      for (int k = 0; k < D / 8; ++k) q[k] = __ldg(src + k);
     };
     bool more = take_next();
-    if (more) load_queries();
     while (more) {
       const Work& p = sh.now[x][(taken - 1) & 1];
       const int len = p.len, M = p.rows * a.group, top_step = p.s1 - 1;
@@ -493,6 +497,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
           sh.parents[x][i] = a.parents[(size_t)p.b * a.R + i];
       float f;
       {
+        uint4 q[D / 8];
+        const uint4* const src = queries();
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) q[k] = __ldg(src + k);
         uint32_t top2 = 0;                       // largest magnitudes of two columns, in bf16
 #pragma unroll
         for (int k = 0; k < D / 8; ++k)
@@ -559,76 +567,70 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
           }
           if (__any_sync(0xffffffffu, (see.x & see.y & see.z & see.w) != 0xffffffffu))
             hide_scores(ts, see);
-          // the largest score, of the second half first: the first half's stay in registers
-          uint32_t c[2][32];
-          float top4[4] = {TV_NEG_INF, TV_NEG_INF, TV_NEG_INF, TV_NEG_INF};
+          const float2 ff = make_float2(f, f);
+          float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t c[2][32], w[32];
+          tmem_ld32(ts, c[0]);
 #pragma unroll
-          for (int half = 1; half >= 0; --half) {
-            tmem_ld32(ts + kHalfTile * half, c[0]);
-            tmem_ld32(ts + kHalfTile * half + 32, c[1]);
-            tmem_wait(c[0]);
-            tmem_wait(c[1]);
+          for (int k = 0; k < 4; ++k) {
+            uint32_t(&z)[32] = c[k & 1];
+            tmem_wait(z);
+            if (k < 3) tmem_ld32(ts + 32 * (k + 1), c[(k + 1) & 1]);
+            float top2[2] = {TV_NEG_INF, TV_NEG_INF};
 #pragma unroll
-            for (int y = 0; y < 64; y += 2) {
-              float& t = top4[(y >> 1) & 3];
-              t = fmaxf(fmaxf(t, __uint_as_float(c[y >> 5][y & 31])),
-                        __uint_as_float(c[y >> 5][(y & 31) + 1]));
+            for (int y = 0; y < 32; y += 4) {
+              top2[0] = fmaxf(fmaxf(top2[0], __uint_as_float(z[y])), __uint_as_float(z[y + 1]));
+              top2[1] = fmaxf(fmaxf(top2[1], __uint_as_float(z[y + 2])),
+                              __uint_as_float(z[y + 3]));
             }
-          }
-          // (lanes without a row hold scores of whatever was there, and have no say)
-          const float top = in ? f * fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]))
-                               : TV_NEG_INF;
-          // weights are relative to what the largest score was, until it has grown too far
-          if (__any_sync(0xffffffffu, top > mref + kSlack)) {
-            float down = 1.f;
-            if (top > mref) {
-              down = ex2(mref - top);
-              mref = top;
+            // (lanes without a row hold scores of whatever was there, and have no say)
+            const float top = in ? f * fmaxf(top2[0], top2[1]) : TV_NEG_INF;
+            // weights are relative to what the largest score was, until it has grown too far
+            if (__any_sync(0xffffffffu, top > mref + kSlack)) {
+              float down = 1.f;
+              if (top > mref) {
+                down = ex2(mref - top);
+                mref = top;
+              }
               l *= down;
-            }
-            if (i >= 2) {                                  // there is a sum to scale
-              wait_on(&sh.ofull[x], (count - 1) & 1, bad);
-              tc_fence_after();
-#pragma unroll 1
-              for (int k = 0; k < D; k += 16) {
-                uint32_t d[16];
-                tmem_ld16(to + k, d);
-                tmem_wait16(d);
+              acc[0] = make_float2(acc[0].x * down, acc[0].y * down);
+              acc[1] = make_float2(acc[1].x * down, acc[1].y * down);
+              if (k & 1) {                       // weights that were not handed over yet
 #pragma unroll
-                for (int y = 0; y < 16; ++y) d[y] = __float_as_uint(__uint_as_float(d[y]) * down);
-                tmem_st16(to + k, d);
+                for (int y = 0; y < 16; ++y) {
+                  const float2 e = widen(w[y]);
+                  const __half2 h = __floats2half2_rn(e.x * down, e.y * down);
+                  w[y] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+              }
+              if (i >= 2 || k >= 2) {            // there is a sum to scale
+                if (k < 2)
+                  wait_on(&sh.ofull[x][1], (count - 1) & 1, bad);
+                else
+                  wait_on(&sh.ofull[x][0], count & 1, bad);
+                tc_fence_after();
+                scale_sums<D>(to, down);
               }
             }
-          }
-          const float off = kLift - (mref == TV_NEG_INF ? 0.f : mref);
-          const float2 ff = make_float2(f, f), oo = make_float2(off, off);
-          float2 acc[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            const float off = kLift - (mref == TV_NEG_INF ? 0.f : mref);
+            const float2 oo = make_float2(off, off);
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (half) {
-              tmem_ld32(ts + kHalfTile, c[0]);
-              tmem_ld32(ts + kHalfTile + 32, c[1]);
-              tmem_wait(c[0]);
-              tmem_wait(c[1]);
-            }
-            uint32_t w[32];
-#pragma unroll
-            for (int y = 0; y < 64; y += 2) {
-              const uint32_t(&z)[32] = c[y >> 5];
-              float2 e = __ffma2_rn(make_float2(__uint_as_float(z[y & 31]),
-                                                __uint_as_float(z[(y & 31) + 1])),
-                                    ff, oo);
+            for (int y = 0; y < 32; y += 2) {
+              float2 e = __ffma2_rn(
+                  make_float2(__uint_as_float(z[y]), __uint_as_float(z[y + 1])), ff, oo);
               e.x = ex2(e.x);
               e.y = ex2(e.y);
               acc[(y >> 1) & 1] = __fadd2_rn(acc[(y >> 1) & 1], e);
               const __half2 h = __floats2half2_rn(e.x, e.y);
-              w[y >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+              w[16 * (k & 1) + (y >> 1)] = *reinterpret_cast<const uint32_t*>(&h);
             }
-            tmem_st32(ts + kHalfTile * half, w);
-            tmem_stored();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.pfull[x][half]);
+            if (k & 1) {
+              tmem_st32(ts + 32 * (k - 1), w);
+              tmem_stored();
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.pfull[x][k >> 1]);
+            }
           }
           acc[0] = __fadd2_rn(acc[0], acc[1]);
           l += acc[0].x + acc[0].y;
@@ -638,12 +640,17 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         }
       }
       steps_done += (uint32_t)n;
-      // (the next queries on their way while the sums are stored)
+      // (the next queries on their way to L2 while the sums are stored)
       more = take_next();
-      if (more) load_queries();
+      if (more) {
+        const uint4* const src = queries();
+#pragma unroll
+        for (int k = 0; k < D / 8; k += 8)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(src + k));
+      }
 
       // the sums
-      if (x < ops) wait_on(&sh.ofull[x], (count - 1) & 1, bad);
+      if (x < ops) wait_on(&sh.ofull[x][1], (count - 1) & 1, bad);
       tc_fence_after();
       float fac[2] = {1.f, 0.f};
       if (split) {
