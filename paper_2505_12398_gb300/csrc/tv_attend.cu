@@ -77,32 +77,46 @@ struct Raw {
   uint32_t ks, vs;                               // scales of two tokens of a chunk
 };
 
+// Where a lane's parts of a unit are, from the first byte of its token's piece of a page's
+// block of keys: bytes of K, V and scales, and what a slot adds.
 template <int D>
-__device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, int page_size, int slot,
-                                          int lane) {
-  const int g = lane >> 2, t = lane & 3;
-  const uint8_t* const values = keys + (size_t)page_size * D * 9 / 16;
-  constexpr int kChunks = D / 32;
-  const int kc = t * kChunks / 4, vc = g * kChunks / 8;      // chunks of the lane's columns
-  const uint8_t* const kp = keys + ((size_t)kc * page_size + slot) * 16 + (t * (D / 8)) % 16;
-  const uint8_t* const vp = values + ((size_t)vc * page_size + slot) * 16 + (g * (D / 16)) % 16;
+struct Lane {
+  uint32_t k, v, scale;
+  __device__ __forceinline__ Lane(int page_size, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    constexpr int kChunks = D / 32;
+    const uint32_t block = (uint32_t)page_size * D * 9 / 16, plane = (uint32_t)page_size * 16;
+    k = (uint32_t)(t * kChunks / 4) * plane + (uint32_t)((t * (D / 8)) % 16 + g * 16);
+    v = block + (uint32_t)(g * kChunks / 8) * plane + (uint32_t)((g * (D / 16)) % 16 + t * 32);
+    // lane 8 c + j: tokens 2 j and 2 j + 1 of chunk c
+    scale = (uint32_t)page_size * D / 2 +
+            (uint32_t)((lane >> 3) % kChunks) * (uint32_t)page_size * 2 + (lane & 7) * 4;
+  }
+};
+// keys: the block's first byte.
+template <int D>
+__device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, const Lane<D>& at,
+                                          uint32_t block, uint32_t slot) {
+  const uint8_t* const kp = keys + (at.k + slot * 16);
+  const uint8_t* const vp = keys + (at.v + slot * 16);
+  const uint8_t* const sp = keys + (at.scale + slot * 2);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if constexpr (D == 128) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(kp + (g + 8 * i) * 16));
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(kp + 128 * i));
       r.k[i][0] = u.x;
       r.k[i][1] = u.y;
       r.k[i][2] = u.z;
       r.k[i][3] = u.w;
     } else {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(kp + (g + 8 * i) * 16));
+      const uint2 u = __ldg(reinterpret_cast<const uint2*>(kp + 128 * i));
       r.k[i][0] = u.x;
       r.k[i][1] = u.y;
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint8_t* const p = vp + (2 * t + (i & 1) + 8 * (i >> 1)) * 16;
+  for (int i = 0; i < 4; ++i) {                    // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    const uint8_t* const p = vp + ((i & 1) + 8 * (i >> 1)) * 16;
     if constexpr (D == 128) {
       const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
       r.v[i][0] = u.x;
@@ -111,11 +125,8 @@ __device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, int pa
       r.v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
     }
   }
-  // lane 8 c + j: tokens 2 j and 2 j + 1 of chunk c
-  const size_t at = (size_t)page_size * D / 2 +
-                    ((size_t)((lane >> 3) % kChunks) * page_size + slot) * 2 + (lane & 7) * 4;
-  r.ks = __ldg(reinterpret_cast<const uint32_t*>(keys + at));
-  r.vs = __ldg(reinterpret_cast<const uint32_t*>(values + at));
+  r.ks = __ldg(reinterpret_cast<const uint32_t*>(sp));
+  r.vs = __ldg(reinterpret_cast<const uint32_t*>(sp + block));
 }
 
 // Shared memory of a CTA; what follows it: the warps' sums [kWarps][rows][D + 4].
@@ -220,28 +231,29 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       l[n][0] = l[n][1] = 0.f;
     }
 
+    // pages and units are a step ahead, in two sets of registers
+    const Lane<D> at(a.c.page_size, lane);
+    const uint32_t block = (uint32_t)a.c.page_size * D * 9 / 16;
+    const size_t page_bytes = (size_t)block * 2 * H;
+    const uint8_t* const blocks = a.c.data + (size_t)a.layer * a.c.pages * page_bytes +
+                                  (size_t)head * 2 * block;
+    const int32_t* const table = a.t.table + (size_t)b * a.t.max_pages;
     auto page_at = [&](int s) -> int {
       const int pos = s * kStep + warp * kUnit;
-      return s < s1 && pos < tokens ? page_of(a.c, a.t, b, pos) : -1;
+      if (s >= s1 || pos >= tokens) return -1;
+      const int page = __ldg(table + (pos >> a.c.page_shift));   // (tokens end with the table)
+      return (unsigned)page < (unsigned)a.c.pages ? page : -1;
     };
     auto fetch = [&](Raw<D>& r, int page, int s) {
       if (page >= 0)
-        load_unit<D>(r, block_of(a.c, a.layer, page, head, 0), a.c.page_size,
-                     (s * kStep + warp * kUnit) & (a.c.page_size - 1), lane);
+        load_unit<D>(r, blocks + (size_t)page * page_bytes, at, block,
+                     (uint32_t)(s * kStep + warp * kUnit) & (a.c.page_size - 1));
     };
-    Raw<D> raw;
-    int page = page_at(s0), page_next = page_at(s0 + 1);
-    fetch(raw, page, s0);
-    for (int s = s0; s < s1; ++s) {
-      const int pos = s * kStep + warp * kUnit;
-      Raw<D> now = raw;
-      const bool there = page >= 0;
-      if (!there && pos < tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
-      page = page_next;
-      fetch(raw, page, s + 1);
-      page_next = page_at(s + 2);
-      if (!there) continue;
-
+    auto use = [&](const Raw<D>& now, bool there, int pos) {
+      if (!there) {
+        if (pos < tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+        return;
+      }
       // S^T
       float st[NT][4];
 #pragma unroll
@@ -367,6 +379,20 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
           }
         }
       }
+    };
+    Raw<D> even, odd;
+    int page = page_at(s0), page_next = page_at(s0 + 1);
+    fetch(even, page, s0);
+    for (int s = s0; s < s1; s += 2) {
+      const int pos = s * kStep + warp * kUnit;
+      const bool there = page >= 0, there_next = page_next >= 0;
+      fetch(odd, page_next, s + 1);
+      page = page_at(s + 2);
+      use(even, there, pos);
+      if (s + 1 >= s1) break;
+      fetch(even, page, s + 2);
+      page_next = page_at(s + 3);
+      use(odd, there_next, pos + kStep);
     }
 
     // the warps' sums joined.  o[n][i][k]: column (D / 8) g + 2 i + (k >> 1), row
@@ -489,9 +515,8 @@ int tv_attend_counters(int sm_count) { return kPerSm * sm_count; }
 
 int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const long long rows = (long long)a.R * a.group;
-  if (rows > (a.c.head_dim == 128 ? 16 : 32)) return tv_launch_attend_tile(a, sm_count, stream);
-  if (a.c.head_dim == 128)
-    return rows <= 8 ? launch<128, 1>(a, sm_count, stream) : launch<128, 2>(a, sm_count, stream);
-  if (rows <= 8) return launch<64, 1>(a, sm_count, stream);
-  return rows <= 16 ? launch<64, 2>(a, sm_count, stream) : launch<64, 4>(a, sm_count, stream);
+  const int most = a.c.head_dim == 128 ? 8 : 16;
+  if (rows > most) return tv_launch_attend_tile(a, sm_count, stream);
+  if (a.c.head_dim == 128) return launch<128, 1>(a, sm_count, stream);
+  return rows <= 8 ? launch<64, 1>(a, sm_count, stream) : launch<64, 2>(a, sm_count, stream);
 }
