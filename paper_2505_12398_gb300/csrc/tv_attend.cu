@@ -3,14 +3,15 @@
 //
 //   o_i = sum_j p_ij v_j,  p_i = softmax_j(scale q_i . k_j)  over the tokens j that row i sees.
 //
-// Bound by the cache's bytes, and next to that by the instructions that widen the codes, so
-// neither goes through shared memory: a warp takes 16 tokens at a time from global memory
-// into the registers of mma.sync fragments, each lane widening the codes it loaded.
-// (tcgen05 wants its operands in shared memory, 4 bytes of traffic there per value, written and
-// read, for the 9/16 that come from memory.)  With lane = 4 g + t:
-//   S^T [16 tokens x 8 rows]  = K Q^T      A: the lane's 2 tokens, g and g + 8, in the D / 4
-//                                          columns of index t; the order of columns inside
-//                                          a product is free, so these are D / 4 adjacent ones
+// Bound by the cache's bytes, and next to that by the instructions that widen the codes.  One
+// warp of a CTA copies whole pages of keys and values (they lie together) to a ring in shared
+// memory by TMA, from piece to piece without a stop; eight take 16 tokens of a step each, and
+// widen the codes in the registers of mma.sync fragments (tcgen05 wants its operands in shared
+// memory: 4 bytes of traffic there per value, written and read, for the 9/16 that come from
+// memory).  With lane = 4 g + t:
+//   S^T [16 tokens x 8 rows]  = K Q^T      A: the lane's 2 tokens, g and g + 8, in 8 columns
+//                                          (index t) of each 32; the order of columns inside
+//                                          a product is free, so these are adjacent ones
 //   O^T [16 columns x 8 rows] += V^T P^T   A: the lane's D / 8 columns of index g in its 4
 //                                          tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9; codes of two
 //                                          tokens are paired before they are widened
@@ -37,6 +38,7 @@
 #include "tv_cache.cuh"
 #include "tv_device.cuh"
 #include "tv_launch.h"
+#include "tv_ptx.cuh"
 
 namespace tvk {
 namespace attend {
@@ -44,7 +46,7 @@ namespace attend {
 
 
 constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
+constexpr int kThreads = 32 * (kWarps + 1);      // and the copying warp
 constexpr int kUnit = 16;                        // tokens of a warp's step
 static_assert(kStep == kUnit * kWarps, "a step is 16 tokens of each warp");
 constexpr int kMaxNodes = 1024;                  // rows of a tree
@@ -68,74 +70,61 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// A unit's codes and scales as a lane loads them.
-template <int D>
-struct Raw {
-  static constexpr int kK = D / 32;              // words of a token's codes, D / 4 columns
-  static constexpr int kV = D / 64;              // D / 8 columns
-  uint32_t k[2][kK], v[4][kV];
-  uint32_t ks, vs;                               // scales of two tokens of a chunk
-};
+constexpr int kWorkSlots = 4;
 
-// Where a lane's parts of a unit are, from the first byte of its token's piece of a page's
-// block of keys: bytes of K, V and scales, and what a slot adds.
+// Steps that the ring holds, of 128 tokens' codes and scales, keys and values.
 template <int D>
-struct Lane {
-  uint32_t k, v, scale;
-  __device__ __forceinline__ Lane(int page_size, int lane) {
-    const int g = lane >> 2, t = lane & 3;
-    constexpr int kChunks = D / 32;
-    const uint32_t block = (uint32_t)page_size * D * 9 / 16, plane = (uint32_t)page_size * 16;
-    k = (uint32_t)(t * kChunks / 4) * plane + (uint32_t)((t * (D / 8)) % 16 + g * 16);
-    v = block + (uint32_t)(g * kChunks / 8) * plane + (uint32_t)((g * (D / 16)) % 16 + t * 32);
-    // lane 8 c + j: tokens 2 j and 2 j + 1 of chunk c
-    scale = (uint32_t)page_size * D / 2 +
-            (uint32_t)((lane >> 3) % kChunks) * (uint32_t)page_size * 2 + (lane & 7) * 4;
-  }
-};
-// keys: the block's first byte.
+constexpr int kRing = D == 128 ? 3 : 6;
 template <int D>
-__device__ __forceinline__ void load_unit(Raw<D>& r, const uint8_t* keys, const Lane<D>& at,
-                                          uint32_t block, uint32_t slot) {
-  const uint8_t* const kp = keys + (at.k + slot * 16);
-  const uint8_t* const vp = keys + (at.v + slot * 16);
-  const uint8_t* const sp = keys + (at.scale + slot * 2);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if constexpr (D == 128) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4*>(kp + 128 * i));
-      r.k[i][0] = u.x;
-      r.k[i][1] = u.y;
-      r.k[i][2] = u.z;
-      r.k[i][3] = u.w;
-    } else {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(kp + 128 * i));
-      r.k[i][0] = u.x;
-      r.k[i][1] = u.y;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {                    // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-    const uint8_t* const p = vp + ((i & 1) + 8 * (i >> 1)) * 16;
-    if constexpr (D == 128) {
-      const uint2 u = __ldg(reinterpret_cast<const uint2*>(p));
-      r.v[i][0] = u.x;
-      r.v[i][1] = u.y;
-    } else {
-      r.v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-    }
-  }
-  r.ks = __ldg(reinterpret_cast<const uint32_t*>(sp));
-  r.vs = __ldg(reinterpret_cast<const uint32_t*>(sp + block));
+constexpr uint32_t kStepBytes = (uint32_t)kStep * D * 9 / 8;
+
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t at) {
+  uint16_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=h"(v) : "r"(at));
+  return v;
+}
+__device__ __forceinline__ void consumers() {    // a barrier of the warps that do not copy
+  asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory");
 }
 
-// Shared memory of a CTA; what follows it: the warps' sums [kWarps][rows][D + 4].
+// Where a lane's codes and scales are in a step of the ring.
+template <int D>
+struct Lane {
+  uint32_t k, ks, v, vs, plane;
+  int page;                                      // of the step's
+  __device__ __forceinline__ Lane(const CacheArgs& c, int warp, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    constexpr int kChunks = D / 32;
+    const uint32_t block = (uint32_t)c.page_size * D * 9 / 16;
+    const uint32_t slot = (uint32_t)(warp * kUnit) & (c.page_size - 1);
+    page = (warp * kUnit) >> c.page_shift;
+    plane = (uint32_t)c.page_size;               // tokens of a chunk's codes or scales
+    const uint32_t keys = (uint32_t)page * 2 * block, values = keys + block;
+    const uint32_t scales = plane * D / 2, chunk = (uint32_t)(g * kChunks / 8) * plane;
+    k = keys + (slot + g) * 16 + t * 4;
+    ks = keys + scales + (slot + g) * 2 + (t >> 1);
+    v = values + (chunk + slot + 2 * t) * 16 + (g * (D / 16)) % 16;
+    vs = values + scales + (chunk + slot + 2 * t) * 2;
+  }
+};
+// Shared memory of a CTA; what follows it: the ring, and the warps' sums [kWarps][rows][D + 4].
 struct alignas(16) Shared {
+  uint64_t given[kWorkSlots], taken[kWorkSlots], full[8], empty[8];
+  Piece pieces[kWorkSlots], now[2];              // the ring of them, and the consumers' two
+  int more[kWorkSlots], going[2];
+  uint32_t valid[8];                             // the pages of a step that are there
   Schedule plan;
-  Shares shares;
-  Walker walker;                                 // (thread 0's)
-  Piece piece;
-  int more, last;
+  int last;
   float m[kWarps][32], l[kWarps][32];
   float fac[kWarps][32], sum[32], top[32];
   int32_t parents[kMaxNodes];
@@ -152,37 +141,101 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
   constexpr int kPitch = D + 4;
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  float* const sums = reinterpret_cast<float*>(smem + sizeof(Shared));
+  const uint32_t ring = smem_u32(smem + sizeof(Shared));
+  float* const sums =
+      reinterpret_cast<float*>(smem + sizeof(Shared) + kRing<D> * (size_t)kStepBytes<D>);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int G = a.group, H = a.c.kv_heads;
+  uint32_t bad = 0;
 
-  {
-    Walker w;
-    const Shares shares = plan(a, sh.plan, kRows, blockIdx.x, gridDim.x, w);
-    if (tid == 0) {
-      sh.shares = shares;
-      sh.walker = w;
+  if (tid == 0) {
+    for (int i = 0; i < kWorkSlots; ++i) {
+      mbar_init(&sh.given[i], 1);
+      mbar_init(&sh.taken[i], 1);
     }
+    for (int i = 0; i < kRing<D>; ++i) {
+      mbar_init(&sh.full[i], 1);
+      mbar_init(&sh.empty[i], kWarps);
+    }
+    fence_mbar_init();
   }
-  const Piece& p = sh.piece;
-  for (;;) {
-    if (tid == 0) sh.more = sh.walker.next(a, kRows, sh.piece);
-    __syncthreads();
-    if (!sh.more) break;
+  Walker walker;
+  const Shares shares = plan(a, sh.plan, kRows, blockIdx.x, gridDim.x, walker);   // (a barrier)
+
+  if (warp == kWarps) {
+    // ---- pages to the ring ----
+    const uint32_t block2 = (uint32_t)a.c.page_size * D * 9 / 8;      // keys and values
+    const int pages = kStep >> a.c.page_shift;                        // of a step, 8 at most
+    uint32_t count = 0;
+    for (uint32_t n = 0;; ++n) {
+      Piece& p = sh.pieces[n % kWorkSlots];
+      if (lane == 0) {
+        wait_on(&sh.taken[n % kWorkSlots], ((n / kWorkSlots) & 1) ^ 1, bad);
+        sh.more[n % kWorkSlots] = !bad && walker.next(a, kRows, p);
+        mbar_arrive(&sh.given[n % kWorkSlots]);
+      }
+      __syncwarp();
+      if (!sh.more[n % kWorkSlots]) break;
+      const int b = p.b, s0 = p.s0, s1 = p.s1, tokens = p.tokens;
+      const uint8_t* const blocks =
+          a.c.data + ((size_t)a.layer * a.c.pages * H + p.head) * block2;
+      const int32_t* const table = a.t.table + (size_t)b * a.t.max_pages;
+      auto page_at = [&](int s) -> int {
+        const int pos = s * kStep + (lane << a.c.page_shift);
+        return lane < pages && s < s1 && pos < tokens
+                   ? __ldg(table + (pos >> a.c.page_shift))            // (inside the table)
+                   : -2;
+      };
+      int page = page_at(s0), page_next = page_at(s0 + 1);
+      for (int s = s0; s < s1; ++s, ++count) {
+        const uint32_t stage = count % kRing<D>;
+        const bool there = (unsigned)page < (unsigned)a.c.pages;
+        if (!there && page != -2) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
+        const uint32_t valid = __ballot_sync(0xffffffffu, there);
+        wait_on(&sh.empty[stage], ((count / kRing<D>) & 1) ^ 1, bad);
+        if (lane == 0) {
+          sh.valid[stage] = valid;
+          mbar_arrive_expect_tx(&sh.full[stage], (uint32_t)__popc(valid) * block2);
+        }
+        __syncwarp();
+        if (there)
+          tma_load_1d(smem + sizeof(Shared) + stage * (size_t)kStepBytes<D> + lane * block2,
+                      blocks + (size_t)page * H * block2, block2, &sh.full[stage]);
+        page = page_next;
+        page_next = page_at(s + 2);
+      }
+    }
+    zero_rows(a, D, blockIdx.x, gridDim.x);
+    if (bad && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_TIMEOUT);
+    return;
+  }
+
+  const Lane<D> at(a.c, warp, lane);
+  uint32_t count = 0;
+  for (uint32_t n = 0;; ++n) {
+    if (tid == 0) {                              // (the others meet at barriers)
+      wait_on(&sh.given[n % kWorkSlots], (n / kWorkSlots) & 1, bad);
+      sh.going[n & 1] = !bad && sh.more[n % kWorkSlots];
+      sh.now[n & 1] = sh.pieces[n % kWorkSlots];
+      mbar_arrive(&sh.taken[n % kWorkSlots]);
+    }
+    consumers();
+    if (!sh.going[n & 1]) break;
+    const Piece& p = sh.now[n & 1];
     const int b = p.b, head = p.head, m0 = p.m0, s0 = p.s0, s1 = p.s1;
     const int len = p.rq.len, nrows = p.rq.rows, tokens = p.tokens;
     const bool masked = (long long)s1 * kStep > len;       // some tokens are the tree's
     if (masked && a.parents) {
       const int words = (nrows + 31) / 32;
-      for (int i = tid; i < nrows; i += kThreads) sh.parents[i] = a.parents[(size_t)b * a.R + i];
-      for (int i = tid; i < kRows * words; i += kThreads) sh.seen[i / words][i % words] = 0u;
-      __syncthreads();
+      for (int i = tid; i < nrows; i += 32 * kWarps) sh.parents[i] = a.parents[(size_t)b * a.R + i];
+      for (int i = tid; i < kRows * words; i += 32 * kWarps) sh.seen[i / words][i % words] = 0u;
+      consumers();
       if (tid < kRows && m0 + tid < nrows * G) {
         if (!walk(sh.parents, (m0 + tid) / G,
                   [&](int j) { sh.seen[tid][j >> 5] |= 1u << (j & 31); }))
           atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
       }
-      __syncthreads();
+      consumers();
     }
 
     // queries: row 8 n + g, the columns of index t, in the order of a product's pairs
@@ -195,12 +248,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       const bool in = m < nrows * G;
       const uint4* const src = reinterpret_cast<const uint4*>(
           a.q + (((size_t)b * a.R + (in ? m / G : 0)) * H * G + (size_t)head * G + m % G) * D +
-          t * (D / 4));
+          t * 8);
       uint32_t w[D / 8];
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const uint4 u = in ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+        const uint4 u = in ? __ldg(src + 4 * i) : make_uint4(0, 0, 0, 0);
         w[4 * i] = u.x;
         w[4 * i + 1] = u.y;
         w[4 * i + 2] = u.z;
@@ -220,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       fac[n][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4);
     }
 
-    float o[NT][kDT][4], mref[NT][2], l[NT][2];
+    float o[NT][kDT][4], mref[NT][2], l[NT][2], off[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -229,31 +282,19 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
         for (int k = 0; k < 4; ++k) o[n][i][k] = 0.f;
       mref[n][0] = mref[n][1] = TV_NEG_INF;
       l[n][0] = l[n][1] = 0.f;
+      off[n][0] = off[n][1] = kLift;
     }
 
-    // pages and units are a step ahead, in two sets of registers
-    const Lane<D> at(a.c.page_size, lane);
-    const uint32_t block = (uint32_t)a.c.page_size * D * 9 / 16;
-    const size_t page_bytes = (size_t)block * 2 * H;
-    const uint8_t* const blocks = a.c.data + (size_t)a.layer * a.c.pages * page_bytes +
-                                  (size_t)head * 2 * block;
-    const int32_t* const table = a.t.table + (size_t)b * a.t.max_pages;
-    auto page_at = [&](int s) -> int {
+    for (int s = s0; s < s1; ++s, ++count) {
       const int pos = s * kStep + warp * kUnit;
-      if (s >= s1 || pos >= tokens) return -1;
-      const int page = __ldg(table + (pos >> a.c.page_shift));   // (tokens end with the table)
-      return (unsigned)page < (unsigned)a.c.pages ? page : -1;
-    };
-    auto fetch = [&](Raw<D>& r, int page, int s) {
-      if (page >= 0)
-        load_unit<D>(r, blocks + (size_t)page * page_bytes, at, block,
-                     (uint32_t)(s * kStep + warp * kUnit) & (a.c.page_size - 1));
-    };
-    auto use = [&](const Raw<D>& now, bool there, int pos) {
+      const uint32_t stage = count % kRing<D>;
+      wait_on(&sh.full[stage], (count / kRing<D>) & 1, bad);
+      const bool there = sh.valid[stage] >> at.page & 1;
       if (!there) {
-        if (pos < tokens && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
-        return;
+        if (lane == 0) mbar_arrive(&sh.empty[stage]);
+        continue;
       }
+      const uint32_t step = ring + stage * kStepBytes<D>;
       // S^T
       float st[NT][4];
 #pragma unroll
@@ -261,22 +302,14 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
 #pragma unroll
         for (int k = 0; k < 4; ++k) st[n][k] = 0.f;
       {
-        constexpr int kChunks = D / 32;
-        const int from = (t * kChunks / 4) * 8 + (g >> 1);
-        uint32_t sc[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint32_t w = __shfl_sync(0xffffffffu, now.ks, from + 4 * i);
-          sc[i] = decode_scales(g & 1 ? w >> 16 : w & 0xffffu);
-        }
-#pragma unroll
-        for (int w = 0; w < Raw<D>::kK; ++w) {             // 8 columns: two products
+        for (int w = 0; w < D / 32; ++w) {                 // 8 columns: two products
           uint32_t h[2][4];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            decode8(now.k[i][w], h[i]);
-            const bool upper = D == 128 ? w >= 2 : (t & 1);
-            const uint32_t s2 = upper ? hi_hi(sc[i]) : lo_lo(sc[i]);
+            decode8(lds32(step + at.k + w * at.plane * 16 + 128 * i), h[i]);
+            const uint32_t s2 = decode_scales(
+                __byte_perm(lds8(step + at.ks + w * at.plane * 2 + 16 * i), 0u, 0x4400u));
 #pragma unroll
             for (int k = 0; k < 4; ++k) h[i][k] = mul2(h[i][k], s2);
           }
@@ -289,6 +322,25 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
           }
         }
       }
+
+      // the values' codes, and the step is this warp's no longer
+      constexpr int kV = D / 64;                 // words of a lane's D / 8 columns of a token
+      uint32_t v[4][kV], vs[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {              // tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+        const uint32_t from = step + at.v + ((i & 1) + 8 * (i >> 1)) * 16;
+        if constexpr (D == 128) {
+          const uint2 u = lds64(from);
+          v[i][0] = u.x;
+          v[i][1] = u.y;
+        } else {
+          v[i][0] = lds32(from);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) vs[i] = lds32(step + at.vs + 16 * i);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.empty[stage]);
 
       // weights: st[n][k] is token g (k < 2) or g + 8, row 8 n + 2 t + (k & 1)
       bool grow = false;
@@ -319,6 +371,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
             if (top > mref[n][k]) {
               const float down = ex2(mref[n][k] - top);    // (0 from -inf)
               mref[n][k] = top;
+              off[n][k] = kLift - top;
               l[n][k] *= down;
 #pragma unroll
               for (int i = 0; i < kDT; ++i) {
@@ -334,8 +387,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
         float x[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float m = mref[n][k & 1];
-          x[k] = ex2(st[n][k] - (m == TV_NEG_INF ? 0.f : m) + kLift);
+          x[k] = ex2(st[n][k] + off[n][k & 1]);
           l[n][k & 1] += x[k];
         }
         pb[n][0] = transpose8(pack_half2(x[0], x[1]));
@@ -344,25 +396,22 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
 
       // O^T
       {
-        constexpr int kChunks = D / 32;
-        const int from = (g * kChunks / 8) * 8 + t;
         uint32_t sc[2];                                    // of tokens 2 t, 2 t + 1; 8 further
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint32_t w = __shfl_sync(0xffffffffu, now.vs, from + 4 * i);
           const bool upper = D == 128 ? (g & 1) : (g & 2);
-          uint32_t two = __byte_perm(w, 0u, upper ? 0x4431u : 0x4420u);
+          uint32_t two = __byte_perm(vs[i], 0u, upper ? 0x4431u : 0x4420u);
           // (bytes behind the last token may be anything, a NaN among it)
           const int left = tokens - (pos + 2 * t + 8 * i);
           if (left < 2) two = left < 1 ? 0u : two & 0xffu;
           sc[i] = decode_scales(two);
         }
 #pragma unroll
-        for (int w = 0; w < Raw<D>::kV; ++w) {             // 8 columns: four tiles
+        for (int w = 0; w < kV; ++w) {                     // 8 columns: four tiles
           uint32_t e[2][4], f[2][4];                       // even and odd columns, token pairs
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const uint32_t x = now.v[2 * i][w], y = now.v[2 * i + 1][w];
+            const uint32_t x = v[2 * i][w], y = v[2 * i + 1][w];
             decode8((x & 0x0f0f0f0fu) | (y << 4 & 0xf0f0f0f0u), e[i]);
             decode8((x >> 4 & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u), f[i]);
 #pragma unroll
@@ -379,20 +428,6 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
           }
         }
       }
-    };
-    Raw<D> even, odd;
-    int page = page_at(s0), page_next = page_at(s0 + 1);
-    fetch(even, page, s0);
-    for (int s = s0; s < s1; s += 2) {
-      const int pos = s * kStep + warp * kUnit;
-      const bool there = page >= 0, there_next = page_next >= 0;
-      fetch(odd, page_next, s + 1);
-      page = page_at(s + 2);
-      use(even, there, pos);
-      if (s + 1 >= s1) break;
-      fetch(even, page, s + 2);
-      page_next = page_at(s + 3);
-      use(odd, there_next, pos + kStep);
     }
 
     // the warps' sums joined.  o[n][i][k]: column (D / 8) g + 2 i + (k >> 1), row
@@ -413,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
         for (int i = 0; i < kDT; ++i)
           *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[n][i][k], o[n][i][k + 2]);
       }
-    __syncthreads();
+    consumers();
     if (tid < kRows) {
       float top = TV_NEG_INF, sum = 0.f;
       for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.m[w][tid]);
@@ -426,11 +461,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       sh.top[tid] = top;
       sh.sum[tid] = sum;
     }
-    __syncthreads();
+    consumers();
     const bool whole = p.whole();
     const float up = pow2i(ev);
     const int slot = 2 * (int)blockIdx.x + (s0 == 0);
-    for (int x = tid; x < kRows * D / 4; x += kThreads) {
+    for (int x = tid; x < kRows * D / 4; x += 32 * kWarps) {
       const int row = x / (D / 4), col = x % (D / 4) * 4;
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int w = 0; w < kWarps; ++w) {
@@ -451,23 +486,25 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       float2* const stats = reinterpret_cast<float2*>(a.part + (size_t)2 * gridDim.x * kRows * D);
       if (tid < kRows) stats[(size_t)slot * kRows + tid] = make_float2(sh.top[tid], sh.sum[tid]);
       // pieces lie in the CTAs from the one with the item's first step to that with its last
-      const int c0 = sh.shares.owner(p.first), c1 = sh.shares.owner(p.first + p.steps - 1);
+      const int c0 = shares.owner(p.first), c1 = shares.owner(p.first + p.steps - 1);
       __threadfence();
-      __syncthreads();
+      consumers();
       if (tid == 0) {
         const int seen = atomicAdd(&a.counters[c0], 1);
         sh.last = seen == c1 - c0;
         if (sh.last) a.counters[c0] = 0;
       }
-      __syncthreads();
+      consumers();
       if (sh.last) {
         __threadfence();
-        for (int x = tid; x < kRows * D / 4; x += kThreads) {
+        for (int x = tid; x < kRows * D / 4; x += 32 * kWarps) {
           const int row = x / (D / 4), col = x % (D / 4) * 4;
           float top = TV_NEG_INF, sum = 0.f;
+#pragma unroll 8
           for (int c = c0; c <= c1; ++c)
             top = fmaxf(top, __ldcg(&stats[(size_t)(2 * c + (c == c0)) * kRows + row]).x);
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
           for (int c = c0; c <= c1; ++c) {
             const size_t at = 2 * c + (c == c0);
             const float2 ms = __ldcg(&stats[at * kRows + row]);
@@ -484,14 +521,15 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
         }
       }
     }
-    __syncthreads();
+    consumers();
   }
-  zero_rows(a, D, blockIdx.x * kWarps + warp, gridDim.x * kWarps);
+  if (bad && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_TIMEOUT);
 }
 
 template <int D, int NT>
 int launch(const AttendArgs& a, int sm_count, cudaStream_t stream) {
-  const size_t smem = sizeof(Shared) + (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
+  const size_t smem = sizeof(Shared) + kRing<D> * (size_t)kStepBytes<D> +
+                      (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
   if (cudaFuncSetAttribute(attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            (int)smem) != cudaSuccess) {
     cudaGetLastError();

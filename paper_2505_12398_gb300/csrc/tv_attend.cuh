@@ -12,6 +12,7 @@
 #include "tv_cache.cuh"
 #include "tv_device.cuh"
 #include "tv_launch.h"
+#include "tv_ptx.cuh"
 
 namespace tvk {
 namespace attend {
@@ -243,6 +244,11 @@ struct QueryScale {
     return finite ? f : __int_as_float(0x7fffffff);
   }
 };
+
+// Waits for a phase of a barrier, unless an earlier wait gave up; `bad` becomes 1 if this does.
+__device__ __forceinline__ void wait_on(uint64_t* bar, uint32_t parity, uint32_t& bad) {
+  if (!mbar_try_wait(bar, parity) && !bad) bad = mbar_wait(bar, parity) ? 0u : 1u;
+}
 
 // Four columns of row m (of M) of a (request, head), sums y over weights that sum to `sum`.
 __device__ __forceinline__ void store_out(const AttendArgs& a, int b, int head, int m, int M,

@@ -69,12 +69,12 @@ struct Work {
   int more, b, head, m0, s0, s1, steps, tokens, len, rows;
   __device__ __forceinline__ bool whole() const { return s0 == 0 && s1 == steps; }
 };
-constexpr int kWorkSlots = 4;
+constexpr int kPieceSlots = 4;
 constexpr int kTakers = 2 + kWidenWarps + 2;       // (of the softmax one of each tile)
 
 struct TileShared {
-  uint64_t given[kWorkSlots], taken[kWorkSlots];
-  Work work[kWorkSlots];
+  uint64_t given[kPieceSlots], taken[kPieceSlots];
+  Work work[kPieceSlots];
   Work now[2][2];                                // [tile][piece % 2], the softmax's
   uint64_t kfull[kStages], kempty[kStages], vfull[kStages], vempty[kStages];
   uint64_t sfull[2], pfull[2][2], ofull[2][2];   // [tile][half of the tokens]
@@ -97,20 +97,16 @@ __device__ __forceinline__ void regs_more() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs));
 }
 
-__device__ __forceinline__ void wait_on(uint64_t* bar, uint32_t parity, uint32_t& bad) {
-  if (!mbar_try_wait(bar, parity) && !bad) bad = mbar_wait(bar, parity) ? 0u : 1u;
-}
-
 // The n-th piece.  Whether there is one is only one thread's or one warp's to say: after a
 // wait that gave up others may see something else.
 __device__ __forceinline__ const Work* take(TileShared& sh, uint32_t n, uint32_t& bad) {
-  wait_on(&sh.given[n % kWorkSlots], (n / kWorkSlots) & 1, bad);
-  const Work* const w = &sh.work[n % kWorkSlots];
+  wait_on(&sh.given[n % kPieceSlots], (n / kPieceSlots) & 1, bad);
+  const Work* const w = &sh.work[n % kPieceSlots];
   return __all_sync(0xffffffffu, !bad && w->more) ? w : nullptr;
 }
 __device__ __forceinline__ void give_back(TileShared& sh, uint32_t n) {
   __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.taken[n % kWorkSlots]);
+  if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.taken[n % kPieceSlots]);
 }
 
 // Descriptors of operands whose rows are 128 bytes with the 128-byte swizzle, in two words:
@@ -327,7 +323,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       mbar_init(&sh.qfull[x], split ? kSoftmaxWarps : kSoftmaxWarps / 2);
     }
     mbar_init(&sh.merge, kSoftmaxWarps);
-    for (int i = 0; i < kWorkSlots; ++i) {
+    for (int i = 0; i < kPieceSlots; ++i) {
       mbar_init(&sh.given[i], 1);
       mbar_init(&sh.taken[i], kTakers);
     }
@@ -401,15 +397,15 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       Piece p;
       Split split_item = {-1, 0, 0, 0};
       for (uint32_t n = 0;; ++n) {
-        wait_on(&sh.taken[n % kWorkSlots], ((n / kWorkSlots) & 1) ^ 1, bad);
+        wait_on(&sh.taken[n % kPieceSlots], ((n / kPieceSlots) & 1) ^ 1, bad);
         Work w = {};
         if (!bad && walker.next(a, rows_of_item, p)) {
           w = Work{1, p.b, p.head, p.m0, p.s0, p.s1, p.steps, p.tokens, p.rq.len, p.rq.rows};
           if (p.s0 == 0 && p.s1 < p.steps)
             split_item = Split{p.b, p.head, p.m0, shares.owner(p.first + p.steps - 1)};
         }
-        sh.work[n % kWorkSlots] = w;
-        mbar_arrive(&sh.given[n % kWorkSlots]);
+        sh.work[n % kPieceSlots] = w;
+        mbar_arrive(&sh.given[n % kPieceSlots]);
         if (!w.more) break;
       }
       splits_of(a, D, gridDim.x)[blockIdx.x] = split_item;
@@ -465,7 +461,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       if ((warp & 3) == 0) {
         const bool more = take(sh, taken, bad) != nullptr;
         if (lane == 0) {
-          w = sh.work[taken % kWorkSlots];
+          w = sh.work[taken % kPieceSlots];
           w.more = more;
         }
         give_back(sh, taken);
