@@ -138,7 +138,7 @@ struct Schedule {
 // The steps of all requests, and a walker over those of CTA `cta` of at most `ctas`.  By all
 // threads of the block; has a barrier of it.
 __device__ __forceinline__ Shares plan(const AttendArgs& a, Schedule& sh, int tile, int cta,
-                                       int ctas, Walker& w) {
+                                       int ctas, float pieces_per_step, Walker& w) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = blockDim.x;
   const int per = (a.B + n - 1) / n;
   long long mine = 0;
@@ -159,7 +159,13 @@ __device__ __forceinline__ Shares plan(const AttendArgs& a, Schedule& sh, int ti
   }
   Shares s;
   s.total = total;
-  s.ctas = min((long long)ctas, total);
+  // `pieces_per_step`: of how many pieces the joining takes as long as a step.  Of an item of S
+  // steps a CTA then takes sqrt(S / pieces_per_step) at least, where steps and joining together
+  // are shortest.
+  const long long items =
+      (long long)a.B * a.c.kv_heads * (((long long)a.R * a.group + tile - 1) / tile);
+  const int least = max((int)sqrtf((float)(total / items) / pieces_per_step), 1);
+  s.ctas = min((long long)ctas, (total + least - 1) / least);
   w.cur = cta < s.ctas ? s.begin(cta) : 0;
   w.end = cta < s.ctas ? s.begin(cta + 1) : 0;
   if (w.cur < w.end && w.cur >= before && w.cur < before + mine) {
