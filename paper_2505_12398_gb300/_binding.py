@@ -644,6 +644,7 @@ class KVCache:
             raise ValueError(f"page_size: expected 16, 32, 64 or 128, got {page_size}")
         if min(layers, pages, kv_heads) < 1:
             raise ValueError("layers, pages and kv_heads: expected at least one of each")
+        self.torch = torch                       # (an import statement a call costs 0.3 us each)
         self.verifier, self.device = verifier, verifier.device
         self.layers, self.pages, self.kv_heads = layers, pages, kv_heads
         self.head_dim, self.page_size = head_dim, page_size
@@ -665,18 +666,16 @@ class KVCache:
 
     def _table(self, lengths, table, B):
         """The number of pages in a row of a page table that is one."""
-        import torch
         n = table.shape[1] if table.dim() == 2 else -1
-        _check_in(lengths, torch.int32, (B,), self.device, "lengths")
-        _check_in(table, torch.int32, (B, n), self.device, "table")
+        _check_in(lengths, self.torch.int32, (B,), self.device, "lengths")
+        _check_in(table, self.torch.int32, (B, n), self.device, "table")
         return n
 
     def _kind(self, dtype):
-        import torch
-        if dtype in ("bf16", torch.bfloat16):
-            return TV_BF16, torch.bfloat16
-        if dtype in ("fp32", torch.float32):
-            return TV_FP32, torch.float32
+        if dtype in ("bf16", self.torch.bfloat16):
+            return TV_BF16, self.torch.bfloat16
+        if dtype in ("fp32", self.torch.float32):
+            return TV_FP32, self.torch.float32
         raise ValueError(f"dtype: expected bf16 or fp32, got {dtype}")
 
     def write(self, layer, k, v, lengths, table, rows=None, stream=None):
@@ -684,7 +683,6 @@ class KVCache:
         positions behind what is cached, row i of request b at lengths[b] + i; ``rows`` [B]
         int32 gives the rows of each request (default: all R).  Lengths do not change
         (tv_cache_write)."""
-        import torch
         B, R = k.shape[:2]
         code = self.verifier._float_code(k, "k")
         shape = (B, R, self.kv_heads, self.head_dim)
@@ -692,7 +690,7 @@ class KVCache:
         _check_in(v, k.dtype, shape, self.device, "v")
         n = self._table(lengths, table, B)
         if rows is not None:
-            _check_in(rows, torch.int32, (B,), self.device, "rows")
+            _check_in(rows, self.torch.int32, (B,), self.device, "rows")
         self._call("tv_cache_write", layer, B, R, code, k.data_ptr(), v.data_ptr(),
                    lengths.data_ptr(), table.data_ptr(), n, _at(rows),
                    self.verifier._stream(stream))
@@ -701,12 +699,11 @@ class KVCache:
         """Keys and values [B, n, kv_heads, head_dim] of positions first[b] + i < lengths[b]
         (``first`` [B] int32, default 0), zeros behind the last (tv_cache_read).  ``out`` =
         (k, v) to write into."""
-        import torch
         B = lengths.shape[0]
         pages = self._table(lengths, table, B)
         code, kind = self._kind(dtype)
         if first is not None:
-            _check_in(first, torch.int32, (B,), self.device, "first")
+            _check_in(first, self.torch.int32, (B,), self.device, "first")
         shape = (B, n, self.kv_heads, self.head_dim)
         k, v = self.verifier._empty(stream, (shape, kind), (shape, kind)) if out is None else out
         if out is not None:
@@ -725,19 +722,18 @@ class KVCache:
         gives the rows of each request (the output's others are 0), ``scale`` the factor of the
         scores (default head_dim ** -0.5).  heads is a multiple of kv_heads, whose query heads
         lie together (tv_tree_attention)."""
-        import torch
         B, R, heads = q.shape[:3]
         shape = (B, R, heads, self.head_dim)
-        _check_in(q, torch.bfloat16, shape, self.device, "q")
+        _check_in(q, self.torch.bfloat16, shape, self.device, "q")
         n = self._table(lengths, table, B)
         if parents is not None:
-            _check_in(parents, torch.int32, (B, R), self.device, "parents")
+            _check_in(parents, self.torch.int32, (B, R), self.device, "parents")
         if rows is not None:
-            _check_in(rows, torch.int32, (B,), self.device, "rows")
+            _check_in(rows, self.torch.int32, (B,), self.device, "rows")
         if out is None:
-            out, = self.verifier._empty(stream, (shape, torch.bfloat16))
+            out, = self.verifier._empty(stream, (shape, self.torch.bfloat16))
         else:
-            _check_out(out, torch.bfloat16, shape, self.device)
+            _check_out(out, self.torch.bfloat16, shape, self.device)
         self._call("tv_tree_attention", layer, B, R, heads, q.data_ptr(), lengths.data_ptr(),
                    table.data_ptr(), n, _at(parents), _at(rows),
                    float(scale) if scale is not None else self.head_dim ** -0.5,
@@ -749,15 +745,14 @@ class KVCache:
         every layer, the accepted nodes' rows behind the root's and returns the new lengths
         lengths + 1 + tau (tv_cache_accept); a tree marked invalid keeps its length.
         ``out`` [B] int32 to write them into, not ``lengths`` itself."""
-        import torch
         B, N = path.shape
-        _check_in(path, torch.int32, (B, N), self.device, "path")
-        _check_in(tau, torch.int32, (B,), self.device, "tau")
+        _check_in(path, self.torch.int32, (B, N), self.device, "path")
+        _check_in(tau, self.torch.int32, (B,), self.device, "tau")
         n = self._table(lengths, table, B)
         if out is None:
-            out, = self.verifier._empty(stream, ((B,), torch.int32))
+            out, = self.verifier._empty(stream, ((B,), self.torch.int32))
         else:
-            _check_out(out, torch.int32, (B,), self.device)
+            _check_out(out, self.torch.int32, (B,), self.device)
         self._call("tv_cache_accept", B, N, lengths.data_ptr(), table.data_ptr(), n,
                    path.data_ptr(), tau.data_ptr(), out.data_ptr(),
                    self.verifier._stream(stream))

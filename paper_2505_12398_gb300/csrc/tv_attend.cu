@@ -532,11 +532,8 @@ template <int D, int NT>
 int launch(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const size_t smem = sizeof(Shared) + kRing<D> * (size_t)kStepBytes<D> +
                       (size_t)kWarps * 8 * NT * (D + 4) * sizeof(float);
-  if (cudaFuncSetAttribute(attend_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)smem) != cudaSuccess) {
-    cudaGetLastError();
-    return -5;
-  }
+  static std::atomic<uint64_t> allowed{0};
+  if (!allow_smem(attend_kernel<D, NT>, smem, allowed)) return -5;
   attend_kernel<D, NT><<<kPerSm * sm_count, kThreads, smem, stream>>>(a);
   return cudaGetLastError() == cudaSuccess ? 0 : -5;
 }

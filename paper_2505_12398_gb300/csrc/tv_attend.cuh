@@ -8,6 +8,8 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/tv.h"
 #include "tv_cache.cuh"
 #include "tv_device.cuh"
@@ -254,6 +256,23 @@ struct QueryScale {
 // Waits for a phase of a barrier, unless an earlier wait gave up; `bad` becomes 1 if this does.
 __device__ __forceinline__ void wait_on(uint64_t* bar, uint32_t parity, uint32_t& bad) {
   if (!mbar_try_wait(bar, parity) && !bad) bad = mbar_wait(bar, parity) ? 0u : 1u;
+}
+
+// Lets a kernel of this device take that much shared memory, once (a call costs the host 1 us).
+// `done` is the kernel's own: bit i for device i.
+template <typename K>
+bool allow_smem(K kernel, size_t bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return false;
+  const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+  if (bit && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) !=
+      cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
 }
 
 // Four columns of row m (of M) of a (request, head), sums y over weights that sum to `sum`.

@@ -805,11 +805,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int split, int 
 template <int D>
 int launch_tiles(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const size_t smem = (size_t)(2 + 2 * kStages) * kTile * D * 2 + 1024;
-  if (cudaFuncSetAttribute(tile_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           (int)smem) != cudaSuccess) {
-    cudaGetLastError();
-    return -5;
-  }
+  static std::atomic<uint64_t> allowed{0};
+  if (!allow_smem(tile_kernel<D>, smem, allowed)) return -5;
   const int split = (long long)a.R * a.group <= kTile;
   const int wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   tile_kernel<D><<<sm_count, kTileThreads, smem, stream>>>(a, split, wide);

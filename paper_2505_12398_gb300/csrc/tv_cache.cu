@@ -13,9 +13,11 @@
 // of the division.
 //
 // Bound by the bytes of the rows that are not quantised.  A warp takes 8 consecutive
-// positions, aligned to 8 so that they lie in one page, and 4 chunks of 32 columns: it
-// loads (or stores) 256 consecutive bytes of bf16 of a row, and the codes of a chunk's 8
-// positions are 128 consecutive bytes.
+// positions, aligned to 8 so that they lie in one page, 4 lanes for each: a lane loads 16
+// columns, the four whole lines of a row, or stores 32 bytes, the four a line; the codes of a
+// chunk's 8 positions are 128 consecutive bytes.  (With a chunk of 32 columns for each lane the
+// stores of fp32 rows went to 32 lines at once, and the kernel was bound by L1: 226 us for ...
+// at 32 requests of 4096 rows of 8 heads.)
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -32,63 +34,59 @@ namespace cache {
 constexpr int kWarps = 8;
 constexpr int kSpan = 8;                 // positions of a warp
 
-// 32 consecutive elements as float32, 16-byte aligned.
-__device__ __forceinline__ void load32(const __nv_bfloat16* p, float (&x)[32]) {
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// 16 consecutive elements, 16-byte aligned, as they come.
+template <typename T>
+struct Row16 {
+  uint4 v[sizeof(T)];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 u = reinterpret_cast<const uint4*>(p)[i];
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  }
+  // as float32
+  __device__ __forceinline__ void widen(float (&x)[16]) const {
+    const uint32_t* const w = reinterpret_cast<const uint32_t*>(v);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[8 * i + 2 * j] = bf16_lo(w[j]);
-      x[8 * i + 2 * j + 1] = bf16_hi(w[j]);
+    for (int i = 0; i < 16; ++i) {
+      if constexpr (sizeof(T) == 2)
+        x[i] = i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+      else
+        x[i] = __uint_as_float(w[i]);
     }
   }
-}
-__device__ __forceinline__ void load32(const float* p, float (&x)[32]) {
+  // the largest magnitude, NaN if one is
+  __device__ __forceinline__ float top() const {
+    const uint32_t* const w = reinterpret_cast<const uint32_t*>(v);
+    if constexpr (sizeof(T) == 2) {
+      uint32_t m = w[0] & 0x7fff7fffu;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float4 u = reinterpret_cast<const float4*>(p)[i];
-    x[4 * i] = u.x;
-    x[4 * i + 1] = u.y;
-    x[4 * i + 2] = u.z;
-    x[4 * i + 3] = u.w;
+      for (int i = 1; i < 8; ++i)
+        asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i] & 0x7fff7fffu));
+      return max_nan(bf16_lo(m), bf16_hi(m));
+    } else {
+      float m = fabsf(__uint_as_float(w[0]));
+#pragma unroll
+      for (int i = 1; i < 16; ++i) m = max_nan(m, fabsf(__uint_as_float(w[i])));
+      return m;
+    }
   }
-}
-// Stores words in pieces of 32 bytes (a 16-byte store writes half a sector) or 16.
-template <int N>
-__device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[N], bool wide) {
+};
+// Stores 32 bytes (a 16-byte store writes half a sector), or twice 16.
+__device__ __forceinline__ void store_words(void* p, const uint32_t (&w)[8], bool wide) {
   if (wide) {
-#pragma unroll
-    for (int i = 0; i < N; i += 8)
-      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
-                       static_cast<uint32_t*>(p) + i),
-                   "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]),
-                   "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
-                   : "memory");
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]),
+                 "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
   } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4)
-      reinterpret_cast<uint4*>(p)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
-__device__ __forceinline__ void pack32(const float (&x)[32], uint32_t (&w)[16]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t*>(&h);
-  }
-}
-__device__ __forceinline__ void pack32(const float (&x)[32], uint32_t (&w)[32]) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i) w[i] = __float_as_uint(x[i]);
-}
-template <typename T>
-struct Words;
-template <>
-struct Words<__nv_bfloat16> { static constexpr int n = 16; };
-template <>
-struct Words<float> { static constexpr int n = 32; };
 
 // Eight values as e2m1 codes, lowest first; magnitudes past 6 become 6.
 __device__ __forceinline__ uint32_t encode8(const float* x) {
@@ -101,115 +99,126 @@ __device__ __forceinline__ uint32_t encode8(const float* x) {
       : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
   return w;
 }
-// The quotient y / s that e2m1 rounds (see above); inv = 1 / s.
-__device__ __forceinline__ float quotient(float y, float, float inv, __nv_bfloat16) {
-  return __uint_as_float((__float_as_uint(y * inv) + 0x400u) & 0xfffff800u);
+// The quotient x / unit that e2m1 rounds (see above), unit = s G and inv = 1 / unit.
+__device__ __forceinline__ float quotient(float x, float, float inv, __nv_bfloat16) {
+  return __uint_as_float((__float_as_uint(x * inv) + 0x400u) & 0xfffff800u);
 }
-__device__ __forceinline__ float quotient(float y, float s, float, float) {
-  return __fdiv_rn(y, s);
+__device__ __forceinline__ float quotient(float x, float unit, float, float) {
+  return __fdiv_rn(x, unit);
 }
 
-// What one lane of a warp works on: chunk `at` of the row's 2 * kv_heads * d / 32 (keys
-// first), its head and side.
+// Which request, span of positions and first of kPer strips a warp works on: a strip is kCols
+// columns for each of a row's 4 lanes.  A request has whole blocks, so that one division by their
+// number is all that its index takes.
+template <int kCols, int kPer>
+struct Part {
+  int b, span, strip, strips;
+  __device__ __forceinline__ Part(const CacheArgs& c, int spans, int blocks) {
+    strips = 2 * c.kv_heads * c.head_dim / (4 * kCols);
+    const int groups = (strips + kPer - 1) / kPer;
+    b = (int)(blockIdx.x / (unsigned)blocks);
+    const int i = (int)(blockIdx.x - (unsigned)b * blocks) * kWarps + (int)(threadIdx.x >> 5);
+    span = i / groups;
+    strip = (i - span * groups) * kPer;
+    if (span >= spans) span = -1;
+  }
+};
+// Where a column of the 2 * kv_heads * head_dim of a row (keys first) is.
 struct Where {
-  int side, head, chunk;
-  __device__ __forceinline__ Where(const CacheArgs& c, int at) {
-    const int chunks = c.head_dim / kChunk32;
-    chunk = at % chunks;
-    at /= chunks;
-    side = at >= c.kv_heads;
-    head = at - side * c.kv_heads;
+  int side, head, col;
+  __device__ __forceinline__ Where(const CacheArgs& c, int x) {
+    const int shift = c.head_dim == 128 ? 7 : 6;
+    head = x >> shift;
+    col = x & (c.head_dim - 1);
+    side = head >= c.kv_heads;
+    head -= side * c.kv_heads;
   }
 };
 
-template <typename T>
+template <typename T, int kPer>
 __global__ void __launch_bounds__(32 * kWarps)
-    write_kernel(CacheArgs c, PageTable t, int layer, int B, int R, int spans,
+    write_kernel(CacheArgs c, PageTable t, int layer, int R, int spans, int blocks,
                  const T* __restrict__ k, const T* __restrict__ v,
                  const int32_t* __restrict__ rows, uint32_t* status) {
-  const int quads = 2 * c.kv_heads * (c.head_dim / kChunk32) / 4;
-  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
-  const int q = (int)(w % quads);
-  const int span = (int)(w / quads % spans);
-  const int b = (int)(w / quads / spans);
-  if (b >= B) return;
+  const Part<kGroup, kPer> part(c, spans, blocks);
+  if (part.span < 0) return;
+  const int b = part.b;
   const int len = t.lengths[b];
   const int want = rows ? rows[b] : R, r = min(max(want, 0), R);
   if (len < 0 || want != r) {
-    if (span == 0 && q == 0 && lane == 0) atomicOr(status, (uint32_t)TV_STATUS_BAD_LENGTH);
+    if (part.span == 0 && part.strip == 0 && lane == 0)
+      atomicOr(status, (uint32_t)TV_STATUS_BAD_LENGTH);
     if (len < 0) return;
   }
-  const int off = span * kSpan - (len & (kSpan - 1));       // of the span's first position
+  const int off = part.span * kSpan - (len & (kSpan - 1));  // of the span's first position
   if (off >= r) return;
   const int i = off + (lane >> 2);                          // this lane's row
+  const bool mine = i >= 0 && i < r;
+  Row16<T> raw[kPer];
+#pragma unroll
+  for (int n = 0; n < kPer; ++n) {
+    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup);
+    if (mine && part.strip + n < part.strips)
+      raw[n].load((at.side ? v : k) + (((size_t)b * R + i) * c.kv_heads + at.head) * c.head_dim +
+                  at.col);
+  }
   const int page = page_of(c, t, b, (int)((unsigned)len + (unsigned)off));   // (the span's)
   if (page < 0) {
     if (lane == 0) atomicOr(status, (uint32_t)TV_STATUS_BAD_PAGE);
     return;
   }
-  if (i < 0 || i >= r) return;
+  if (!mine) return;
   const int slot = (int)((unsigned)len + (unsigned)i) & (c.page_size - 1);
-  const Where at(c, 4 * q + (lane & 3));
-  float x[32];
-  load32((at.side ? v : k) + (((size_t)b * R + i) * c.kv_heads + at.head) * c.head_dim +
-             at.chunk * kChunk32,
-         x);
-  const float down = pow2i(-exponent_of(c, layer, at.side, at.head));
-  uint32_t code[4], scale = 0;
-  bool nan = false;
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    float top = 0.f;
+  for (int n = 0; n < kPer; ++n) {
+    if (part.strip + n >= part.strips) break;
+    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup);
+    const int e = exponent_of(c, layer, at.side, at.head);
+    float x[kGroup], top = raw[n].top();
+    raw[n].widen(x);
+    if (top != top) {                      // a NaN counts as 0
+      atomicOr(status, (uint32_t)TV_STATUS_NAN);
+      top = 0.f;
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      float& y = x[g * kGroup + j];
-      y *= down;
-      nan |= y != y;
-      y = y != y ? 0.f : y;
-      top = fmaxf(top, fabsf(y));
+      for (int j = 0; j < kGroup; ++j) {
+        x[j] = x[j] != x[j] ? 0.f : x[j];
+        top = fmaxf(top, fabsf(x[j]));
+      }
     }
     uint16_t s8;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;"
         : "=h"(s8)
-        : "f"(0.f), "f"(__fdiv_rn(top, 6.f)));
-    scale |= (uint32_t)s8 << (8 * g);
-    const float s = widen(decode_scales(s8)).x;
-    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+        : "f"(0.f), "f"(__fdiv_rn(top * pow2i(-e), 6.f)));
+    const float unit = widen(decode_scales(s8)).x * pow2i(e);
+    const float inv = s8 ? __fdiv_rn(1.f, unit) : 0.f;
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
-      float& y = x[g * kGroup + j];
-      y = s > 0.f ? quotient(y, s, inv, T()) : 0.f;
-    }
-    code[2 * g] = encode8(x + g * kGroup);
-    code[2 * g + 1] = encode8(x + g * kGroup + 8);
+    for (int j = 0; j < kGroup; ++j) x[j] = s8 ? quotient(x[j], unit, inv, T()) : 0.f;
+    uint8_t* const block = block_of(c, layer, page, at.head, at.side);
+    const size_t piece = (size_t)(at.col / kChunk32) * c.page_size + slot;
+    const int half = (at.col / kGroup) & 1;
+    *reinterpret_cast<uint2*>(block + piece * 16 + 8 * half) =
+        make_uint2(encode8(x), encode8(x + 8));
+    block[(size_t)c.page_size * c.head_dim / 2 + piece * 2 + half] = (uint8_t)s8;
   }
-  uint8_t* const block = block_of(c, layer, page, at.head, at.side);
-  const size_t piece = (size_t)at.chunk * c.page_size + slot;
-  *reinterpret_cast<uint4*>(block + piece * 16) = make_uint4(code[0], code[1], code[2], code[3]);
-  *reinterpret_cast<uint16_t*>(block + (size_t)c.page_size * c.head_dim / 2 + piece * 2) =
-      (uint16_t)scale;
-  if (nan) atomicOr(status, (uint32_t)TV_STATUS_NAN);
 }
 
-template <typename T>
+template <typename T, int kPer>
 __global__ void __launch_bounds__(32 * kWarps)
-    read_kernel(CacheArgs c, PageTable t, int layer, int B, int n, int spans,
+    read_kernel(CacheArgs c, PageTable t, int layer, int n, int spans, int blocks,
                 const int32_t* __restrict__ first, T* __restrict__ k, T* __restrict__ v,
                 int wide, uint32_t* status) {
-  const int quads = 2 * c.kv_heads * (c.head_dim / kChunk32) / 4;
-  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  constexpr int kCols = 32 / (int)sizeof(T);
   const int lane = threadIdx.x & 31;
-  const int q = (int)(w % quads);
-  const int span = (int)(w / quads % spans);
-  const int b = (int)(w / quads / spans);
-  if (b >= B) return;
+  const Part<kCols, kPer> part(c, spans, blocks);
+  if (part.span < 0) return;
+  const int b = part.b;
   const int len = t.lengths[b], from = first ? first[b] : 0;
-  if ((len < 0 || from < 0) && span == 0 && q == 0 && lane == 0)
+  if ((len < 0 || from < 0) && part.span == 0 && part.strip == 0 && lane == 0)
     atomicOr(status, (uint32_t)TV_STATUS_BAD_LENGTH);
   const int start = max(from, 0);
   const int count = min(max(from < 0 ? 0 : len - start, 0), n);       // rows that are read
-  const int off = span * kSpan - (start & (kSpan - 1));
+  const int off = part.span * kSpan - (start & (kSpan - 1));
   const int i = off + (lane >> 2);
   int page = -1;
   if (off < count) {
@@ -217,38 +226,57 @@ __global__ void __launch_bounds__(32 * kWarps)
     if (page < 0 && lane == 0) atomicOr(status, (uint32_t)TV_STATUS_BAD_PAGE);
   }
   if (i < 0 || i >= n) return;
-  const Where at(c, 4 * q + (lane & 3));
-  float x[32];
-  if (page >= 0 && i < count) {
-    const int slot = (int)((unsigned)start + (unsigned)i) & (c.page_size - 1);
-    const uint8_t* const block = block_of(c, layer, page, at.head, at.side);
-    const size_t piece = (size_t)at.chunk * c.page_size + slot;
-    const uint4 code = *reinterpret_cast<const uint4*>(block + piece * 16);
-    const uint32_t s2 = decode_scales(*reinterpret_cast<const uint16_t*>(
-        block + (size_t)c.page_size * c.head_dim / 2 + piece * 2));
+  const bool there = page >= 0 && i < count;
+  const int slot = (int)((unsigned)start + (unsigned)i) & (c.page_size - 1);
+  uint32_t code[kPer][kCols / 8];
+  uint32_t scale[kPer];
+#pragma unroll
+  for (int m = 0; m < kPer; ++m) {
+#pragma unroll
+    for (int j = 0; j < kCols / 8; ++j) code[m][j] = 0;
+    scale[m] = 0;
+    if (there && part.strip + m < part.strips) {
+      const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols);
+      const uint8_t* const block = block_of(c, layer, page, at.head, at.side);
+      const size_t piece = (size_t)(at.col / kChunk32) * c.page_size + slot;
+      const uint8_t* const src = block + piece * 16 + at.col % kChunk32 / 2;
+      if constexpr (kCols == 16) {
+        const uint2 u = *reinterpret_cast<const uint2*>(src);
+        code[m][0] = u.x;
+        code[m][1] = u.y;
+      } else {
+        code[m][0] = *reinterpret_cast<const uint32_t*>(src);
+      }
+      scale[m] = block[(size_t)c.page_size * c.head_dim / 2 + piece * 2 + ((at.col / kGroup) & 1)];
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < kPer; ++m) {
+    if (part.strip + m >= part.strips) break;
+    const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols);
     const float up = pow2i(exponent_of(c, layer, at.side, at.head));
-    const uint32_t words[4] = {code.x, code.y, code.z, code.w};
+    const uint32_t s2 = lo_lo(decode_scales(scale[m]));
+    uint32_t out[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kCols / 8; ++j) {
       uint32_t h[4];
-      decode8(words[j], h);
-      const uint32_t s = j < 2 ? lo_lo(s2) : hi_hi(s2);
+      decode8(code[m][j], h);
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float2 f = widen(mul2(h[m], s));
-        x[8 * j + 2 * m] = f.x * up;
-        x[8 * j + 2 * m + 1] = f.y * up;
+      for (int z = 0; z < 4; ++z) {
+        const float2 f = widen(mul2(h[z], s2));
+        if constexpr (kCols == 16) {
+          const __nv_bfloat162 y = __floats2bfloat162_rn(f.x * up, f.y * up);
+          out[4 * j + z] = *reinterpret_cast<const uint32_t*>(&y);
+        } else {
+          out[2 * z] = __float_as_uint(f.x * up);
+          out[2 * z + 1] = __float_as_uint(f.y * up);
+        }
       }
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[j] = 0.f;
+    store_words((at.side ? v : k) + (((size_t)b * n + i) * c.kv_heads + at.head) * c.head_dim +
+                    at.col,
+                out, wide != 0);
   }
-  uint32_t out[Words<T>::n];
-  pack32(x, out);
-  store_words((at.side ? v : k) + (((size_t)b * n + i) * c.kv_heads + at.head) * c.head_dim +
-                  at.chunk * kChunk32,
-              out, wide != 0);
 }
 
 // One thread for each (layer, head, side, chunk) of a request.  Moves go down (position
@@ -341,10 +369,17 @@ using namespace tvk::cache;
 namespace {
 // Spans of `rows` rows that may start anywhere in one.
 int spans_of(int rows) { return (int)(((long long)rows + 2 * kSpan - 2) / kSpan); }
-long long row_blocks(const CacheArgs& c, int B, int rows) {
-  const long long quads = 2ll * c.kv_heads * (c.head_dim / kChunk32) / 4;
-  const long long per_request = spans_of(rows) * quads;     // below 2^28 * 2^17
-  return ((long long)B * per_request + kWarps - 1) / kWarps;
+// Blocks of a request whose warps take `per` strips of 4 * cols columns each.
+long long row_blocks(const CacheArgs& c, int rows, int cols, int per) {
+  const long long strips = 2ll * c.kv_heads * c.head_dim / (4 * cols);
+  return (spans_of(rows) * ((strips + per - 1) / per) + kWarps - 1) / kWarps;   // below 2^45
+}
+// Strips of a warp: with many warps several, which share what finds their rows and have their
+// loads on the way together; with few one, so that more SMs have some.
+constexpr int kSeveral = 4;
+constexpr long long kManyBlocks = 1024;
+bool several(const CacheArgs& c, int B, int rows, int cols) {
+  return B * row_blocks(c, rows, cols, 1) >= kManyBlocks;
 }
 long long move_blocks(const CacheArgs& c) {                 // of a request; below 2^50
   return ((long long)c.layers * c.kv_heads * 2 * (c.head_dim / kChunk32) + 127) / 128;
@@ -352,42 +387,58 @@ long long move_blocks(const CacheArgs& c) {                 // of a request; bel
 }  // namespace
 
 bool tv_cache_rows_fit(const CacheArgs& c, int B, int R) {
-  const long long quads = 2ll * c.kv_heads * (c.head_dim / kChunk32) / 4;
-  return quads * spans_of(R) <= INT_MAX && row_blocks(c, B, R) <= INT_MAX;
+  const long long most = INT_MAX / kWarps;                  // (a warp's index is an int)
+  const long long blocks = row_blocks(c, R, 8, 1);
+  return blocks <= most && blocks <= INT_MAX / (long long)B;
 }
 bool tv_cache_moves_fit(const CacheArgs& c, int B) {
   return move_blocks(c) <= INT_MAX / (long long)B;
 }
 
+namespace {
+template <typename T, int kPer>
+void launch_write(const CacheArgs& c, const PageTable& t, int layer, int B, int R, const void* k,
+                  const void* v, const int32_t* rows, uint32_t* status, cudaStream_t stream) {
+  const int blocks = (int)row_blocks(c, R, kGroup, kPer);
+  write_kernel<T, kPer><<<(unsigned)B * (unsigned)blocks, 32 * kWarps, 0, stream>>>(
+      c, t, layer, R, spans_of(R), blocks, static_cast<const T*>(k), static_cast<const T*>(v),
+      rows, status);
+}
+template <typename T, int kPer>
+void launch_read(const CacheArgs& c, const PageTable& t, int layer, int B, int n,
+                 const int32_t* first, void* k, void* v, uint32_t* status, cudaStream_t stream) {
+  const int blocks = (int)row_blocks(c, n, 32 / (int)sizeof(T), kPer);
+  const int wide =
+      ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 31u) == 0;
+  read_kernel<T, kPer><<<(unsigned)B * (unsigned)blocks, 32 * kWarps, 0, stream>>>(
+      c, t, layer, n, spans_of(n), blocks, first, static_cast<T*>(k), static_cast<T*>(v), wide,
+      status);
+}
+}  // namespace
+
 int tv_launch_cache_write(const CacheArgs& c, const PageTable& t, int layer, int B, int R,
                           int is_bf16, const void* k, const void* v, const int32_t* rows,
                           uint32_t* status, cudaStream_t stream) {
-  const unsigned blocks = (unsigned)row_blocks(c, B, R);
+  const bool many = several(c, B, R, kGroup);
   if (is_bf16)
-    write_kernel<__nv_bfloat16><<<blocks, 32 * kWarps, 0, stream>>>(
-        c, t, layer, B, R, spans_of(R), static_cast<const __nv_bfloat16*>(k),
-        static_cast<const __nv_bfloat16*>(v), rows, status);
+    many ? launch_write<__nv_bfloat16, kSeveral>(c, t, layer, B, R, k, v, rows, status, stream)
+         : launch_write<__nv_bfloat16, 1>(c, t, layer, B, R, k, v, rows, status, stream);
   else
-    write_kernel<float><<<blocks, 32 * kWarps, 0, stream>>>(
-        c, t, layer, B, R, spans_of(R), static_cast<const float*>(k),
-        static_cast<const float*>(v), rows, status);
+    many ? launch_write<float, kSeveral>(c, t, layer, B, R, k, v, rows, status, stream)
+         : launch_write<float, 1>(c, t, layer, B, R, k, v, rows, status, stream);
   return cudaGetLastError() == cudaSuccess ? 0 : -5;
 }
 
 int tv_launch_cache_read(const CacheArgs& c, const PageTable& t, int layer, int B, int n,
                          int is_bf16, const int32_t* first, void* k, void* v, uint32_t* status,
                          cudaStream_t stream) {
-  const unsigned blocks = (unsigned)row_blocks(c, B, n);
-  const int wide =
-      ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 31u) == 0;
+  const bool many = several(c, B, n, is_bf16 ? 16 : 8);
   if (is_bf16)
-    read_kernel<__nv_bfloat16><<<blocks, 32 * kWarps, 0, stream>>>(
-        c, t, layer, B, n, spans_of(n), first, static_cast<__nv_bfloat16*>(k),
-        static_cast<__nv_bfloat16*>(v), wide, status);
+    many ? launch_read<__nv_bfloat16, kSeveral>(c, t, layer, B, n, first, k, v, status, stream)
+         : launch_read<__nv_bfloat16, 1>(c, t, layer, B, n, first, k, v, status, stream);
   else
-    read_kernel<float><<<blocks, 32 * kWarps, 0, stream>>>(
-        c, t, layer, B, n, spans_of(n), first, static_cast<float*>(k), static_cast<float*>(v),
-        wide, status);
+    many ? launch_read<float, kSeveral>(c, t, layer, B, n, first, k, v, status, stream)
+         : launch_read<float, 1>(c, t, layer, B, n, first, k, v, status, stream);
   return cudaGetLastError() == cudaSuccess ? 0 : -5;
 }
 
