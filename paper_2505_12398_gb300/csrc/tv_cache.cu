@@ -8,9 +8,9 @@
 // quotient a / 6 or y / s rounds to the same 4- or 8-bit value as the exact one: a middle m
 // between two values times the divisor has at most 7 bits, so a quotient that is not m
 // itself is at least ulp(a) / divisor away from it, more than half an ulp of the quotient.
-// In bf16 input that distance is at least 2^-9 of the value, so that y times the rounded 1 / s,
-// rounded to 13 bits (which puts the quotients that are m back on it), serves in place
-// of the division.
+// In bf16 input that distance is at least 2^-9 of the value, 2^-11 for the least middle, 1/4, so
+// that y times the rounded 1 / s, rounded to multiples of 2^-12 (which puts the quotients that are
+// m back on it), serves in place of the division.
 //
 // Bound by the bytes of the rows that are not quantised.  A warp takes 8 consecutive
 // positions, aligned to 8 so that they lie in one page, 4 lanes for each: a lane loads 16
@@ -99,12 +99,24 @@ __device__ __forceinline__ uint32_t encode8(const float* x) {
       : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
   return w;
 }
-// The quotient x / unit that e2m1 rounds (see above), unit = s G and inv = 1 / unit.
-__device__ __forceinline__ float quotient(float x, float, float inv, __nv_bfloat16) {
-  return __uint_as_float((__float_as_uint(x * inv) + 0x400u) & 0xfffff800u);
+// The quotients x / unit that e2m1 rounds (see above), unit = s G, 0 where the scale is 0.
+__device__ __forceinline__ void quotients(float (&x)[16], float unit, __nv_bfloat16) {
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(unit));
+  if (unit == 0.f) inv = 0.f;
+  const float2 ii = make_float2(inv, inv), up = make_float2(2560.f, 2560.f);
+#pragma unroll
+  for (int j = 0; j < 16; j += 2) {        // float32 has 12 bits behind the point at 2560
+    const float2 y = __fadd2_rn(__ffma2_rn(make_float2(x[j], x[j + 1]), ii, up),
+                                make_float2(-2560.f, -2560.f));
+    x[j] = y.x;
+    x[j + 1] = y.y;
+  }
 }
-__device__ __forceinline__ float quotient(float x, float unit, float, float) {
-  return __fdiv_rn(x, unit);
+__device__ __forceinline__ void quotients(float (&x)[16], float unit, float) {
+  if (unit == 0.f) unit = __int_as_float(0x7f800000);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) x[j] = __fdiv_rn(x[j], unit);
 }
 
 // Which request, span of positions and first of kPer strips a warp works on: a strip is kCols
@@ -123,15 +135,22 @@ struct Part {
     if (span >= spans) span = -1;
   }
 };
-// Where a column of the 2 * kv_heads * head_dim of a row (keys first) is.
+// Where a column of the 2 * kv_heads * head_dim of a row (keys first) is: in the keys or values
+// of the row, and in a page, in bytes from its first to the codes and the scale of its 16.
 struct Where {
-  int side, head, col;
-  __device__ __forceinline__ Where(const CacheArgs& c, int x) {
-    const int shift = c.head_dim == 128 ? 7 : 6;
-    head = x >> shift;
-    col = x & (c.head_dim - 1);
-    side = head >= c.kv_heads;
-    head -= side * c.kv_heads;
+  int side, head;
+  uint32_t x, code, scale;
+  __device__ __forceinline__ Where(const CacheArgs& c, int column, int slot) {
+    const uint32_t d = (uint32_t)c.head_dim, width = (uint32_t)c.kv_heads * d;
+    const uint32_t block = (uint32_t)c.page_size * d * 9 / 16;
+    side = (uint32_t)column >= width;
+    x = (uint32_t)column - side * width;
+    head = (int)(x >> (d == 128 ? 7 : 6));
+    const uint32_t col = x & (d - 1);
+    const uint32_t piece = col / kChunk32 * c.page_size + slot;
+    const uint32_t from = (uint32_t)(2 * head + side) * block;       // below 2^31
+    code = from + piece * 16 + col % kChunk32 / 2;
+    scale = from + c.page_size * d / 2 + piece * 2 + (col / kGroup & 1);
   }
 };
 
@@ -155,13 +174,14 @@ __global__ void __launch_bounds__(32 * kWarps)
   if (off >= r) return;
   const int i = off + (lane >> 2);                          // this lane's row
   const bool mine = i >= 0 && i < r;
+  const int slot = (int)((unsigned)len + (unsigned)i) & (c.page_size - 1);
+  const size_t row = ((size_t)b * R + i) * c.kv_heads * c.head_dim;
+  const T *const krow = k + row, *const vrow = v + row;
   Row16<T> raw[kPer];
 #pragma unroll
   for (int n = 0; n < kPer; ++n) {
-    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup);
-    if (mine && part.strip + n < part.strips)
-      raw[n].load((at.side ? v : k) + (((size_t)b * R + i) * c.kv_heads + at.head) * c.head_dim +
-                  at.col);
+    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup, slot);
+    if (mine && part.strip + n < part.strips) raw[n].load((at.side ? vrow : krow) + at.x);
   }
   const int page = page_of(c, t, b, (int)((unsigned)len + (unsigned)off));   // (the span's)
   if (page < 0) {
@@ -169,11 +189,11 @@ __global__ void __launch_bounds__(32 * kWarps)
     return;
   }
   if (!mine) return;
-  const int slot = (int)((unsigned)len + (unsigned)i) & (c.page_size - 1);
+  uint8_t* const dst = block_of(c, layer, page, 0, 0);
 #pragma unroll
   for (int n = 0; n < kPer; ++n) {
     if (part.strip + n >= part.strips) break;
-    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup);
+    const Where at(c, ((part.strip + n) * 4 + (lane & 3)) * kGroup, slot);
     const int e = exponent_of(c, layer, at.side, at.head);
     float x[kGroup], top = raw[n].top();
     raw[n].widen(x);
@@ -190,16 +210,9 @@ __global__ void __launch_bounds__(32 * kWarps)
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;"
         : "=h"(s8)
         : "f"(0.f), "f"(__fdiv_rn(top * pow2i(-e), 6.f)));
-    const float unit = widen(decode_scales(s8)).x * pow2i(e);
-    const float inv = s8 ? __fdiv_rn(1.f, unit) : 0.f;
-#pragma unroll
-    for (int j = 0; j < kGroup; ++j) x[j] = s8 ? quotient(x[j], unit, inv, T()) : 0.f;
-    uint8_t* const block = block_of(c, layer, page, at.head, at.side);
-    const size_t piece = (size_t)(at.col / kChunk32) * c.page_size + slot;
-    const int half = (at.col / kGroup) & 1;
-    *reinterpret_cast<uint2*>(block + piece * 16 + 8 * half) =
-        make_uint2(encode8(x), encode8(x + 8));
-    block[(size_t)c.page_size * c.head_dim / 2 + piece * 2 + half] = (uint8_t)s8;
+    quotients(x, widen(decode_scales(s8)).x * pow2i(e), T());
+    *reinterpret_cast<uint2*>(dst + at.code) = make_uint2(encode8(x), encode8(x + 8));
+    dst[at.scale] = (uint8_t)s8;
   }
 }
 
@@ -228,6 +241,9 @@ __global__ void __launch_bounds__(32 * kWarps)
   if (i < 0 || i >= n) return;
   const bool there = page >= 0 && i < count;
   const int slot = (int)((unsigned)start + (unsigned)i) & (c.page_size - 1);
+  const uint8_t* const src = there ? block_of(c, layer, page, 0, 0) : nullptr;
+  const size_t row = ((size_t)b * n + i) * c.kv_heads * c.head_dim;
+  T *const krow = k + row, *const vrow = v + row;
   uint32_t code[kPer][kCols / 8];
   uint32_t scale[kPer];
 #pragma unroll
@@ -236,24 +252,21 @@ __global__ void __launch_bounds__(32 * kWarps)
     for (int j = 0; j < kCols / 8; ++j) code[m][j] = 0;
     scale[m] = 0;
     if (there && part.strip + m < part.strips) {
-      const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols);
-      const uint8_t* const block = block_of(c, layer, page, at.head, at.side);
-      const size_t piece = (size_t)(at.col / kChunk32) * c.page_size + slot;
-      const uint8_t* const src = block + piece * 16 + at.col % kChunk32 / 2;
+      const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols, slot);
       if constexpr (kCols == 16) {
-        const uint2 u = *reinterpret_cast<const uint2*>(src);
+        const uint2 u = __ldg(reinterpret_cast<const uint2*>(src + at.code));
         code[m][0] = u.x;
         code[m][1] = u.y;
       } else {
-        code[m][0] = *reinterpret_cast<const uint32_t*>(src);
+        code[m][0] = __ldg(reinterpret_cast<const uint32_t*>(src + at.code));
       }
-      scale[m] = block[(size_t)c.page_size * c.head_dim / 2 + piece * 2 + ((at.col / kGroup) & 1)];
+      scale[m] = __ldg(src + at.scale);
     }
   }
 #pragma unroll
   for (int m = 0; m < kPer; ++m) {
     if (part.strip + m >= part.strips) break;
-    const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols);
+    const Where at(c, ((part.strip + m) * 4 + (lane & 3)) * kCols, slot);
     const float up = pow2i(exponent_of(c, layer, at.side, at.head));
     const uint32_t s2 = lo_lo(decode_scales(scale[m]));
     uint32_t out[8];
@@ -273,9 +286,7 @@ __global__ void __launch_bounds__(32 * kWarps)
         }
       }
     }
-    store_words((at.side ? v : k) + (((size_t)b * n + i) * c.kv_heads + at.head) * c.head_dim +
-                    at.col,
-                out, wide != 0);
+    store_words((at.side ? vrow : krow) + at.x, out, wide != 0);
   }
 }
 
