@@ -198,6 +198,14 @@ __device__ __forceinline__ void sts128(uint32_t at, uint32_t a, uint32_t b, uint
                "r"(d)
                : "memory");
 }
+__device__ __forceinline__ uint4 lds128_at(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
 // Where 16-byte piece x (8 columns) of row r of a tile is.
 __device__ __forceinline__ uint32_t piece_at(uint32_t base, int r, int x) {
   return base + (uint32_t)(x >> 3) * kHalfBytes + (uint32_t)r * 128u +
@@ -298,7 +306,7 @@ __device__ __forceinline__ Split* splits_of(const AttendArgs& a, int D, int ctas
 }
 
 template <int D>
-__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int split, int wide) {
+__global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int split) {
   constexpr uint32_t kTileBytes = kTile * D * 2;
   extern __shared__ uint8_t smem_raw[];
   __shared__ TileShared sh;
@@ -472,14 +480,16 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       ++taken;
       return w.more;
     };
-    // this thread's row of queries
-    auto queries = [&]() {
-      const Work& next = sh.now[x][(taken - 1) & 1];
-      const int m = min(next.m0 + (split ? 0 : x * kTile) + r, next.rows * a.group - 1);
+    // A warp's 32 rows of queries come, and its rows of sums go, through its rows of a tile of
+    // queries, so that lanes beside one another have pieces of one row: a row for each lane
+    // takes L1 32 lines at once (5 and 4 thousand clocks a piece, 2 and 2 so).
+    const uint32_t mine = smem_u32(q_tiles) + (uint32_t)x * kTileBytes;
+    const int w0 = (warp & 3) * 32;
+    // rows of all heads before this thread's one of a request
+    auto row_of = [&](const Work& w) {
+      const int m = min(w.m0 + (split ? 0 : x * kTile) + r, w.rows * a.group - 1);
       const int i = m / a.group;
-      return reinterpret_cast<const uint4*>(
-          a.q + (((size_t)next.b * a.R + i) * a.c.kv_heads * a.group +
-                 (size_t)next.head * a.group + (m - i * a.group)) * D);
+      return (i * a.c.kv_heads + w.head) * a.group + (m - i * a.group);
     };
     bool more = take_next();
     while (more) {
@@ -489,16 +499,30 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       const bool in = m < M;
       const int node = in ? m / a.group : 0;
       const bool live = __any_sync(0xffffffffu, in);
+      const int row = row_of(p);
       const int32_t* const parents = sh.parents[x];
       if (a.parents && p.s1 * kStep > len)
         for (int i = r; i < p.rows; i += kTile)
           sh.parents[x][i] = a.parents[(size_t)p.b * a.R + i];
       float f;
       {
+        constexpr int kLanes = D / 8, kRows = 32 / kLanes;
+        const uint4* const src = reinterpret_cast<const uint4*>(a.q) +
+                                 (size_t)p.b * a.R * a.c.kv_heads * a.group * kLanes +
+                                 lane % kLanes;
         uint4 q[D / 8];
-        const uint4* const src = queries();
 #pragma unroll
-        for (int k = 0; k < D / 8; ++k) q[k] = __ldg(src + k);
+        for (int k = 0; k < D / 8; ++k) {        // (32 / kRows = D / 8 loads)
+          const int from = __shfl_sync(0xffffffffu, row, k * kRows + lane / kLanes);
+          q[k] = __ldg(src + (size_t)from * kLanes);
+        }
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k)
+          sts128(piece_at(mine, w0 + k * kRows + lane / kLanes, lane % kLanes), q[k].x, q[k].y,
+                 q[k].z, q[k].w);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < D / 8; ++k) q[k] = lds128_at(piece_at(mine, r, k));
         uint32_t top2 = 0;                       // largest magnitudes of two columns, in bf16
 #pragma unroll
         for (int k = 0; k < D / 8; ++k)
@@ -511,10 +535,9 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         const float up0 = f < 0.f ? -s.up0 : s.up0;        // the factor is made positive,
         f = fabsf(f);
         if (f < 1e-37f || !in) f = 1e-37f;                 // and keeps -inf what it is
-        const uint32_t q_at = smem_u32(q_tiles) + (split ? 0u : (uint32_t)x * kTileBytes);
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) {
-          if (split && k / (D / 16) != x) continue;        // (half of a row's columns each)
+          if (split && x == 1) break;            // (both tiles take the first's)
           const uint32_t u[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
           uint32_t h[4];
 #pragma unroll
@@ -523,7 +546,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
                                                 bf16_hi(u[y]) * up0 * s.up1);
             h[y] = *reinterpret_cast<const uint32_t*>(&z);
           }
-          sts128(piece_at(q_at, r, k), h[0], h[1], h[2], h[3]);
+          sts128(piece_at(mine, r, k), h[0], h[1], h[2], h[3]);
         }
       }
       async_visible();
@@ -641,9 +664,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       // (the next queries on their way to L2 while the sums are stored)
       more = take_next();
       if (more) {
-        const uint4* const src = queries();
+        const Work& next = sh.now[x][(taken - 1) & 1];
+        const __nv_bfloat16* const src =
+            a.q + ((size_t)next.b * a.R * a.c.kv_heads * a.group + row_of(next)) * D;
 #pragma unroll
-        for (int k = 0; k < D / 8; k += 8)
+        for (int k = 0; k < D; k += 64)
           asm volatile("prefetch.global.L2 [%0];" ::"l"(src + k));
       }
 
@@ -668,7 +693,10 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
         const float inv = !whole ? 1.f
                           : l == 0.f ? 0.f
                                      : pow2i(exponent_of(a.c, a.layer, 1, p.head)) / l;
-        const size_t row = (2 * (size_t)blockIdx.x + (p.s0 == 0)) * 2 * kTile + (m - p.m0);
+        // the warp's first row among the CTA's pieces' rows, and its rows that there are
+        const size_t part0 = (2 * (size_t)blockIdx.x + (p.s0 == 0)) * 2 * kTile +
+                             (split ? 0 : x * kTile) + w0;
+        const int rows = min(M - (m - lane), 32);
         fac[0] *= inv;
         fac[1] *= inv;
         // (split: of both tiles' sums half of the columns each)
@@ -695,34 +723,48 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             }
           }
           if (whole) {
-            uint32_t w[16];
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(c[2 * y]),
-                                                             __uint_as_float(c[2 * y + 1]));
-              w[y] = *reinterpret_cast<const uint32_t*>(&h);
-            }
-            if (in) {
-              __nv_bfloat16* const dst =
-                  a.out + (((size_t)p.b * a.R + node) * a.c.kv_heads * a.group +
-                           (size_t)p.head * a.group + m % a.group) * D + col;
-              if (wide) {
-                st_global_32b(dst, w);
-                st_global_32b(dst + 16, w + 8);
-              } else {
+            for (int z = 0; z < 4; ++z) {
+              uint32_t w[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y)
-                  reinterpret_cast<uint4*>(dst)[y] =
-                      make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+              for (int y = 0; y < 4; ++y) {
+                const __nv_bfloat162 h =
+                    __floats2bfloat162_rn(__uint_as_float(c[8 * z + 2 * y]),
+                                          __uint_as_float(c[8 * z + 2 * y + 1]));
+                w[y] = *reinterpret_cast<const uint32_t*>(&h);
               }
+              sts128(piece_at(mine, r, col / 8 + z), w[0], w[1], w[2], w[3]);
             }
-          } else if (in) {
+          } else {                               // 32 sums of a row, 8 lanes a row
 #pragma unroll
-            for (int y = 0; y < 32; y += 8) st_global_32b(a.part + row * D + col + y, c + y);
+            for (int z = 0; z < 8; ++z)
+              sts128(piece_at(mine, r, z), c[4 * z], c[4 * z + 1], c[4 * z + 2], c[4 * z + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              const int to_row = k + lane / 8;
+              const uint4 v = lds128_at(piece_at(mine, w0 + to_row, lane % 8));
+              if (to_row < rows)
+                *reinterpret_cast<uint4*>(a.part + (part0 + to_row) * D + col + lane % 8 * 4) = v;
+            }
+            __syncwarp();
           }
         }
+        if (whole) {
+          __syncwarp();
+          const int pieces = (c1 - c0) / 8, per = 32 / pieces, at = lane % pieces;
+          uint4* const dst = reinterpret_cast<uint4*>(a.out) +
+                             (size_t)p.b * a.R * a.c.kv_heads * a.group * (D / 8) + c0 / 8 + at;
+          for (int k = 0; k < 32; k += per) {
+            const int to_row = k + lane / pieces;
+            const int from = __shfl_sync(0xffffffffu, row, to_row);
+            const uint4 v = lds128_at(piece_at(mine, w0 + to_row, c0 / 8 + at));
+            if (to_row < rows) dst[(size_t)from * (D / 8)] = v;
+          }
+          __syncwarp();
+        }
         if (!whole && !(split && x == 1) && in)
-          stats_of(a, D, gridDim.x)[row] = make_float2(mref, l);
+          stats_of(a, D, gridDim.x)[part0 + lane] = make_float2(mref, l);
       }
       tc_fence_before();
       if (split) {                               // both tiles' sums may be overwritten
@@ -808,8 +850,7 @@ int launch_tiles(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   static std::atomic<uint64_t> allowed{0};
   if (!allow_smem(tile_kernel<D>, smem, allowed)) return -5;
   const int split = (long long)a.R * a.group <= kTile;
-  const int wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
-  tile_kernel<D><<<sm_count, kTileThreads, smem, stream>>>(a, split, wide);
+  tile_kernel<D><<<sm_count, kTileThreads, smem, stream>>>(a, split);
   cudaLaunchAttribute early;
   early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   early.val.programmaticStreamSerializationAllowed = 1;
