@@ -12,11 +12,12 @@ A ``Verifier`` also has the steps on either side: drafting, the target's final n
 head (bf16, or e4m3 with block scales), and penalties, biases and grammar masks on the
 tree's logits, for which a ``TokenContext`` holds what the requests' texts add up to.  A
 ``KVCache`` is the target's key/value cache in 4 bits: its rows are quantised as they are
-written, read back, and moved after a verification.
+written, read back, moved after a verification, and attended by trees, prompts and single
+tokens.
 """
 
 from ._binding import (PATH_FLAGS, TV_BF16, TV_FP32, TV_STATUS, KVCache, LibraryError,
                        TokenContext, Verifier, library, library_path, status_names)
 
-__all__ = ["Verifier", "TokenContext", "KVCache", "library", "library_path", "LibraryError", "PATH_FLAGS",
-           "TV_BF16", "TV_FP32", "TV_STATUS", "status_names"]
+__all__ = ["Verifier", "TokenContext", "KVCache", "library", "library_path", "LibraryError",
+           "PATH_FLAGS", "TV_BF16", "TV_FP32", "TV_STATUS", "status_names"]

@@ -43,8 +43,6 @@
 namespace tvk {
 namespace attend {
 
-
-
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * (kWarps + 1);      // and the copying warp
 constexpr int kUnit = 16;                        // tokens of a warp's step
@@ -173,11 +171,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       Piece& p = sh.pieces[n % kWorkSlots];
       if (lane == 0) {
         wait_on(&sh.taken[n % kWorkSlots], ((n / kWorkSlots) & 1) ^ 1, bad);
-        sh.more[n % kWorkSlots] = !bad && walker.next(a, kRows, p);
+        sh.more[n % kWorkSlots] = bad ? -1 : walker.next(a, kRows, p);
         mbar_arrive(&sh.given[n % kWorkSlots]);
       }
       __syncwarp();
-      if (!sh.more[n % kWorkSlots]) break;
+      if (sh.more[n % kWorkSlots] <= 0) break;
       const int b = p.b, s0 = p.s0, s1 = p.s1, tokens = p.tokens;
       const uint8_t* const blocks =
           a.c.data + ((size_t)a.layer * a.c.pages * H + p.head) * block2;
@@ -191,10 +189,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       int page = page_at(s0), page_next = page_at(s0 + 1);
       for (int s = s0; s < s1; ++s, ++count) {
         const uint32_t stage = count % kRing<D>;
-        const bool there = (unsigned)page < (unsigned)a.c.pages;
+        bool there = (unsigned)page < (unsigned)a.c.pages;
         if (!there && page != -2) atomicOr(a.status, (uint32_t)TV_STATUS_BAD_PAGE);
-        const uint32_t valid = __ballot_sync(0xffffffffu, there);
         wait_on(&sh.empty[stage], ((count / kRing<D>) & 1) ^ 1, bad);
+        const bool gave_up = __any_sync(0xffffffffu, bad != 0);
+        there = there && !gave_up;               // (copied to what is free only)
+        const uint32_t valid = __ballot_sync(0xffffffffu, there);
         if (lane == 0) {
           sh.valid[stage] = valid;
           mbar_arrive_expect_tx(&sh.full[stage], (uint32_t)__popc(valid) * block2);
@@ -208,16 +208,20 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       }
     }
     zero_rows(a, D, blockIdx.x, gridDim.x);
+    // (no copy is on its way when the CTA ends, although a warp that gave up may not have waited)
+    for (uint32_t i = count - min(count, (uint32_t)kRing<D>); i < count; ++i)
+      if (!mbar_wait(&sh.full[i % kRing<D>], (i / kRing<D>) & 1)) bad = 1;
     if (bad && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_TIMEOUT);
     return;
   }
 
   const Lane<D> at(a.c, warp, lane);
-  uint32_t count = 0;
-  for (uint32_t n = 0;; ++n) {
+  uint32_t count = 0, n = 0;
+  for (;; ++n) {
     if (tid == 0) {                              // (the others meet at barriers)
       wait_on(&sh.given[n % kWorkSlots], (n / kWorkSlots) & 1, bad);
-      sh.going[n & 1] = !bad && sh.more[n % kWorkSlots];
+      if (sh.more[n % kWorkSlots] < 0) bad = 1;
+      sh.going[n & 1] = !bad && sh.more[n % kWorkSlots] > 0;
       sh.now[n & 1] = sh.pieces[n % kWorkSlots];
       mbar_arrive(&sh.taken[n % kWorkSlots]);
     }
@@ -293,6 +297,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       wait_on(&sh.full[stage], (count / kRing<D>) & 1, bad);
       const bool there = sh.valid[stage] >> at.page & 1;
       if (!there) {
+        __syncwarp();                            // (all lanes have read which pages there are)
         if (lane == 0) mbar_arrive(&sh.empty[stage]);
         continue;
       }
@@ -524,6 +529,18 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
       }
     }
     consumers();
+  }
+  // after a wait that gave up the pieces that are left arrive all the same, so that the counters
+  // are 0 for the next call
+  if (bad && tid == 0 && (long long)blockIdx.x < shares.ctas) {
+    Walker w = {sh.plan.request, sh.plan.offset, shares.begin(blockIdx.x),
+                shares.begin(blockIdx.x + 1)};
+    Piece p;
+    for (uint32_t i = 0; w.next(a, kRows, p); ++i) {
+      if (i < n || p.whole()) continue;
+      const int c0 = shares.owner(p.first), c1 = shares.owner(p.first + p.steps - 1);
+      if (atomicAdd(&a.counters[c0], 1) == c1 - c0) a.counters[c0] = 0;
+    }
   }
   if (bad && lane == 0) atomicOr(a.status, (uint32_t)TV_STATUS_TIMEOUT);
 }

@@ -294,5 +294,3 @@ int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream);
 // The same on the tensor cores' large tiles, for many rows (tv_attend_tile.cu).
 size_t tv_attend_tile_scratch(int sm_count);
 int tv_launch_attend_tile(const AttendArgs& a, int sm_count, cudaStream_t stream);
-
-
