@@ -539,7 +539,7 @@ int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int
  *              reported in the status word and the path taken as far as it goes), or NULL: row i
  *              sees rows 0 to i (a piece of a prompt behind what is cached of it).
  *   rows       [B] int32 rows of each request, NULL: R of all; the rows behind are 0 in out.
- *   scale      finite.
+ *   scale      finite, and finite as a float32 when times log2(e).
  *   out        [B][R][heads][head_dim] bf16, 16-byte aligned; must not overlap q.
  * Tokens without a page (TV_STATUS_BAD_PAGE) are left out; a row that sees nothing is 0.
  * The first call allocates the handle's scratch and may not be captured; later ones may.

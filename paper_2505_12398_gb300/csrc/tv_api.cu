@@ -964,7 +964,8 @@ int tv_tree_attention(tv_handle* h, const tv_cache* cache, int layer, int B, int
   if (!h || !cache_args(cache, &a.c) || layer < 0 || layer >= a.c.layers || B < 0 || R < 0)
     return TV_ERR_INVALID_ARG;
   if (heads < a.c.kv_heads || (heads % a.c.kv_heads) != 0) return TV_ERR_INVALID_ARG;
-  if (!std::isfinite(scale)) return TV_ERR_INVALID_ARG;
+  a.scale_log2e = static_cast<float>(1.4426950408889634 * static_cast<double>(scale));
+  if (!std::isfinite(a.scale_log2e)) return TV_ERR_INVALID_ARG;
   if (B > h->max_batch || (parents && R > h->max_nodes + 1)) return TV_ERR_CAPACITY;
   if (B == 0 || R == 0) return TV_OK;
   if (!page_table(lengths, table, max_pages, &a.t) || !q || !out || !aligned16(q) ||
@@ -1002,7 +1003,6 @@ int tv_tree_attention(tv_handle* h, const tv_cache* cache, int layer, int B, int
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.parents = parents;
   a.rows = rows;
-  a.scale_log2e = static_cast<float>(1.4426950408889634 * static_cast<double>(scale));
   a.out = static_cast<__nv_bfloat16*>(out);
   a.part = h->attend_part;
   a.counters = h->attend_counters;
