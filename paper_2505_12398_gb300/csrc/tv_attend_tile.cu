@@ -23,10 +23,12 @@
 // Steps go from the last tokens to the first, so that a row's path to the root is walked once,
 // and the tree's tokens, which rows see in part, come first.
 //
-// A product that overwrites a tile's scores is issued after the one that reads its weights,
-// by the same thread and of the same shape: the tensor cores take them in that order (where
-// the head dimension is 64 their shapes differ, and the first waits for the second).  Every wait
-// is bounded; one that gives up raises the timeout status, and the loops go on to their end.
+// A product that overwrites a tile's scores waits until the one that reads its weights has ended
+// (1 % of the time).  Where a product's operands were not known to be the warp's, its issue took
+// as long as the product: 432 us for 406 at 128 trees of 61 rows over 4096 tokens.  Scores by 64
+// tokens, made while the softmax works on the other 64, took as long (404 us there, but
+// 178 for 172 of prompts): with 64 columns a product is bound by shared memory.  Every wait is
+// bounded; one that gives up raises the timeout status, and the loops go on to their end.
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -51,7 +53,7 @@ constexpr int kMmaWarp = kSoftmaxWarps + kWidenWarps;
 constexpr int kPieceWarp = kMmaWarp + 2;
 constexpr int kTileThreads = 32 * (kPieceWarp + 2);
 // registers per thread after the split
-constexpr int kRegsSoftmax = 136, kRegsWiden = 72, kRegsOther = 64, kRegsLaunch = 96;
+constexpr int kRegsSoftmax = 144, kRegsWiden = 64, kRegsOther = 64, kRegsLaunch = 96;
 static_assert(32 * (kSoftmaxWarps * kRegsSoftmax + kWidenWarps * kRegsWiden + 4 * kRegsOther) <=
                   kTileThreads * kRegsLaunch,
               "the warpgroups' registers fit what the block was launched with");
@@ -107,6 +109,13 @@ __device__ __forceinline__ const Work* take(TileShared& sh, uint32_t n, uint32_t
 __device__ __forceinline__ void give_back(TileShared& sh, uint32_t n) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.taken[n % kPieceSlots]);
+}
+
+// What all lanes of a warp hold alike, known as such to the compiler: a product takes its operands
+// from registers of the whole warp.
+template <typename T>
+__device__ __forceinline__ T uniform(T x) {
+  return __shfl_sync(0xffffffffu, x, 0);
 }
 
 // Descriptors of operands whose rows are 128 bytes with the 128-byte swizzle, in two words:
@@ -314,7 +323,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   uint8_t* const q_tiles = smem;                               // [2]
   uint8_t* const k_tiles = smem + 2 * kTileBytes;              // [kStages]
   uint8_t* const v_tiles = k_tiles + kStages * kTileBytes;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const int rows_of_item = split ? kTile : 2 * kTile;
 
   if (tid == 0) {
@@ -345,7 +354,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = sh.tmem;
+  const uint32_t tmem = uniform(sh.tmem);
   uint32_t bad = 0, taken = 0;                   // pieces so far
 
   if (warp >= kMmaWarp) regs_fewer<kRegsOther>();
@@ -357,7 +366,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
     const uint32_t ts = tmem + x * kTile, to = tmem + 2 * kTile + x * D;
     uint32_t steps_done = 0, count = 0;          // count: weights of this tile taken
     for (; const Work* const w = take(sh, taken, bad); ++taken) {
-      const int n = w->s1 - w->s0, stride = split ? 2 : 1, first = split ? x : 0;
+      const int n = uniform(w->s1 - w->s0), stride = split ? 2 : 1, first = split ? x : 0;
       give_back(sh, taken);
       auto scores = [&](int j) {
         const uint32_t s = steps_done + (uint32_t)j, stage = s % kStages;
@@ -396,7 +405,7 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
           }
           __syncwarp();
         }
-        if (D != kTile) wait_on(&sh.ofull[x][1], count & 1, bad);
+        wait_on(&sh.ofull[x][1], count & 1, bad);
         if (j + stride < n) scores(j + stride);
       }
       steps_done += (uint32_t)n;
