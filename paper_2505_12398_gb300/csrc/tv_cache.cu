@@ -399,6 +399,7 @@ long long move_blocks(const CacheArgs& c) {                 // of a request; bel
 
 bool tv_cache_rows_fit(const CacheArgs& c, int B, int R) {
   const long long most = INT_MAX / kWarps;                  // (a warp's index is an int)
+  if (R > INT_MAX - 2 * kSpan) return false;                // (and a row's, of the last span too)
   const long long blocks = row_blocks(c, R, 8, 1);
   return blocks <= most && blocks <= INT_MAX / (long long)B;
 }

@@ -128,3 +128,18 @@ def test_scales_that_are_no_float32_times_log2e(tv):
             s.cache.attend(0, q, s.lengths, s.table, scale=scale)
         assert e.value.code == -1
     assert s.v.status() == 0
+
+
+def test_more_rows_than_an_index_has_are_refused(tv):
+    """By the host, from sizes alone."""
+    s = Setup(tv, [20], 1, 1, 64, 16)
+    lib, z = s.v.lib, None
+    at = s.cache.data.data_ptr()
+    n, t = s.lengths.data_ptr(), s.table.data_ptr()
+    pages = s.table.shape[1]
+    for rows in (2 ** 31 - 1, 2 ** 31 - 10):
+        assert lib.tv_cache_read(s.v.handle, s.cache.ref, 0, 1, rows, 0, n, t, pages, z, at, at,
+                                 z) == -1
+        assert lib.tv_cache_write(s.v.handle, s.cache.ref, 0, 1, rows, 0, at, at, n, t, pages, z,
+                                  z) == -1
+    assert s.v.status() == 0
