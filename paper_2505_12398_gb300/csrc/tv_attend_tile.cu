@@ -617,6 +617,8 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
             const float top = in ? f * fmaxf(top2[0], top2[1]) : TV_NEG_INF;
             // weights are relative to what the largest score was, until it has grown too far
             if (__any_sync(0xffffffffu, top > mref + kSlack)) {
+              // (the next scores are on their way to registers that a call may move)
+              if (k < 3) tmem_wait(c[(k + 1) & 1]);
               float down = 1.f;
               if (top > mref) {
                 down = ex2(mref - top);
