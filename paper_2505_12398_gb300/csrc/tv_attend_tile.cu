@@ -690,9 +690,11 @@ __global__ void __launch_bounds__(kTileThreads, 1) tile_kernel(AttendArgs a, int
       if (split) {
         sh.m[x][r] = x < ops ? mref : TV_NEG_INF;
         sh.l[x][r] = x < ops ? l : 0.f;
+        tc_fence_before();                       // (each tile's threads read both tiles' sums)
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.merge);
         wait_on(&sh.merge, merged++ & 1, bad);
+        tc_fence_after();
         const float m0 = sh.m[0][r], m1 = sh.m[1][r];
         mref = fmaxf(m0, m1);
         fac[0] = m0 == TV_NEG_INF ? 0.f : ex2(m0 - mref);

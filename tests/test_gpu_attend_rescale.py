@@ -62,3 +62,22 @@ def test_rows_whose_largest_score_grows_beside_others(tv, d, G, R, lens):
     check(s, q, R, scale=1.0, held=held)
     if R <= 64:
         check(s, q, R, parents=[tree(R, b) for b in range(len(lens))], scale=1.0, held=held)
+
+
+@pytest.mark.parametrize("d,G,R,lens", [
+    (128, 4, 32, [1500, 1370]), (64, 4, 20, [1500, 1370]), (128, 1, 27, [900, 31]),
+    (128, 16, 1, [1000, 5, 700]), (128, 4, 20, [120 * i + 7 * i % 50 for i in range(12)]),
+    (64, 1, 61, [40 * i + 7 * i % 50 for i in range(100)])])
+def test_two_sums_of_the_same_rows(tv, d, G, R, lens):
+    """Up to 128 rows: both tiles hold sums of the same rows over alternate steps, scaled apart
+    and then joined, each half of the columns by another tile's threads."""
+    s = Setup(tv, lens, R, 1, d, 64, seed=3)
+    held = rising(s, R)
+    q = mixed_queries(len(lens), R, G, d)
+    parents = [tree(R, b) for b in range(len(lens))]
+    check(s, q, R, parents=parents, scale=1.0, held=held)
+    check(s, q, R, scale=1.0, held=held)
+    qd = q.cuda()
+    first = s.cache.attend(0, qd, s.lengths, s.table, scale=1.0)
+    for _ in range(20):
+        assert torch.equal(first, s.cache.attend(0, qd, s.lengths, s.table, scale=1.0))
