@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(32 * kWarps)
     if (len < 0) return;
   }
   const int off = part.span * kSpan - (len & (kSpan - 1));  // of the span's first position
-  if (off >= r) return;
+  if (off >= r || r == 0) return;                           // (off may be negative)
   const int i = off + (lane >> 2);                          // this lane's row
   const bool mine = i >= 0 && i < r;
   const int slot = (int)((unsigned)len + (unsigned)i) & (c.page_size - 1);

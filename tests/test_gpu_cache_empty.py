@@ -1,0 +1,39 @@
+"""Requests of a batch for which there is nothing to write to the 4-bit cache or to read from it:
+they have no pages, their lengths are whatever an idle slot holds, and nothing is reported."""
+
+import pytest
+import torch
+
+from tests.cache_setup import Setup
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tv():
+    import paper_2505_12398_gb300 as tv
+    from paper_2505_12398_gb300.build import build
+    build()
+    return tv
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("R", [5, 3000])
+def test_no_rows_to_write(tv, dtype, R):
+    """Row counts of 0 behind lengths that do and do not begin a run of 8 positions."""
+    lens = [13, 0, 8, 127, 2 ** 31 - 3, 20, 1, 15]
+    s = Setup(tv, [20] * len(lens), R, 8, 64, 16)
+    k = s.rows(R, dtype).cuda()
+    before = s.cache.data.clone()
+    gone = torch.full_like(s.table, -1)
+    s.cache.write(0, k, k, ints(lens), gone, rows=ints([0] * len(lens)))
+    assert s.v.status() == 0
+    assert torch.equal(s.cache.data, before)
+    rows = ints([0, 0, 0, 0, 0, 2, 0, 0])            # (one request has some, and no pages)
+    s.cache.write(0, k, k, ints(lens), gone, rows=rows)
+    assert tv.status_names(s.v.status()) == ["BAD_PAGE"]
+    assert torch.equal(s.cache.data, before)
