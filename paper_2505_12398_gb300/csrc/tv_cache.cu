@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(32 * kWarps)
   const int off = part.span * kSpan - (start & (kSpan - 1));
   const int i = off + (lane >> 2);
   int page = -1;
-  if (off < count) {
+  if (count > 0 && off < count) {                                      // (off may be negative)
     page = page_of(c, t, b, (int)((unsigned)start + (unsigned)off));
     if (page < 0 && lane == 0) atomicOr(status, (uint32_t)TV_STATUS_BAD_PAGE);
   }
