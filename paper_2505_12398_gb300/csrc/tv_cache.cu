@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(32 * kWarps)
   if ((len < 0 || from < 0) && part.span == 0 && part.strip == 0 && lane == 0)
     atomicOr(status, (uint32_t)TV_STATUS_BAD_LENGTH);
   const int start = max(from, 0);
-  const int count = min(max(from < 0 ? 0 : len - start, 0), n);       // rows that are read
+  const int count = from < 0 || len <= start ? 0 : min(len - start, n);  // rows that are read
   const int off = part.span * kSpan - (start & (kSpan - 1));
   const int i = off + (lane >> 2);
   int page = -1;

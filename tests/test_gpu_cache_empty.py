@@ -59,3 +59,16 @@ def test_nothing_to_read(tv, dtype, n):
     assert np.array_equal(gk[7, :m].double().cpu().numpy(), s.want(k, 0, 0)[7, :m])
     assert np.array_equal(gv[7, :m].double().cpu().numpy(), s.want(k, 0, 1)[7, :m])
     assert not bool(gk[7, m:].any()) and not bool(gv[7, m:].any())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_lowest_lengths_are_empty(tv, dtype):
+    """Negative lengths, so low that first positions taken from them pass 32 bits."""
+    s = Setup(tv, [20] * 4, 0, 2, 64, 16)
+    s.fill()
+    first = ints([1, 5, 19, 2 ** 31 - 1])
+    for low in (-2 ** 31, -2 ** 31 + 3, -1):
+        gk, gv = s.cache.read(0, torch.full_like(first, low), s.table, 12, first=first,
+                              dtype=dtype)
+        assert tv.status_names(s.v.status()) == ["BAD_LENGTH"]
+        assert not bool(gk.any()) and not bool(gv.any())
