@@ -541,7 +541,8 @@ int tv_cache_accept(tv_handle* h, const tv_cache* cache, int B, int N, const int
  *   rows       [B] int32 rows of each request, NULL: R of all; the rows behind are 0 in out.
  *   scale      finite, and finite as a float32 when times log2(e).
  *   out        [B][R][heads][head_dim] bf16, 16-byte aligned; must not overlap q.
- * Tokens without a page (TV_STATUS_BAD_PAGE) are left out; a row that sees nothing is 0.
+ * Tokens without a page (TV_STATUS_BAD_PAGE) are left out; a row that sees nothing is 0; one
+ * with a score that is no float32 when times log2(e) is undefined.
  * The first call allocates the handle's scratch and may not be captured; later ones may.
  * Errors: TV_ERR_INVALID_ARG, TV_ERR_CAPACITY, TV_ERR_CUDA.
  */

@@ -248,7 +248,8 @@ struct QueryScale {
   // row that is not finite
   __device__ __forceinline__ float factor(float scale_log2e, int key_exponent) const {
     const int n = e + key_exponent, half = n / 2;
-    const float f = scale_log2e * pow2i(half) * pow2i(n - half);
+    const float most = 3.4028234e38f;              // (0 times an infinity would be no score)
+    const float f = fminf(fmaxf(scale_log2e * pow2i(half) * pow2i(n - half), -most), most);
     return finite ? f : __int_as_float(0x7fffffff);
   }
 };
