@@ -52,7 +52,7 @@ constexpr int kWarps = 8;
 constexpr int kThreads = 32 * (kWarps + 1);      // and the copying warp
 constexpr int kUnit = 16;                        // tokens of a warp's step
 static_assert(kStep == kUnit * kWarps, "a step is 16 tokens of each warp");
-constexpr int kMaxNodes = 1024;                  // rows of a tree
+constexpr int kMaxRows = 16;                     // rows of an item, and so of a tree
 constexpr int kPerSm = 2;
 
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
@@ -128,10 +128,10 @@ struct alignas(16) Shared {
   uint32_t valid[8];                             // the pages of a step that are there
   Schedule plan;
   int last;
-  float m[kWarps][32], l[kWarps][32];
-  float fac[kWarps][32], sum[32], top[32];
-  int32_t parents[kMaxNodes];
-  uint32_t seen[32][kMaxNodes / 32];             // tree rows that a tile's rows see
+  float m[kWarps][kMaxRows], l[kWarps][kMaxRows];
+  float fac[kWarps][kMaxRows], sum[kMaxRows], top[kMaxRows];
+  int32_t parents[kMaxRows];
+  uint32_t seen[kMaxRows];                       // bit j: an item's row sees the tree's row j
 };
 
 static_assert(sizeof(Shared) % 16 == 0, "the sums behind it are read 16 bytes at a time");
@@ -139,6 +139,7 @@ static_assert(sizeof(Shared) % 16 == 0, "the sums behind it are read 16 bytes at
 template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) {
   constexpr int kRows = 8 * NT;
+  static_assert(kRows <= kMaxRows, "");
   constexpr int kDT = D / 16;                    // column tiles of O^T
   constexpr int kKS = D / 16;                    // products of S^T
   constexpr int kPitch = D + 4;
@@ -237,14 +238,14 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
     const int len = p.rq.len, nrows = p.rq.rows, tokens = p.tokens;
     const bool masked = (long long)s1 * kStep > len;       // some tokens are the tree's
     if (masked && a.parents) {
-      const int words = (nrows + 31) / 32;
-      for (int i = tid; i < nrows; i += 32 * kWarps) sh.parents[i] = a.parents[(size_t)b * a.R + i];
-      for (int i = tid; i < kRows * words; i += 32 * kWarps) sh.seen[i / words][i % words] = 0u;
+      if (tid < nrows) sh.parents[tid] = a.parents[(size_t)b * a.R + tid];
       consumers();
-      if (tid < kRows && m0 + tid < nrows * G) {
-        if (!walk(sh.parents, (m0 + tid) / G,
-                  [&](int j) { sh.seen[tid][j >> 5] |= 1u << (j & 31); }))
+      if (tid < kRows) {
+        uint32_t seen = 0;
+        if (m0 + tid < nrows * G &&
+            !walk(sh.parents, (m0 + tid) / G, [&](int j) { seen |= 1u << j; }))
           atomicOr(a.status, (uint32_t)TV_STATUS_BAD_TREE);
+        sh.seen[tid] = seen;
       }
       consumers();
     }
@@ -365,8 +366,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) attend_kernel(AttendArgs a) 
             const int at = pos + g + (k & 2) * 4 - len, row = 8 * n + 2 * t + (k & 1);
             bool on = at < 0;
             if (!on && at < nrows && at + len < tokens)
-              on = a.parents ? (sh.seen[row][at >> 5] >> (at & 31) & 1u) != 0u
-                             : at <= (m0 + row) / G;
+              on = a.parents ? (sh.seen[row] >> at & 1u) != 0u : at <= (m0 + row) / G;
             x = on ? x : TV_NEG_INF;
           }
           st[n][k] = x;
@@ -566,15 +566,16 @@ int launch(const AttendArgs& a, int sm_count, cudaStream_t stream) {
 using namespace tvk::attend;
 
 size_t tv_attend_scratch(int sm_count) {
-  // two pieces of each CTA, of 32 rows of 64 columns or 16 of 128 (and their statistics)
-  const size_t few = (size_t)kPerSm * sm_count * 2 * (16 * 128 + 2 * 32) * sizeof(float);
+  // two pieces of each CTA, of 16 rows of 64 columns or 8 of 128 (and their statistics)
+  const size_t few =
+      (size_t)kPerSm * sm_count * 2 * (kMaxRows * 64 + 2 * kMaxRows) * sizeof(float);
   return std::max(few, tv_attend_tile_scratch(sm_count));
 }
 int tv_attend_counters(int sm_count) { return kPerSm * sm_count; }
 
 int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const long long rows = (long long)a.R * a.group;
-  const int most = a.c.head_dim == 128 ? 8 : 16;
+  const int most = a.c.head_dim == 128 ? 8 : kMaxRows;
   if (rows > most) return tv_launch_attend_tile(a, sm_count, stream);
   if (a.c.head_dim == 128) return launch<128, 1>(a, sm_count, stream);
   return rows <= 8 ? launch<64, 1>(a, sm_count, stream) : launch<64, 2>(a, sm_count, stream);

@@ -223,12 +223,6 @@ __device__ __forceinline__ void zero_rows(const AttendArgs& a, int D, int me, in
   }
 }
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-
 // Scales a row of queries whose largest magnitude is `top` by a power of two, to [2^14, 2^15)
 // (or, of subnormal ones, as near as the exponent of the least normal one brings it).
 struct QueryScale {

@@ -34,12 +34,6 @@ namespace cache {
 constexpr int kWarps = 8;
 constexpr int kSpan = 8;                 // positions of a warp
 
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-
 // 16 consecutive elements, 16-byte aligned, as they come.
 template <typename T>
 struct Row16 {

@@ -78,5 +78,11 @@ __device__ __forceinline__ float2 widen(uint32_t h) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
 }  // namespace cache
 }  // namespace tvk
