@@ -16,8 +16,12 @@
 // positions, aligned to 8 so that they lie in one page, 4 lanes for each: a lane loads 16
 // columns, the four whole lines of a row, or stores 32 bytes, the four a line; the codes of a
 // chunk's 8 positions are 128 consecutive bytes.  (With a chunk of 32 columns for each lane the
-// stores of fp32 rows went to 32 lines at once, and the kernel was bound by L1: 226 us for 179
-// at 32 requests of 4096 rows of 8 heads, 5.1 TB/s, 0.76 of what a copy reaches.)
+// stores of fp32 rows went to 32 lines at once, and the kernel was bound by L1: 226 us for 178
+// at 32 requests of up to 4096 rows of 8 heads of 128 columns.)  With the zeros behind the shorter
+// requests that is 6.7 TB/s, 0.98 of what a copy reaches; in bf16 100 us, 0.96.  16 x 2048 rows of
+// bf16 are written in 34 us and read in 31, 5.0 and 5.5 TB/s (0.74 and 0.81), and of fp32 in 58
+// and 52 (0.78 and 0.88): calls so short are mostly waits of loads and instructions, at 0.6 to 0.8
+// of the issue slots.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -380,7 +384,17 @@ long long row_blocks(const CacheArgs& c, int rows, int cols, int per) {
   return (spans_of(rows) * ((strips + per - 1) / per) + kWarps - 1) / kWarps;   // below 2^45
 }
 // Strips of a warp: with many warps several, which share what finds their rows and have their
-// loads on the way together; with few one, so that more SMs have some.
+// loads on the way together; with few one, so that more SMs have some.  Times in us with one and
+// with four, requests of 61 rows (the last of 2048), 8 heads of 128 columns:
+//     requests           8          16          32          64         128    16 of 2048
+//     blocks of one    288         576        1152        2304        4608        16448
+//     write, bf16  2.7 3.3     3.3 3.3     4.7 4.1     7.2 6.2    12.5 9.7      41  34
+//     read, bf16   2.9 3.2     3.5 3.3     5.0 4.0     7.6 5.2    12.9 8.3      44  31
+//     write, fp32  3.6 5.8     4.6 5.8     6.4 7.3     9.9 12.8   16.9 22.2     58  77
+//     read, fp32   3.3 3.4     4.5 4.0     7.2 5.2    12.0 7.7    22.3 12.6     77  52
+// (fp32 reads have twice the blocks).  Rows of fp32 are written one strip a warp at any size: four
+// take 97 registers a thread, which leaves 2 CTAs an SM, and one already fills 0.81 of the issue
+// slots, mostly with divisions.
 constexpr int kSeveral = 4;
 constexpr long long kManyBlocks = 1024;
 bool several(const CacheArgs& c, int B, int rows, int cols) {
@@ -425,13 +439,12 @@ void launch_read(const CacheArgs& c, const PageTable& t, int layer, int B, int n
 int tv_launch_cache_write(const CacheArgs& c, const PageTable& t, int layer, int B, int R,
                           int is_bf16, const void* k, const void* v, const int32_t* rows,
                           uint32_t* status, cudaStream_t stream) {
-  const bool many = several(c, B, R, kGroup);
-  if (is_bf16)
-    many ? launch_write<__nv_bfloat16, kSeveral>(c, t, layer, B, R, k, v, rows, status, stream)
-         : launch_write<__nv_bfloat16, 1>(c, t, layer, B, R, k, v, rows, status, stream);
+  if (!is_bf16)
+    launch_write<float, 1>(c, t, layer, B, R, k, v, rows, status, stream);
+  else if (several(c, B, R, kGroup))
+    launch_write<__nv_bfloat16, kSeveral>(c, t, layer, B, R, k, v, rows, status, stream);
   else
-    many ? launch_write<float, kSeveral>(c, t, layer, B, R, k, v, rows, status, stream)
-         : launch_write<float, 1>(c, t, layer, B, R, k, v, rows, status, stream);
+    launch_write<__nv_bfloat16, 1>(c, t, layer, B, R, k, v, rows, status, stream);
   return cudaGetLastError() == cudaSuccess ? 0 : -5;
 }
 
