@@ -28,10 +28,11 @@
 // consecutive steps, found from the lengths on the device.  An item that spans CTAs is joined by
 // the last of them to finish, in the order of its pieces.
 //
-// 128 requests of 8192 tokens, 8 heads of 128 columns, 4 query heads each: 218 us, 4.1 TB/s of
-// the cache (0.61 of what a copy reaches).  More than 8 rows (16 of 64 columns) are faster on
-// the tiles of tv_attend_tile.cu: 32 trees of 27 rows over 3001 tokens, 16 heads of 64 columns,
-// 150 us here, 92 there.
+// 128 requests of up to 8192 tokens, 8 heads of 128 columns, 4 query heads each: 211 to 218 us, 4.1
+// to 4.3 TB/s of the cache (0.61 to 0.63 of what a copy reaches).  Nine warps twice an SM leave a
+// thread 96 registers, and all three forms spill to local memory: 96 bytes stored and 208 loaded
+// by a thread at 128 columns, 28 and 28 with 8 rows of 64, 144 and 280 with 16.  More rows go to
+// the tiles of tv_attend_tile.cu (tv_launch_attend has both sides' times).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -573,6 +574,18 @@ size_t tv_attend_scratch(int sm_count) {
 }
 int tv_attend_counters(int sm_count) { return kPerSm * sm_count; }
 
+// Times in us by warps and on the tiles (8 heads, pages of 64; 1 x 2000 is one request of 2000
+// tokens, 32 x 1000 are requests of 500 to 1000, 128 x 4096 of 2048 to 4096), rows as query heads
+// of one token; a tree's rows take up to 3 % more by warps, on the tiles up to 8 % (37 % at 64
+// columns).  9 rows and more of 128 columns, and 24 and 32 of 64, were timed by warps in forms that
+// are not kept.  The rule's worst place is one short request of 9 to 16 rows of 128 columns.
+//                  rows     1 x 2000    1 x 131000    32 x 1000    128 x 4096
+//     128 columns   1, 4     11   18       51   81        23   38     119  232
+//                   8        12   18       51   81        23   40     120  233
+//                   9, 16    18   22      165   87        59   41     403  238
+//      64 columns   4, 8     11   15       38   59        19   31      82  183
+//                   9, 16    13   15       50   60        25   32     126  185
+//                  24, 32    22   15      218   61        77   32     630  188
 int tv_launch_attend(const AttendArgs& a, int sm_count, cudaStream_t stream) {
   const long long rows = (long long)a.R * a.group;
   const int most = a.c.head_dim == 128 ? 8 : kMaxRows;
