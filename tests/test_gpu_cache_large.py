@@ -1,6 +1,7 @@
 """Large writes to the 4-bit cache and large reads of it, whose warps take four strips of a row
-each: against the float64 restatement and against small calls, both exactly, with ragged rows and
-lengths inside a run of 8 positions; and outputs at 16 bytes that are not 32."""
+each (but for writes of fp32): against the float64 restatement and against small calls, both
+exactly, with ragged rows and lengths inside a run of 8 positions; and outputs at 16 bytes that
+are not 32."""
 
 import numpy as np
 import pytest
